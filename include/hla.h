@@ -359,6 +359,106 @@ int ahla_forward(const void *q, const void *k, const void *v, float *out,
                  int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * The operators around the attention.  Their conventions differ from the
+ * above where said:
+ *   - Activations come as a projection leaves them, token by token: x
+ *     [B, n, ...] with the elements of a token contiguous and any strides
+ *     >= 0 between batches (_bs) and tokens (_ts), in elements (a stride of 0
+ *     repeats a row; the stride of a dimension of size one is not used).
+ *     Outputs are contiguous and must not alias inputs.
+ *   - Outputs and gradients have the type of what they belong to (`dtype`,
+ *     `w_dtype`, `dt_dtype`: HLA_FP32 or HLA_BF16), states of the scan and its
+ *     per-head parameters are fp32.  All arithmetic is fp32 or better, rounded
+ *     once on the way out unless said otherwise.
+ *   - A pointer said to be optional may be NULL.
+ * ------------------------------------------------------------------------- */
+
+/* hla_conv_forward — short causal convolution along the tokens:
+ *   z[b,t,c] = bias[c] + sum_{j<K} weight[c,j] x[b,t-K+1+j,c],
+ *   y = z sigmoid(z) with silu = 1, else z.
+ * x [B, n, D]; weight [D, K], bias [D] (optional) of w_dtype; y [B, n, D].
+ * state (optional) [B, K-1, D] of dtype: the K-1 inputs before the first,
+ * oldest first; replaced by the last K-1 inputs of [state; x].  Without it
+ * they are zeros.  One call with n = 1 is a decode step.
+ * K in {2, 3, 4}, any D, n <= 2^22, B <= 65535.  Pointers need the alignment
+ * of their type; rows in whole 16-byte pieces (base, strides and D) are
+ * faster. */
+int hla_conv_forward(const void *x, long long x_bs, long long x_ts, const void *weight, const void *bias,
+                     void *state, void *y, int B, int n, int D, int K, int silu, int dtype, int w_dtype,
+                     void *stream);
+
+/* hla_conv_backward — gradients of hla_conv_forward without a state: dx
+ * [B, n, D], dweight [D, K] and dbias [D] (optional) for dy [B, n, D].
+ * workspace: at least hla_conv_backward_workspace_bytes(...) bytes. */
+size_t hla_conv_backward_workspace_bytes(int B, int n, int D, int K);
+int hla_conv_backward(const void *x, long long x_bs, long long x_ts, const void *weight, const void *bias,
+                      const void *dy, long long dy_bs, long long dy_ts, void *dx, void *dweight, void *dbias,
+                      int B, int n, int D, int K, int silu, int dtype, int w_dtype, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/* hla_qk_norm_rope — norm and position rotation of queries and keys, head by
+ * head, from q [B, n, H, d] and k [B, n, Hk, d] (the heads of a token
+ * contiguous) to q_out [B, H, n, d] and k_out [B, Hk, n, d]:
+ *   u = weight x / sqrt(mean(x^2) + eps),
+ *   (u_i, u_j) -> (u_i c - u_j s, u_j c + u_i s), c = cos[p, m], s = sin[p, m],
+ * for the m-th pair of the first rot dimensions: (i, j) = (m, m + rot/2), or
+ * (2m, 2m + 1) with interleaved = 1; the other dimensions keep u.
+ * q_weight, k_weight (optional) [d]; cos, sin fp32 [positions, rot/2] (unused
+ * with rot = 0).  p: pos[b, t] (optional; int64 with pos64 = 1, else int32;
+ * pos_bs elements between batches, 0 for one row for all), without it t.  A
+ * position outside [0, positions) gives NaN in the rotated dimensions.
+ * d: a multiple of 8 from 16 to 256; rot even.  q, k and the outputs are
+ * 16-byte aligned with strides of whole 16-byte pieces. */
+int hla_qk_norm_rope(const void *q, long long q_bs, long long q_ts, const void *k, long long k_bs,
+                     long long k_ts, const void *q_weight, const void *k_weight, const float *cos,
+                     const float *sin, const void *pos, long long pos_bs, void *q_out, void *k_out, int B,
+                     int n, int H, int Hk, int d, int rot, int positions, int interleaved, float eps,
+                     int dtype, int w_dtype, int pos64, void *stream);
+
+/* hla_qk_norm_rope_backward — its gradients: dq [B, n, H, d], dk [B, n, Hk, d]
+ * and dq_weight, dk_weight [d] (optional) for dq_out [B, H, n, d] and dk_out
+ * [B, Hk, n, d], both contiguous.  workspace: at least
+ * hla_qk_norm_rope_backward_workspace_bytes(d) bytes. */
+size_t hla_qk_norm_rope_backward_workspace_bytes(int d);
+int hla_qk_norm_rope_backward(const void *q, long long q_bs, long long q_ts, const void *k, long long k_bs,
+                              long long k_ts, const void *q_weight, const void *k_weight, const float *cos,
+                              const float *sin, const void *pos, long long pos_bs, const void *dq_out,
+                              const void *dk_out, void *dq, void *dk, void *dq_weight, void *dk_weight,
+                              int B, int n, int H, int Hk, int d, int rot, int positions, int interleaved,
+                              float eps, int dtype, int w_dtype, int pos64, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* hla_ssm_forward — selective state space scan with a scalar decay a head:
+ *   dt_t = softplus(dt[b,t,h] + dt_bias[h])  (without the softplus: softplus = 0),
+ *   h_t = exp(dt_t A[h]) h_{t-1} + dt_t Bm_t x_t^T,   y_t = h_t^T Cm_t + D[h] x_t.
+ * x [B, n, H, P] (the heads of a token contiguous), dt [B, n, H] of dt_dtype,
+ * Bm, Cm [B, n, G, N]: head h reads group h / (H / G); A, D (optional),
+ * dt_bias (optional) fp32 [H]; y [B, n, H, P].  state (optional) fp32
+ * [B, H, N, P]: the state before the first token, replaced by the one after
+ * the last; without it the scan starts from zero.
+ * P and N: multiples of 16 from 16 to 128; G divides H; B*H <= 65535;
+ * B*H*n < 2^31.  A <= 0 is meant (a growing state may overflow).  x, Bm, Cm:
+ * 16-byte aligned, strides of whole 16-byte pieces.  bf16 inputs: scores and
+ * the state that the outputs read are rounded to bf16 (2^-9 of a term, as the
+ * outputs are), the state itself is kept in fp32.  An infinite or NaN input
+ * gives NaN in every output that depends on it, and in no other.
+ * workspace: at least hla_ssm_workspace_bytes(...) bytes. */
+size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype);
+int hla_ssm_forward(const void *x, long long x_bs, long long x_ts, const void *dt, long long dt_bs,
+                    long long dt_ts, const float *A, const void *Bm, long long b_bs, long long b_ts,
+                    const void *Cm, long long c_bs, long long c_ts, const float *D, const float *dt_bias,
+                    float *state, void *y, int B, int n, int H, int P, int G, int N, int softplus,
+                    int dtype, int dt_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* hla_ssm_step — one token of it for every head, the state updated in place:
+ * x [B, H, P], dt [B, H], Bm, Cm [B, G, N], y [B, H, P]; strides between
+ * batches only.  No workspace. */
+int hla_ssm_step(float *state, const void *x, long long x_bs, const void *dt, long long dt_bs, const float *A,
+                 const void *Bm, long long b_bs, const void *Cm, long long c_bs, const float *D,
+                 const float *dt_bias, void *y, int B, int H, int P, int G, int N, int softplus, int dtype,
+                 int dt_dtype, void *stream);
+
+/* ---------------------------------------------------------------------------
  * Benchmark timing.  hla_profile_begin(max_records) creates 2*max_records HIP
  * events (host objects, no device memory) and starts bracketing every kernel
  * the library launches with events recorded on that kernel's stream;

@@ -20,6 +20,7 @@ _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
+_L = ctypes.c_longlong
 _Z = ctypes.c_size_t
 
 
@@ -32,6 +33,7 @@ class HLA2State(ctypes.Structure):
 
 _SP = ctypes.POINTER(HLA2State)
 _ZP = ctypes.POINTER(_Z)
+_ROWS = [_P, _L, _L]      # a row-strided tensor: address, elements between batches, between tokens
 _IP = ctypes.POINTER(_I)
 
 _SIGS = {
@@ -66,6 +68,16 @@ _SIGS = {
     "ahla_forward": (_I, [_P, _P, _P, _P] + [_I] * 7 + [_F, _I, _P, _Z, _P]),
     "hla3_workspace_bytes": (_Z, [_I] * 7),
     "hla3_forward": (_I, [_P, _P, _P, _P] + [_I] * 8 + [_F, _I, _P, _Z, _P]),
+    "hla_conv_forward": (_I, _ROWS + [_P] * 4 + [_I] * 7 + [_P]),
+    "hla_conv_backward_workspace_bytes": (_Z, [_I] * 4),
+    "hla_conv_backward": (_I, _ROWS + [_P] * 2 + _ROWS + [_P] * 3 + [_I] * 7 + [_P, _Z, _P]),
+    "hla_qk_norm_rope": (_I, _ROWS * 2 + [_P] * 5 + [_L] + [_P] * 2 + [_I] * 8 + [_F] + [_I] * 3 + [_P]),
+    "hla_qk_norm_rope_backward_workspace_bytes": (_Z, [_I]),
+    "hla_qk_norm_rope_backward": (_I, _ROWS * 2 + [_P] * 5 + [_L] + [_P] * 6 + [_I] * 8 + [_F] + [_I] * 3 +
+                                  [_P, _Z, _P]),
+    "hla_ssm_workspace_bytes": (_Z, [_I] * 7),
+    "hla_ssm_forward": (_I, _ROWS * 2 + [_P] + _ROWS * 2 + [_P] * 4 + [_I] * 9 + [_P, _Z, _P]),
+    "hla_ssm_step": (_I, [_P] + [_P, _L] * 2 + [_P] + [_P, _L] * 2 + [_P] * 3 + [_I] * 8 + [_P]),
 }
 
 
@@ -232,6 +244,44 @@ def hla3_workspace_bytes(B, H, n, d, dv, chunk, dtype):
 def hla3_forward(q, k, v, out, B, H, n, d, dv, chunk, masked, normalized, eps, dtype, ws, ws_bytes, stream):
     return _call("hla3_forward", q, k, v, out, B, H, n, d, dv, chunk, masked, normalized, eps, dtype, ws,
                  ws_bytes, stream)
+
+
+# The operators around the attention take many arguments: they are passed on as
+# include/hla.h lists them.
+def hla_conv_forward(*args):
+    return _call("hla_conv_forward", *args)
+
+
+def hla_conv_backward_workspace_bytes(B, n, D, K):
+    return lib().hla_conv_backward_workspace_bytes(B, n, D, K)
+
+
+def hla_conv_backward(*args):
+    return _call("hla_conv_backward", *args)
+
+
+def hla_qk_norm_rope(*args):
+    return _call("hla_qk_norm_rope", *args)
+
+
+def hla_qk_norm_rope_backward_workspace_bytes(d):
+    return lib().hla_qk_norm_rope_backward_workspace_bytes(d)
+
+
+def hla_qk_norm_rope_backward(*args):
+    return _call("hla_qk_norm_rope_backward", *args)
+
+
+def hla_ssm_workspace_bytes(B, n, H, P, G, N, dtype):
+    return lib().hla_ssm_workspace_bytes(B, n, H, P, G, N, dtype)
+
+
+def hla_ssm_forward(*args):
+    return _call("hla_ssm_forward", *args)
+
+
+def hla_ssm_step(*args):
+    return _call("hla_ssm_step", *args)
 
 
 def hla_profile_begin(max_records):

@@ -1,0 +1,136 @@
+// Selective state space scan, a scalar decay a head:
+//   dt_t = softplus(raw_t + bias),  h_t = 2^(l_t) h_{t-1} + dt_t B_t x_t^T,
+//   l_t = dt_t A log2 e,            y_t = h_t^T C_t + D x_t
+// over tiles of Q tokens (64; fp32 inputs 32): with L_t the tile's running sum of l and h the state before the tile,
+//   y_t = 2^(L_t) h^T C_t + sum_{s <= t} 2^(L_t - L_s) dt_s (C_t . B_s) x_s + D x_t
+//   h  <- 2^(L_end) h + sum_s B_s (2^(L_end - L_s) dt_s x_s)^T.
+// Every exponent is a difference within the tile, so nothing overflows for A <= 0.
+//
+// A head's tiles are cut into segments so that the walks fill the chip: the
+// end state of each segment from zero, then one walk a segment from its true
+// state, the decayed sum of the earlier ends (Fig. 1C's two levels with a
+// scalar decay).  The state stays in MFMA accumulators for the whole walk;
+// k_ssm_steps makes each token's dt, L and weights once for all walks.
+#include "ssm_walk.h"
+#include "profile.h"
+
+namespace hla {
+namespace {
+
+// A wave: 64 tokens of one (sequence, head).  Sums in fp64: L reaches the
+// hundreds, where fp32 sums would put 1e-5 into the weights of neighbours.
+template <int Q>
+__global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab, float* __restrict__ tot, int tok,
+                                                   int tiles) {
+  const int wv = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
+  const int head = wv % a.H, blk = (wv / a.H) % (tok / 64), b = wv / a.H / (tok / 64);
+  if (b >= a.B) return;
+  const int t = blk * 64 + lane, bh = b * a.H + head;
+  float dt = 0.f;
+  double la = 0.0;
+  if (t < a.n) {
+    dt = load_any(a.dt.p, a.dt_dtype, (size_t)(b * a.dt.bs + t * a.dt.ts + head));
+    if (a.dt_bias) dt += a.dt_bias[head];
+    if (a.softplus) dt = dt > 20.f ? dt : log1pf(expf(dt));
+    la = (double)dt * (double)a.A[head] * 1.4426950408889634;
+  }
+  double L = la;
+#pragma unroll
+  for (int m = 1; m < Q; m *= 2) {
+    const double o = __shfl_up(L, m, Q);
+    if ((lane & (Q - 1)) >= m) L += o;
+  }
+  const double end = __shfl(L, Q - 1, Q);
+  Step s;
+  s.Lh = (float)L;
+  s.Ll = (float)(L - (double)s.Lh);
+  s.dt = dt;
+  s.w = dt * exp2_((float)(end - L));
+  tab[(size_t)bh * tok + t] = s;
+  if ((lane & (Q - 1)) == Q - 1 && t / Q < tiles) tot[(size_t)bh * tiles + t / Q] = (float)end;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+int tile_of(int dtype) { return dtype == 1 ? Kind<bf16>::Q : Kind<float>::Q; }
+
+}  // namespace
+
+bool ssm_sizes_ok(int P, int N) { return P >= 16 && P <= 128 && P % 16 == 0 && N >= 16 && N <= 128 && N % 16 == 0; }
+
+// Segments a head: walks for two workgroups a CU, each of at least four tiles.
+SsmPlan ssm_plan(int BH, int n, int Q) {
+  SsmPlan p;
+  p.tiles = (n + Q - 1) / Q;
+  int segs = BH >= 512 ? 1 : (512 + BH - 1) / BH;
+  if (segs > p.tiles / 4) segs = p.tiles / 4;
+  if (segs < 1) segs = 1;
+  p.per = (p.tiles + segs - 1) / segs;
+  p.segs = (p.tiles + p.per - 1) / p.per;
+  return p;
+}
+
+struct SsmWs {
+  Step* tab;
+  float *tot, *ends, *segdec;
+  size_t bytes;
+};
+static SsmWs carve(void* ws, int BH, int n, int P, int N, int Q) {
+  const SsmPlan p = ssm_plan(BH, n, Q);
+  const size_t tok = (size_t)(n + 63) / 64 * 64;
+  char* c = static_cast<char*>(ws);
+  SsmWs r;
+  size_t o = 0;
+  r.tab = reinterpret_cast<Step*>(c + o);
+  o += align256(sizeof(Step) * tok * BH);
+  r.tot = reinterpret_cast<float*>(c + o);
+  o += align256(sizeof(float) * (size_t)p.tiles * BH);
+  r.segdec = reinterpret_cast<float*>(c + o);
+  o += align256(sizeof(float) * (size_t)p.segs * BH);
+  r.ends = reinterpret_cast<float*>(c + o);
+  if (p.segs > 1) o += align256(sizeof(float) * (size_t)p.segs * BH * padded(P) * padded(N));
+  r.bytes = o;
+  return r;
+}
+
+size_t ssm_forward_ws(int B, int n, int H, int P, int N, int dtype) {
+  return carve(nullptr, B * H, n, P, N, tile_of(dtype)).bytes;
+}
+
+static hipError_t launch_steps(const Ssm& a, Step* tab, float* tot, int Q, hipStream_t s) {
+  const int tok = (a.n + 63) / 64 * 64, tiles = (a.n + Q - 1) / Q;
+  const long long waves = (long long)a.B * a.H * (tok / 64);
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (Q == 64) return HLA_TIMED("ssm_steps", k_ssm_steps<64>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
+  return HLA_TIMED("ssm_steps", k_ssm_steps<32>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
+}
+
+template <typename T, int NU>
+static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
+  constexpr int Q = Kind<T>::Q;
+  const SsmWs c = carve(ws, a.B * a.H, a.n, a.P, a.N, Q);
+  hipError_t e = launch_steps(a, c.tab, c.tot, Q, s);
+  if (e != hipSuccess) return e;
+  WalkArgs w{};
+  w.x = a.x; w.k = a.Bm; w.q = a.Cm;
+  w.D = a.D; w.tab = c.tab; w.tot = c.tot; w.ends = c.ends; w.segdec = c.segdec;
+  w.state = a.state; w.y = a.y;
+  w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
+  w.plan = ssm_plan(a.B * a.H, a.n, Q);
+  if (w.plan.segs > 1) {
+    w.segs_run = w.plan.segs - 1;
+    e = walk_pn<T, kEnds, NU, false>(w, a.B, s);
+    if (e != hipSuccess) return e;
+  }
+  w.segs_run = w.plan.segs;
+  return walk_pn<T, kOutputs, NU, false>(w, a.B, s);
+}
+
+// The scaled inputs go into the state in three pieces where the state is an
+// output (24 bits: fp32's), in two where only bf16 outputs read it.
+hipError_t launch_ssm_forward(const Ssm& a, void* ws, hipStream_t s) {
+  if (a.dtype != 1) return forward<float, 3>(a, ws, s);
+  return a.state ? forward<bf16, 3>(a, ws, s) : forward<bf16, 2>(a, ws, s);
+}
+
+}  // namespace hla

@@ -1,0 +1,252 @@
+// Device building blocks of the selective state space scan: tiles staged in
+// LDS as bf16 pieces, their MFMA fragments, and the step tables.  Included by
+// the ssm_*.hip files only.
+//
+// An input tile is held as NX bf16 pieces a value: one for bf16 inputs (exact),
+// three for fp32 ones (24 bits).  A product of operands of NA and NB pieces
+// takes the pairs i + j < max(NA, NB), which keeps every product to the
+// accuracy of the coarser operand's last piece.
+#pragma once
+#include "common.h"
+#include "mixer.h"
+#include "vec.h"
+
+namespace hla {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kSsmPad = 16;   // bf16 elements of padding a row: transposed and row reads both spread over the banks
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float nan_() { return __builtin_nanf(""); }
+
+__device__ __forceinline__ rsrc_t rows_rsrc(const void* p, long long bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)(bytes > 0 ? bytes : 0), 0x00020000);
+}
+__device__ __forceinline__ uint4 load16(rsrc_t r, uint32_t off) {
+  const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+// v_mfma_f32_16x16x32_bf16, lane l = 16 g + r:
+//   A: row r, k = 8g .. 8g+7;  B: column r, the same k (any k order that A and
+//   B share);  D: element i is D[4g + i][r].
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+
+template <int NA, int NB>
+__device__ __forceinline__ void mma_pieces(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4& c) {
+  constexpr int M = NA > NB ? NA : NB;
+#pragma unroll
+  for (int s = M - 1; s >= 0; --s)        // the smallest products first
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (s - i >= 0 && s - i < NB) c = mma(a[i], b[s - i], c);
+}
+
+// Eight values in NP pieces, round to nearest.
+template <int NP>
+__device__ __forceinline__ void pieces8(const float (&v)[8], bf16x8 (&p)[NP]) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  uint32_t w[NP][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0 = v[2 * i], x1 = v[2 * i + 1];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      w[k][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){x0, x1}, b2));
+      x0 -= __uint_as_float(w[k][i] << 16);
+      x1 -= __uint_as_float(w[k][i] & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < NP; ++k) p[k] = __builtin_bit_cast(bf16x8, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+}
+template <int NP>
+__device__ __forceinline__ void pieces4(const float (&v)[4], uint2 (&p)[NP]) {
+  float z[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
+  bf16x8 q[NP];
+  pieces8<NP>(z, q);
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    const uint4 u = __builtin_bit_cast(uint4, q[k]);
+    p[k] = make_uint2(u.x, u.y);
+  }
+}
+
+// Fragments of a row-major LDS tile X[row][k] of row stride ld.
+// frag: row row0 + r, k0 + 8g .. + 7.
+__device__ __forceinline__ bf16x8 frag(const uint16_t* X, int ld, int row0, int k0, int l) {
+  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(X + (row0 + (l & 15)) * ld + k0 + 8 * (l >> 4)));
+}
+// frag_acc: row row0 + r in the k order of two accumulator blocks, k0 + 4g .. + 3 and k0 + 16 + 4g .. + 3.
+__device__ __forceinline__ bf16x8 frag_acc(const uint16_t* X, int ld, int row0, int k0, int l) {
+  const uint16_t* p = X + (row0 + (l & 15)) * ld + k0 + 4 * (l >> 4);
+  const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + 16);
+  return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
+}
+// frag_tr: column n0 + r, rows k0 + 8g .. + 7, through the LDS transpose unit:
+// in a group of 16 lanes element m of lane j's result is element j % 4 of the
+// 8 bytes read by lane 4m + j / 4.
+__device__ __forceinline__ bf16x8 frag_tr(const uint16_t* Y, int ld, int n0, int k0, int l) {
+  typedef short v4i16 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+  const int j = l & 15;
+  const uint16_t* p = Y + (k0 + 8 * (l >> 4) + (j >> 2)) * ld + n0 + 4 * (j & 3);
+  const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p));
+  const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 4 * ld));
+  const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
+  return __builtin_bit_cast(bf16x8, make_uint4(ua.x, ua.y, ub.x, ub.y));
+}
+
+// Two accumulator blocks (rows 16 b + 4g + i of one column) as a fragment in frag_acc's k order.
+template <int NP>
+__device__ __forceinline__ void frag_from_acc(const f32x4& lo, const f32x4& hi, bf16x8 (&p)[NP]) {
+  const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  pieces8<NP>(v, p);
+}
+
+// ---------------------------------------------------------------------------
+// A tile of Q token rows of a [B, n, ...] tensor on its way to LDS: THR threads
+// take 16-byte pieces, W values a row (the row's own width w <= W; the rest and
+// the rows past the sequence are zeros, which add nothing).
+template <typename T>
+struct Kind;
+template <>
+struct Kind<bf16> {
+  static constexpr int NX = 1, Q = 64, V = 8;
+};
+template <>
+struct Kind<float> {
+  static constexpr int NX = 3, Q = 32, V = 4;
+};
+
+template <typename T, int W, int THR>
+struct Tile {
+  static constexpr int Q = Kind<T>::Q, V = Kind<T>::V, NX = Kind<T>::NX;
+  static constexpr int PR = W / V, TOT = Q * PR, CNT = (TOT + THR - 1) / THR;
+  static_assert(TOT % THR == 0, "whole pieces a thread");
+  static constexpr int LD = W + kSsmPad, PLANE = Q * LD;
+  uint4 r[CNT];
+
+  // base: the tile's first row; rows valid rows; ts elements between them; w values each
+  __device__ __forceinline__ void load(const T* base, int rows, long long ts, int w, int tid) {
+    const rsrc_t rs = rows_rsrc(base, rows > 0 ? ((long long)(rows - 1) * ts + w) * (long long)sizeof(T) : 0);
+#pragma unroll
+    for (int i = 0; i < CNT; ++i) {
+      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
+      r[i] = load16(rs, row < rows && c < w ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : 0x80000000u);
+    }
+  }
+
+  // The tile as NX planes of Q rows.  Returns whether a value of this thread's is infinite or NaN.
+  __device__ __forceinline__ bool store(uint16_t* X, int tid) const {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < CNT; ++i) {
+      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
+      uint16_t* to = X + row * LD + c;
+      const uint32_t a[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+      if constexpr (NX == 1) {
+        // an exponent of all ones carries into the bit above it
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad |= (a[k] & 0x7f807f80u) + 0x00800080u;
+        *reinterpret_cast<uint4*>(to) = r[i];
+      } else {
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          bad |= (a[k] & 0x7f800000u) + 0x00800000u;
+          v[k] = __uint_as_float(a[k]);
+        }
+        uint2 p[NX];
+        pieces4<NX>(v, p);
+#pragma unroll
+        for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(to + k * PLANE) = p[k];
+      }
+    }
+    return (bad & (NX == 1 ? 0x80008000u : 0x80000000u)) != 0;
+  }
+
+  // After store() found one: such values become zeros in the tile, and the
+  // first token that held one goes to first[column] (per column) or first[0].
+  template <bool COLS>
+  __device__ __forceinline__ void mend(uint16_t* X, int* first, int tid) const {
+#pragma unroll
+    for (int i = 0; i < CNT; ++i) {
+      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
+      const uint32_t a[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        bool bad;
+        if constexpr (NX == 1)
+          bad = ((k & 1 ? a[k / 2] >> 16 : a[k / 2]) & 0x7f80u) == 0x7f80u;
+        else
+          bad = (a[k] & 0x7f800000u) == 0x7f800000u;
+        if (bad) {
+#pragma unroll
+          for (int p = 0; p < NX; ++p) X[p * PLANE + row * LD + c + k] = 0;
+          atomicMin(first + (COLS ? c + k : 0), row);
+        }
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Step table: one entry a (sequence, head, token of whole tiles), made once a
+// call by k_ssm_steps.  L: the sum of dt A over the tile's tokens so far, in
+// log2, high and low part; dt after the softplus; w = dt 2^(Lend - L).
+struct Step {
+  float Lh, Ll, dt, w;
+};
+// and one a tile: its whole L.
+
+struct SsmPlan {
+  int tiles, segs, per;        // tiles a sequence, segments, tiles a segment
+};
+
+template <int NP>
+__device__ __forceinline__ void load_frags(const uint16_t* X, int plane, int ld, int row0, int k0, int l,
+                                           bf16x8 (&f)[NP]) {
+#pragma unroll
+  for (int k = 0; k < NP; ++k) f[k] = frag(X + k * plane, ld, row0, k0, l);
+}
+template <int NP>
+__device__ __forceinline__ void load_frags_acc(const uint16_t* X, int plane, int ld, int row0, int k0, int l,
+                                               bf16x8 (&f)[NP]) {
+#pragma unroll
+  for (int k = 0; k < NP; ++k) f[k] = frag_acc(X + k * plane, ld, row0, k0, l);
+}
+template <int NP>
+__device__ __forceinline__ void load_frags_tr(const uint16_t* X, int plane, int ld, int n0, int k0, int l,
+                                              bf16x8 (&f)[NP]) {
+#pragma unroll
+  for (int k = 0; k < NP; ++k) f[k] = frag_tr(X + k * plane, ld, n0, k0, l);
+}
+
+// The fragment's eight values from all its pieces, scaled, in NU pieces.
+template <int NX, int NU>
+__device__ __forceinline__ void scaled(const bf16x8 (&x)[NX], const float* w, bf16x8 (&u)[NU]) {
+  const float4 a = *reinterpret_cast<const float4*>(w), b = *reinterpret_cast<const float4*>(w + 4);
+  const float ws[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = NX - 1; k >= 0; --k) s += (float)x[k][i];
+    v[i] = s * ws[i];
+  }
+  pieces8<NU>(v, u);
+}
+
+}  // namespace
+}  // namespace hla

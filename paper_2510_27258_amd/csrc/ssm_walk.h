@@ -1,0 +1,379 @@
+// The tile walk of the selective state space scan (ssm_scan.hip has the
+// mathematics and the plan), shared by the outputs and the gradients' states.
+#pragma once
+#include "profile.h"
+#include "ssm_tiles.h"
+
+namespace hla {
+namespace {
+
+// What a walk does: the end state of a segment from zero, the outputs, or the
+// state before every tile (after every tile, backwards).
+enum WalkMode { kEnds = 0, kOutputs = 1, kStates = 2 };
+
+struct WalkArgs {
+  Rows x, k, q;               // x [B, n, H, P]; k, q [B, n, G, N] (backwards: dy and C in x's and k's place)
+  const float* D;             // [H] or null
+  const Step* tab;            // [B H][tok]
+  const float* tot;           // [B H][tiles]
+  float* ends;                // [B H][segs] end states in the walk's own order; slot segs - 1: the first state
+  float* segdec;              // [B H][segs] decay over a segment
+  float* state;               // [B, H, N, P] or null
+  void* y;                    // outputs
+  float* carry;               // kStates: [B H][tiles][N][P]
+  int n, H, P, G, N, tok;
+  SsmPlan plan;
+  int segs_run;               // segments of this launch
+};
+
+template <int PP>
+struct Waves {
+  static constexpr int NW = PP / 16 < 4 ? PP / 16 : 4, THR = 64 * NW, CB = PP / 16 / NW;
+};
+
+template <typename T, int PP, int NN, int MODE>
+struct WalkLds {
+  static constexpr int NX = Kind<T>::NX, Q = Kind<T>::Q;
+  static constexpr int LDK = NN + kSsmPad, LDX = PP + kSsmPad, LDS_ = Q + kSsmPad;
+  uint16_t k[NX * Q * LDK], x[NX * Q * LDX];
+  uint16_t q[MODE == kOutputs ? NX * Q * LDK : 8], s[MODE == kOutputs ? NX * Q * LDS_ : 8];
+  float Lh[Q], Ll[Q], dt[Q], w[Q];
+  int first[PP], first_all, bad[2];
+};
+
+// One workgroup walks one segment of one head; wave w owns 16 CB columns of
+// the state, h[n = 16 nb + 4g + i][p = 16 (w CB + cb) + r], in accumulators.
+// NU pieces carry the scaled inputs into the state; the readout's rounding
+// (one piece of the state and of the scores for bf16 outputs, 2^-9 of each
+// term, as large as the output's own rounding; three for fp32) is NX.
+template <typename T, int PP, int NN, int MODE, int NU, bool REV>
+__global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkArgs a) {
+  using W = Waves<PP>;
+  using L_ = WalkLds<T, PP, NN, MODE>;
+  constexpr int NW = W::NW, THR = W::THR, CB = W::CB, NX = L_::NX, Q = L_::Q, NB = NN / 16, KN = NN / 32;
+  constexpr int TB = Q / 16, KS = Q / 32, LDK = L_::LDK, LDX = L_::LDX, LDQ = L_::LDS_;
+  constexpr int PK = Q * LDK, PX = Q * LDX, PS = Q * LDQ;
+  extern __shared__ __align__(16) char smem[];
+  L_& S = *reinterpret_cast<L_*>(smem);
+  const int tid = threadIdx.x, l = tid & 63, r = l & 15, g = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // heads of one sequence and segment share k and q: neighbours on one XCD
+  const int total = gridDim.x;
+  const int lin = total % 8 ? blockIdx.x : (blockIdx.x % 8) * (total / 8) + blockIdx.x / 8;
+  const int head = lin % a.H, seg = (lin / a.H) % a.segs_run, b = lin / a.H / a.segs_run;
+  const int bh = b * a.H + head, M = a.plan.tiles;
+  const int i0 = seg * a.plan.per, i1 = min(M, i0 + a.plan.per);
+  const int pw = 16 * CB * w;
+  const T* xp = static_cast<const T*>(a.x.p) + b * a.x.bs + (long long)head * a.P;
+  const T* kp = static_cast<const T*>(a.k.p) + b * a.k.bs + (long long)(head / (a.H / a.G)) * a.N;
+  const T* qp = MODE == kOutputs ? static_cast<const T*>(a.q.p) + b * a.q.bs + (long long)(head / (a.H / a.G)) * a.N
+                                 : nullptr;
+  const Step* tab = a.tab + (size_t)bh * a.tok;
+
+  Tile<T, NN, THR> tk, tq;
+  Tile<T, PP, THR> tx;
+  Step st{};
+  auto fetch = [&](int i) {
+    const int t0 = (REV ? M - 1 - i : i) * Q, rows = min(Q, a.n - t0);
+    tk.load(kp + t0 * a.k.ts, rows, a.k.ts, a.N, tid);
+    tx.load(xp + t0 * a.x.ts, rows, a.x.ts, a.P, tid);
+    if (MODE == kOutputs) tq.load(qp + t0 * a.q.ts, rows, a.q.ts, a.N, tid);
+    if (tid < Q) st = tab[t0 + tid];
+  };
+  fetch(i0);
+
+  f32x4 h[NB][CB];
+  // the [N][P] record of a head
+  auto load_state = [&](const float* p) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = 16 * nb + 4 * g + i, c = pw + 16 * cb + r;
+          h[nb][cb][i] = n < a.N && c < a.P ? p[n * a.P + c] : 0.f;
+        }
+  };
+  auto store_state = [&](float* p) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = 16 * nb + 4 * g + i, c = pw + 16 * cb + r;
+          if (n < a.N && c < a.P) p[n * a.P + c] = h[nb][cb][i];
+        }
+  };
+  auto slot = [&](int s) { return reinterpret_cast<f32x4*>(a.ends) + ((size_t)bh * a.plan.segs + s) * NB * CB * THR; };
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) h[nb][cb] = zero4();
+  if (MODE == kEnds) {
+    if (seg == 0 && a.state && !REV) {
+      load_state(a.state + (size_t)bh * a.N * a.P);
+      f32x4* to = slot(a.plan.segs - 1);          // the outputs' last segment overwrites a.state
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) to[(nb * CB + cb) * THR + tid] = h[nb][cb];
+    }
+  } else if (seg == 0) {
+    if (a.state && !REV) {
+      if (a.plan.segs == 1) {
+        load_state(a.state + (size_t)bh * a.N * a.P);
+      } else {
+        const f32x4* from = slot(a.plan.segs - 1);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) h[nb][cb] = from[(nb * CB + cb) * THR + tid];
+      }
+    }
+  } else {
+    // segment 0's end state holds the first state
+    for (int s = 0; s < seg; ++s) {
+      const float d = a.segdec[(size_t)bh * a.plan.segs + s];
+      const f32x4* from = slot(s);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) h[nb][cb] = h[nb][cb] * d + from[(nb * CB + cb) * THR + tid];
+    }
+  }
+
+  for (int c = tid; c < PP; c += THR) S.first[c] = Q;
+  if (tid == 0) {
+    S.first_all = Q;
+    S.bad[0] = S.bad[1] = 0;
+  }
+  __syncthreads();
+
+  const float Dh = MODE == kOutputs && a.D ? a.D[head] : 0.f;
+  float segL = 0.f;
+  for (int i = i0; i < i1; ++i) {
+    const int tile = REV ? M - 1 - i : i, t0 = tile * Q, par = i & 1;
+    const float Ltile = a.tot[(size_t)bh * M + tile];
+    segL += Ltile;
+    bool bad = tk.store(S.k, tid);
+    bad |= tx.store(S.x, tid);
+    if (MODE == kOutputs) tq.store(S.q, tid);
+    if (tid < Q) {
+      S.Lh[tid] = st.Lh;
+      S.Ll[tid] = st.Ll;
+      S.dt[tid] = st.dt;
+      S.w[tid] = REV ? exp2_(st.Lh + st.Ll) : st.w;
+    }
+    if (bad) S.bad[par] = 1;
+    lds_barrier();
+    const bool flagged = __builtin_amdgcn_readfirstlane(S.bad[par]) != 0;
+    if (tid == 0) S.bad[par ^ 1] = 0;
+    if (flagged) {
+      // an infinite or NaN input must not reach the tile's earlier tokens
+      // through a zero weight: it is taken out here and its column (k: every
+      // column) set to NaN from its token on
+      tk.template mend<false>(S.k, &S.first_all, tid);
+      tx.template mend<true>(S.x, S.first, tid);
+      lds_barrier();
+    }
+    if (i + 1 < i1) fetch(i + 1);
+
+    if (MODE == kStates)
+      store_state(a.carry + ((size_t)bh * M + tile) * a.N * a.P);
+
+    bf16x8 xf[KS][CB][NX];
+    if (MODE == kOutputs) {
+      // scores, transposed (rows s, columns t), weighted and stored as s[t][s]
+      constexpr int WPT = NW > TB ? NW / TB : 1;
+#pragma unroll
+      for (int u0 = 0; u0 < TB * WPT; u0 += NW) {
+        const int u = u0 + w, tb = u / WPT;
+        if (u < TB * WPT) {
+          bf16x8 cf[KN][NX];
+#pragma unroll
+          for (int k = 0; k < KN; ++k) load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
+          const int t = 16 * tb + r;
+          const float Lt = S.Lh[t], Ltl = S.Ll[t];
+          for (int sb = u % WPT; sb <= (tb | 1); sb += WPT) {
+            f32x4 acc = zero4();
+            if (sb <= tb) {
+#pragma unroll
+              for (int k = 0; k < KN; ++k) {
+                bf16x8 bf[NX];
+                load_frags<NX>(S.k, PK, LDK, 16 * sb, 32 * k, l, bf);
+                mma_pieces<NX, NX>(bf, cf[k], acc);
+              }
+            }
+            const int s0 = 16 * sb + 4 * g;
+            const float4 Ls = *reinterpret_cast<const float4*>(S.Lh + s0), ds = *reinterpret_cast<const float4*>(S.dt + s0);
+            const float lh[4] = {Ls.x, Ls.y, Ls.z, Ls.w}, dd[4] = {ds.x, ds.y, ds.z, ds.w};
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float d = Lt - lh[e];
+              if (NX == 3) d += Ltl - S.Ll[s0 + e];
+              v[e] = s0 + e <= t ? acc[e] * (exp2_(d) * dd[e]) : 0.f;
+            }
+            uint2 p[NX];
+            pieces4<NX>(v, p);
+#pragma unroll
+            for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(S.s + k * PS + t * LDQ + s0) = p[k];
+          }
+        }
+      }
+      // the state's part, y^T[p][t] = 2^L_t sum_n h[n][p] q[t][n]
+      f32x4 y[TB][CB];
+      bf16x8 hf[KN][CB][NX];
+#pragma unroll
+      for (int k = 0; k < KN; ++k)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) frag_from_acc<NX>(h[2 * k][cb], h[2 * k + 1][cb], hf[k][cb]);
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) y[tb][cb] = zero4();
+#pragma unroll
+        for (int k = 0; k < KN; ++k) {
+          bf16x8 cf[NX];
+          load_frags_acc<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NX>(hf[k][cb], cf, y[tb][cb]);
+        }
+        const float e = exp2_(S.Lh[16 * tb + r] + S.Ll[16 * tb + r]);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) y[tb][cb] *= e;
+      }
+      lds_barrier();
+      // the tile's own part, and the outputs
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) load_frags_tr<NX>(S.x, PX, LDX, pw + 16 * cb, 32 * ks, l, xf[ks][cb]);
+      const int rows = min(Q, a.n - t0);
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          if (2 * ks <= tb) {
+            bf16x8 pf[NX];
+            load_frags<NX>(S.s, PS, LDQ, 16 * tb, 32 * ks, l, pf);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NX>(xf[ks][cb], pf, y[tb][cb]);
+          }
+        const int t = 16 * tb + r;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const int c = pw + 16 * cb + 4 * g;
+          float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = NX - 1; k >= 0; --k) {
+            const uint2 u = *reinterpret_cast<const uint2*>(S.x + k * PX + t * LDX + c);
+            v[0] += __uint_as_float(u.x << 16);
+            v[1] += __uint_as_float(u.x & 0xffff0000u);
+            v[2] += __uint_as_float(u.y << 16);
+            v[3] += __uint_as_float(u.y & 0xffff0000u);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = y[tb][cb][e] + Dh * v[e];
+            if (flagged && t >= min(S.first[c + e], S.first_all)) v[e] = nan_();
+          }
+          if (t < rows && c < a.P) {
+            T* to = static_cast<T*>(a.y) + (((size_t)b * a.n + t0 + t) * a.H + head) * a.P + c;
+            if constexpr (NX == 1) {
+              uint2 p[1];
+              pieces4<1>(v, p);
+              *reinterpret_cast<uint2*>(to) = p[0];
+            } else {
+              *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) load_frags_tr<NX>(S.x, PX, LDX, pw + 16 * cb, 32 * ks, l, xf[ks][cb]);
+    }
+
+    // h <- 2^Ltile h + sum_s k_s (w_s x_s)^T
+    const float dec = exp2_(Ltile);
+    bf16x8 u[KS][CB][NU];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) scaled<NX, NU>(xf[ks][cb], S.w + 32 * ks + 8 * g, u[ks][cb]);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) h[nb][cb] *= dec;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 bt[NX];
+        load_frags_tr<NX>(S.k, PK, LDK, 16 * nb, 32 * ks, l, bt);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NU>(bt, u[ks][cb], h[nb][cb]);
+      }
+    }
+    if (flagged) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+        if (min(S.first[pw + 16 * cb + r], S.first_all) < Q) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) h[nb][cb] = f32x4{nan_(), nan_(), nan_(), nan_()};
+        }
+      lds_barrier();
+      for (int c = tid; c < PP; c += THR) S.first[c] = Q;
+      if (tid == 0) S.first_all = Q;
+    }
+    lds_barrier();
+  }
+
+  if (MODE == kEnds) {
+    f32x4* to = slot(seg);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) to[(nb * CB + cb) * THR + tid] = h[nb][cb];
+    if (tid == 0) a.segdec[(size_t)bh * a.plan.segs + seg] = exp2_(segL);
+  } else if (MODE == kOutputs && a.state && seg == a.plan.segs - 1) {
+    store_state(a.state + (size_t)bh * a.N * a.P);
+  }
+}
+
+template <typename T, int PP, int NN, int MODE, int NU, bool REV>
+hipError_t walk(const WalkArgs& a, int B, hipStream_t s) {
+  constexpr size_t lds = sizeof(WalkLds<T, PP, NN, MODE>);
+  static_assert(lds <= 160 * 1024, "fits a CU's LDS");
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ssm_walk<T, PP, NN, MODE, NU, REV>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  constexpr const char* name = MODE == kEnds ? "ssm_ends" : MODE == kOutputs ? "ssm_outputs" : "ssm_states";
+  return HLA_TIMED(name, (k_ssm_walk<T, PP, NN, MODE, NU, REV>), dim3((unsigned)(B * a.H * a.segs_run)),
+                   dim3(Waves<PP>::THR), lds, s, a);
+}
+
+template <typename T, int PP, int MODE, int NU, bool REV>
+hipError_t walk_n(const WalkArgs& a, int B, hipStream_t s) {
+  if (a.N <= 32) return walk<T, PP, 32, MODE, NU, REV>(a, B, s);
+  if (a.N <= 64) return walk<T, PP, 64, MODE, NU, REV>(a, B, s);
+  return walk<T, PP, 128, MODE, NU, REV>(a, B, s);
+}
+template <typename T, int MODE, int NU, bool REV>
+hipError_t walk_pn(const WalkArgs& a, int B, hipStream_t s) {
+  if (a.P <= 32) return walk_n<T, 32, MODE, NU, REV>(a, B, s);
+  if (a.P <= 64) return walk_n<T, 64, MODE, NU, REV>(a, B, s);
+  return walk_n<T, 128, MODE, NU, REV>(a, B, s);
+}
+
+constexpr int walk_waves(int P) { return P <= 32 ? 2 : 4; }
+constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+}  // namespace
+}  // namespace hla
