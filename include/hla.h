@@ -439,7 +439,7 @@ int hla_qk_norm_rope_backward(const void *q, long long q_bs, long long q_ts, con
  * P and N: multiples of 16 from 16 to 128; G divides H; B*H <= 65535;
  * B*H*n < 2^31.  A <= 0 is meant (a growing state may overflow).  x, Bm, Cm:
  * 16-byte aligned, strides of whole 16-byte pieces.  bf16 inputs: scores and
- * the state that the outputs read are rounded to bf16 (2^-9 of a term, as the
+ * the state that the outputs read are rounded to bf16 (2^-8 of a term, as the
  * outputs are), the state itself is kept in fp32.  An infinite or NaN input
  * gives NaN in every output that depends on it, and in no other.
  * workspace: at least hla_ssm_workspace_bytes(...) bytes. */
@@ -457,6 +457,23 @@ int hla_ssm_step(float *state, const void *x, long long x_bs, const void *dt, lo
                  const void *Bm, long long b_bs, const void *Cm, long long c_bs, const float *D,
                  const float *dt_bias, void *y, int B, int H, int P, int G, int N, int softplus, int dtype,
                  int dt_dtype, void *stream);
+
+/* hla_ssm_backward — gradients of hla_ssm_forward without a state, for dy
+ * [B, n, H, P] (strides as x's): dx [B, n, H, P], dBm, dCm [B, n, G, N] (summed
+ * over the heads of a group), ddt [B, n, H] of dt_dtype, and fp32 [H] dA, dD
+ * (optional), ddt_bias (optional).  bf16 inputs (dtype = HLA_BF16); fp32 ones
+ * return HLA_ERR_UNSUPPORTED.  Inputs and dy are meant to be finite: NaN in
+ * one token may reach the gradients of the 64-token tile around it.
+ * workspace: at least hla_ssm_backward_workspace_bytes(...) bytes (two states
+ * for every 64 tokens of a head). */
+size_t hla_ssm_backward_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype);
+int hla_ssm_backward(const void *x, long long x_bs, long long x_ts, const void *dt, long long dt_bs,
+                     long long dt_ts, const float *A, const void *Bm, long long b_bs, long long b_ts,
+                     const void *Cm, long long c_bs, long long c_ts, const float *D, const float *dt_bias,
+                     const void *dy, long long dy_bs, long long dy_ts, void *dx, void *ddt, float *dA,
+                     void *dBm, void *dCm, float *dD, float *ddt_bias, int B, int n, int H, int P, int G,
+                     int N, int softplus, int dtype, int dt_dtype, void *workspace, size_t workspace_bytes,
+                     void *stream);
 
 /* ---------------------------------------------------------------------------
  * Benchmark timing.  hla_profile_begin(max_records) creates 2*max_records HIP

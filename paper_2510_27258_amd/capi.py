@@ -77,6 +77,8 @@ _SIGS = {
                                   [_P, _Z, _P]),
     "hla_ssm_workspace_bytes": (_Z, [_I] * 7),
     "hla_ssm_forward": (_I, _ROWS * 2 + [_P] + _ROWS * 2 + [_P] * 4 + [_I] * 9 + [_P, _Z, _P]),
+    "hla_ssm_backward_workspace_bytes": (_Z, [_I] * 7),
+    "hla_ssm_backward": (_I, _ROWS * 2 + [_P] + _ROWS * 2 + [_P] * 2 + _ROWS + [_P] * 7 + [_I] * 9 + [_P, _Z, _P]),
     "hla_ssm_step": (_I, [_P] + [_P, _L] * 2 + [_P] + [_P, _L] * 2 + [_P] * 3 + [_I] * 8 + [_P]),
 }
 
@@ -278,6 +280,14 @@ def hla_ssm_workspace_bytes(B, n, H, P, G, N, dtype):
 
 def hla_ssm_forward(*args):
     return _call("hla_ssm_forward", *args)
+
+
+def hla_ssm_backward_workspace_bytes(B, n, H, P, G, N, dtype):
+    return lib().hla_ssm_backward_workspace_bytes(B, n, H, P, G, N, dtype)
+
+
+def hla_ssm_backward(*args):
+    return _call("hla_ssm_backward", *args)
 
 
 def hla_ssm_step(*args):

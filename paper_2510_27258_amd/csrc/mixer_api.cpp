@@ -293,4 +293,41 @@ int hla_ssm_step(float* state, const void* x, long long x_bs, const void* dt, lo
   return done(hla::launch_ssm_step(a, s), "state space step");
 }
 
+size_t hla_ssm_backward_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype) {
+  if (ssm_sizes(B, n, H, P, G, N) != HLA_OK || check_type(dtype, "dtype") != HLA_OK) return 0;
+  if (dtype != HLA_BF16) {
+    fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
+    return 0;
+  }
+  return hla::ssm_backward_ws(B, n, H, P, G, N);
+}
+
+int hla_ssm_backward(const void* x, long long x_bs, long long x_ts, const void* dt, long long dt_bs, long long dt_ts,
+                     const float* A, const void* Bm, long long b_bs, long long b_ts, const void* Cm, long long c_bs,
+                     long long c_ts, const float* D, const float* dt_bias, const void* dy, long long dy_bs,
+                     long long dy_ts, void* dx, void* ddt, float* dA, void* dBm, void* dCm, float* dD,
+                     float* ddt_bias, int B, int n, int H, int P, int G, int N, int softplus, int dtype, int dt_dtype,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  hla::Ssm a{};
+  a.x = {x, x_bs, x_ts};
+  a.dt = {dt, dt_bs, dt_ts};
+  a.Bm = {Bm, b_bs, b_ts};
+  a.Cm = {Cm, c_bs, c_ts};
+  a.dy = {dy, dy_bs, dy_ts};
+  a.A = A; a.D = D; a.dt_bias = dt_bias;
+  a.dx = dx; a.ddt = ddt; a.dA = dA; a.dBm = dBm; a.dCm = dCm; a.dD = dD; a.ddt_bias = ddt_bias;
+  a.B = B; a.n = n; a.H = H; a.P = P; a.G = G; a.N = N; a.softplus = softplus; a.dtype = dtype; a.dt_dtype = dt_dtype;
+  int rc;
+  if ((rc = ssm_check(a)) != HLA_OK) return rc;
+  if (dtype != HLA_BF16) return fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
+  if ((rc = ssm_rows(a.dy, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
+      (rc = check_own(ddt, esize(dt_dtype), "ddt")) || (rc = check_own(dA, 4, "dA")) || (rc = check_16(dBm, "dBm")) ||
+      (rc = check_16(dCm, "dCm")) || (rc = check_own(dD, 4, "dD", false)) ||
+      (rc = check_own(ddt_bias, 4, "ddt_bias", false)) ||
+      (rc = check_ws(workspace, workspace_bytes, hla::ssm_backward_ws(B, n, H, P, G, N))))
+    return rc;
+  return done(hla::launch_ssm_backward(a, workspace, reinterpret_cast<hipStream_t>(stream)),
+              "state space scan's gradients");
+}
+
 }  // extern "C"

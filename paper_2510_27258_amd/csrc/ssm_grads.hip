@@ -1,0 +1,567 @@
+// Gradients of the selective state space scan (bf16 inputs), for the upstream
+// gradient dy.  With h_t the state after token t, g_t its gradient and u_t =
+// dt_t x_t, M_ts = 2^(L_t - L_s):
+//   g_t = C_t dy_t^T + 2^(l_{t+1}) g_{t+1}
+//   dC_t = h_t dy_t,  dB_t = g_t u_t,  du_t = g_t^T B_t,  dx_t = dt_t du_t + D dy_t
+//   d(dt_t) = A da_t + x_t . du_t,     da_t = 2^(l_t) <g_t, h_{t-1}>.
+// Over a tile with the state h before it and the gradient g after it:
+//   dC_t = 2^(L_t) h dy_t            + sum_{s<=t} M_ts dt_s (dy_t . x_s) B_s
+//   dB_s = 2^(Lend - L_s) dt_s g x_s + sum_{t>=s} M_ts dt_s (dy_t . x_s) C_t
+//   du_s = 2^(Lend - L_s) g^T B_s    + sum_{t>=s} M_ts (C_t . B_s) dy_t
+//   da_r = sum_{t>=r} (R_t - dt_t K_t + E_t) + sum_{s<r} dt_s F_s + 2^(Lend) <g, h>
+// with R and K the row and column sums of q_ts = M_ts (C_t . B_s)(dy_t . x_s),
+// s < t (R with dt_s), E_t = 2^(L_t) C_t . (h dy_t) and F_s = 2^(Lend - L_s) B_s .
+// (g x_s).  All cancellation stays within a tile, in fp32 sums.
+//
+// The states before and the gradients after every tile come from two walks
+// (ssm_walk.h), one each way, into the workspace: 2 x 4 N P bytes a tile and
+// head, which is what bounds the whole.  A workgroup here takes a tile and the
+// heads that share its B and C: C B^T is formed once, the heads' M dt V are
+// summed before they meet B and C, and dB and dC stay in accumulators over the
+// heads.  h and g are kept and enter their products to 24 bits (three pieces):
+// dA and d dt_bias are sums of either sign over every token, and with two
+// pieces (2^-17) they were 2.6e-6 off 64 bits instead of 1.8e-6, for 1 % of the time.
+#include "ssm_walk.h"
+
+namespace hla {
+namespace {
+
+constexpr int kGQ = 64;   // Kind<bf16>::Q
+
+struct GradArgs {
+  Rows x, dy, k, q;
+  const Step* tab;
+  const float* tot;
+  const float *h0, *g1;       // [B H][tiles][N][P]
+  const float *A, *D;
+  void *dx, *ddt;
+  void *dk, *dq;              // bf16 [B, n, G, N], or with hs > 1 fp32 [hs][B, n, G, N]
+  float* par;                 // [B H][tiles][3]: dA, dD, d dt_bias
+  int B, n, H, P, G, N, tok, tiles, hs, softplus, dt_dtype;
+};
+
+template <int PP, int NN>
+struct GradLds {
+  static constexpr int LDK = NN + kSsmPad, LDX = PP + kSsmPad, LDP = kGQ + kSsmPad;
+  uint16_t k[kGQ * LDK];
+  union {
+    uint16_t q[kGQ * LDK];
+    uint16_t g[NN * LDX];
+  };
+  uint16_t x[kGQ * LDX], dy[kGQ * LDX], p[kGQ * LDP];
+  float Lh[kGQ], Ll[kGQ], dt[kGQ], el[kGQ], wq[kGQ];
+  float R[kGQ], own[kGQ], K[4][kGQ], E[4][kGQ], F[4][kGQ], one[4][2];
+};
+
+__device__ __forceinline__ float sum_groups(float v) {        // over the four lane groups of 16
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+__device__ __forceinline__ float sum_wave(float v) {
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
+  return v;
+}
+__device__ __forceinline__ void unpack4(const uint2& u, float (&v)[4]) {
+  v[0] = __uint_as_float(u.x << 16);
+  v[1] = __uint_as_float(u.x & 0xffff0000u);
+  v[2] = __uint_as_float(u.y << 16);
+  v[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+
+template <int PP, int NN>
+__global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
+  using L_ = GradLds<PP, NN>;
+  constexpr int LDK = L_::LDK, LDX = L_::LDX, LDP = L_::LDP, KN = NN / 32, KP = PP / 32, TB = 4;
+  constexpr int NBT = NN / 16, NBW = NBT >= 4 ? NBT / 4 : 1, PBT = PP / 16, PBW = PBT >= 4 ? PBT / 4 : 1;
+  extern __shared__ __align__(16) char smem[];
+  L_& S = *reinterpret_cast<L_*>(smem);
+  const int tid = threadIdx.x, l = tid & 63, r = l & 15, g = l >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool has_n = w * NBW < NBT, has_p = w * PBW < PBT;
+
+  int lin = blockIdx.x;
+  const int hs = lin % a.hs; lin /= a.hs;
+  const int grp = lin % a.G; lin /= a.G;
+  const int tile = lin % a.tiles, b = lin / a.tiles;
+  const int share = a.H / a.G, per = (share + a.hs - 1) / a.hs;
+  const int head0 = grp * share + hs * per, heads = min(per, share - hs * per);
+  const int t0 = tile * kGQ, rows = min(kGQ, a.n - t0);
+
+  const uint16_t* kp = static_cast<const uint16_t*>(a.k.p) + b * a.k.bs + t0 * a.k.ts + (long long)grp * a.N;
+  const uint16_t* qp = static_cast<const uint16_t*>(a.q.p) + b * a.q.bs + t0 * a.q.ts + (long long)grp * a.N;
+  const uint16_t* xp = static_cast<const uint16_t*>(a.x.p) + b * a.x.bs + t0 * a.x.ts;
+  const uint16_t* yp = static_cast<const uint16_t*>(a.dy.p) + b * a.dy.bs + t0 * a.dy.ts;
+
+  Tile<bf16, NN, 256> tn;
+  Tile<bf16, PP, 256> tx, ty;
+  Step st{};
+  auto fetch = [&](int head) {
+    tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, a.x.ts, a.P, tid);
+    ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, a.dy.ts, a.P, tid);
+    if (tid < kGQ) st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + tid];
+  };
+  tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, tid);
+  tn.store(S.k, tid);
+  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, tid);
+  tn.store(S.q, tid);
+  if (heads > 0) fetch(head0);
+  lds_barrier();
+
+  // (C B^T)^T of the wave's 16 tokens t, rows s; and B and C where dB and dC will be
+  f32x4 s_[TB], z[TB];
+  {
+    bf16x8 cf[KN];
+#pragma unroll
+    for (int k = 0; k < KN; ++k) cf[k] = frag(S.q, LDK, 16 * w, 32 * k, l);
+#pragma unroll
+    for (int sb = 0; sb < TB; ++sb) {
+      s_[sb] = z[sb] = zero4();
+      if (sb <= w) {
+#pragma unroll
+        for (int k = 0; k < KN; ++k) s_[sb] = mma(frag(S.k, LDK, 16 * sb, 32 * k, l), cf[k], s_[sb]);
+      }
+    }
+  }
+  f32x4 dk[NBW][TB], dq[NBW][TB];
+  uint2 kn[NBW][TB], qn[NBW][TB];
+#pragma unroll
+  for (int j = 0; j < NBW; ++j)
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) {
+      dk[j][tb] = dq[j][tb] = zero4();
+      const int at = (16 * tb + r) * LDK + (has_n ? 16 * (w * NBW + j) + 4 * g : 0);
+      kn[j][tb] = *reinterpret_cast<const uint2*>(S.k + at);
+      qn[j][tb] = *reinterpret_cast<const uint2*>(S.q + at);
+    }
+  lds_barrier();
+
+  for (int hh = 0; hh < heads; ++hh) {
+    const int head = head0 + hh, bh = b * a.H + head;
+    const float Lend = a.tot[(size_t)bh * a.tiles + tile];
+    tx.store(S.x, tid);
+    ty.store(S.dy, tid);
+    if (tid < kGQ) {
+      S.Lh[tid] = st.Lh;
+      S.Ll[tid] = st.Ll;
+      S.dt[tid] = st.dt;
+      S.el[tid] = exp2_(st.Lh + st.Ll);
+      S.wq[tid] = exp2_(Lend - st.Lh - st.Ll);
+    }
+    lds_barrier();
+    if (hh + 1 < heads) fetch(head + 1);
+
+    // (dy x^T)^T, the weighted scores for dx, and their sums
+    {
+      const int t = 16 * w + r;
+      const float Lt = S.Lh[t], Ltl = S.Ll[t];
+      bf16x8 yf[KP];
+#pragma unroll
+      for (int k = 0; k < KP; ++k) yf[k] = frag(S.dy, LDX, 16 * w, 32 * k, l);
+      float rsum = 0.f, diag = 0.f;
+#pragma unroll
+      for (int sb = 0; sb < TB; ++sb) {
+        float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
+        const int s0 = 16 * sb + 4 * g;
+        if (sb <= w) {
+          f32x4 v = zero4();
+#pragma unroll
+          for (int k = 0; k < KP; ++k) v = mma(frag(S.x, LDX, 16 * sb, 32 * k, l), yf[k], v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool in = s0 + e <= t;
+            const float m = in ? exp2_((Lt - S.Lh[s0 + e]) + (Ltl - S.Ll[s0 + e])) : 0.f, dts = S.dt[s0 + e];
+            p[e] = in ? m * s_[sb][e] : 0.f;
+            // q's diagonal has no part in da: left out of the sums that would cancel it
+            q[e] = s0 + e < t ? p[e] * v[e] : 0.f;
+            z[sb][e] += in ? m * v[e] * dts : 0.f;
+            rsum += q[e] * dts;
+            if (s0 + e == t) {
+              diag = v[e];
+              S.own[t] = p[e] * v[e];
+            }
+          }
+        }
+        if (sb <= (w | 1)) {
+          uint2 o[1];
+          pieces4<1>(p, o);
+          *reinterpret_cast<uint2*>(S.p + t * LDP + s0) = o[0];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (sb <= w) {
+#pragma unroll
+            for (int m = 1; m < 16; m *= 2) q[e] += __shfl_xor(q[e], m);
+          }
+          if (r == 0) S.K[w][s0 + e] = q[e];
+        }
+      }
+      rsum = sum_groups(rsum);
+      if (g == 0) S.R[t] = rsum;
+      diag = sum_wave(diag);
+      if (l == 0) S.one[w][0] = diag;
+    }
+
+    // h dy_t and g x_s for the wave's rows n
+    float zz = 0.f, E[TB] = {0.f, 0.f, 0.f, 0.f}, F[TB] = {0.f, 0.f, 0.f, 0.f};
+    if (has_n) {
+      const size_t rec = ((size_t)bh * a.tiles + tile) * a.N * a.P;
+#pragma unroll
+      for (int j = 0; j < NBW; ++j) {
+        const int n = 16 * (w * NBW + j) + r;
+        float hv[KP][8], gv[KP][8];
+#pragma unroll
+        for (int k = 0; k < KP; ++k) {
+          const int c = 32 * k + 8 * g;
+          const bool in = n < a.N && c < a.P;
+          const float4* hp = reinterpret_cast<const float4*>(a.h0 + rec + (size_t)n * a.P + c);
+          const float4* gp = reinterpret_cast<const float4*>(a.g1 + rec + (size_t)n * a.P + c);
+          const float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 h_0 = in ? hp[0] : o, h_1 = in ? hp[1] : o, g_0 = in ? gp[0] : o, g_1 = in ? gp[1] : o;
+          const float hq[8] = {h_0.x, h_0.y, h_0.z, h_0.w, h_1.x, h_1.y, h_1.z, h_1.w};
+          const float gq[8] = {g_0.x, g_0.y, g_0.z, g_0.w, g_1.x, g_1.y, g_1.z, g_1.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            hv[k][i] = hq[i];
+            gv[k][i] = gq[i];
+            zz += hq[i] * gq[i];
+          }
+        }
+        bf16x8 hf[KP][3], gf[KP][3];
+#pragma unroll
+        for (int k = 0; k < KP; ++k) {
+          pieces8<3>(hv[k], hf[k]);
+          pieces8<3>(gv[k], gf[k]);
+          *reinterpret_cast<uint4*>(S.g + n * LDX + 32 * k + 8 * g) = __builtin_bit_cast(uint4, gf[k][0]);
+        }
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) {
+          f32x4 c0 = zero4(), b0 = zero4();
+#pragma unroll
+          for (int k = 0; k < KP; ++k) {
+            const bf16x8 yf = frag(S.dy, LDX, 16 * tb, 32 * k, l), xf = frag(S.x, LDX, 16 * tb, 32 * k, l);
+            c0 = mma(hf[k][2], yf, c0);
+            b0 = mma(gf[k][2], xf, b0);
+            c0 = mma(hf[k][1], yf, c0);
+            b0 = mma(gf[k][1], xf, b0);
+            c0 = mma(hf[k][0], yf, c0);
+            b0 = mma(gf[k][0], xf, b0);
+          }
+          const int t = 16 * tb + r;
+          const float el = S.el[t], wq = S.wq[t], wd = wq * S.dt[t];
+          float kv[4], qv[4];
+          unpack4(kn[j][tb], kv);
+          unpack4(qn[j][tb], qv);
+          float e_ = 0.f, f_ = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            e_ += qv[i] * c0[i];
+            f_ += kv[i] * b0[i];
+            dq[j][tb][i] += el * c0[i];
+            dk[j][tb][i] += wd * b0[i];
+          }
+          E[tb] += el * e_;
+          F[tb] += wq * f_;
+        }
+      }
+    }
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) {
+      const float e_ = sum_groups(E[tb]), f_ = sum_groups(F[tb]);
+      if (g == 0) {
+        S.E[w][16 * tb + r] = e_;
+        S.F[w][16 * tb + r] = f_;
+      }
+    }
+    zz = sum_wave(zz);
+    if (l == 0) S.one[w][1] = zz;
+    lds_barrier();
+
+    // dx^T for the wave's columns p
+    if (has_p) {
+      const float Dh = a.D ? a.D[head] : 0.f;
+#pragma unroll
+      for (int j = 0; j < PBW; ++j) {
+        const int p0 = 16 * (w * PBW + j);
+        f32x4 acc[TB];
+#pragma unroll
+        for (int sb = 0; sb < TB; ++sb) acc[sb] = zero4();
+#pragma unroll
+        for (int k = 0; k < KN; ++k) {
+          const bf16x8 gt = frag_tr(S.g, LDX, p0, 32 * k, l);
+#pragma unroll
+          for (int sb = 0; sb < TB; ++sb) acc[sb] = mma(gt, frag(S.k, LDK, 16 * sb, 32 * k, l), acc[sb]);
+        }
+#pragma unroll
+        for (int sb = 0; sb < TB; ++sb) acc[sb] *= S.wq[16 * sb + r];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          const bf16x8 yt = frag_tr(S.dy, LDX, p0, 32 * ks, l);
+#pragma unroll
+          for (int sb = 0; sb < TB; ++sb)
+            if (sb < 2 * ks + 2) acc[sb] = mma(yt, frag_tr(S.p, LDP, 16 * sb, 32 * ks, l), acc[sb]);
+        }
+#pragma unroll
+        for (int sb = 0; sb < TB; ++sb) {
+          const int s = 16 * sb + r, c = p0 + 4 * g;
+          float v[4];
+          unpack4(*reinterpret_cast<const uint2*>(S.dy + s * LDX + c), v);
+          const float dts = S.dt[s];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = dts * acc[sb][e] + Dh * v[e];
+          if (s < rows && c < a.P) {
+            uint2 o[1];
+            pieces4<1>(v, o);
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dx) + (((size_t)b * a.n + t0 + s) * a.H + head) * a.P + c) =
+                o[0];
+          }
+        }
+      }
+    }
+    // the gradients of dt and the per-head parameters: one wave, a token a lane
+    if (w == (hh & 3)) {
+      const float dt = S.dt[l], R = S.R[l];
+      float K = 0.f, Et = 0.f, Fs = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        K += S.K[i][l];
+        Et += S.E[i][l];
+        Fs += S.F[i][l];
+      }
+      const float hg = S.one[0][1] + S.one[1][1] + S.one[2][1] + S.one[3][1];
+      double suf = (double)R - (double)dt * K + Et, pre = (double)dt * Fs;
+      const double own = pre;
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) {
+        const double u = __shfl_down(suf, m), v = __shfl_up(pre, m);
+        if (l + m < 64) suf += u;
+        if (l >= m) pre += v;
+      }
+      const float da = (float)(suf + (pre - own) + (double)exp2_(Lend) * hg);
+      float d = a.A[head] * da + (K + S.own[l] + Fs);
+      if (a.softplus) d *= -expm1f(-dt);
+      if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, d);
+      const float dA = sum_wave(l < rows ? dt * da : 0.f), db = sum_wave(l < rows ? d : 0.f);
+      if (l == 0) {
+        float* o = a.par + ((size_t)bh * a.tiles + tile) * 3;
+        o[0] = dA;
+        o[1] = S.one[0][0] + S.one[1][0] + S.one[2][0] + S.one[3][0];
+        o[2] = db;
+      }
+    }
+    lds_barrier();
+  }
+
+  // the tile's own part of dB and dC: the heads' sum z[t][s] with C and B
+  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, tid);
+  tn.store(S.q, tid);
+#pragma unroll
+  for (int sb = 0; sb < TB; ++sb)
+    if (sb <= (w | 1)) {
+      const float v[4] = {z[sb][0], z[sb][1], z[sb][2], z[sb][3]};
+      uint2 o[1];
+      pieces4<1>(v, o);
+      *reinterpret_cast<uint2*>(S.p + (16 * w + r) * LDP + 16 * sb + 4 * g) = o[0];
+    }
+  lds_barrier();
+  if (!has_n) return;
+#pragma unroll
+  for (int j = 0; j < NBW; ++j) {
+    const int n0 = 16 * (w * NBW + j);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 kt = frag_tr(S.k, LDK, n0, 32 * ks, l), qt = frag_tr(S.q, LDK, n0, 32 * ks, l);
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
+        if (tb >= 2 * ks) dq[j][tb] = mma(kt, frag(S.p, LDP, 16 * tb, 32 * ks, l), dq[j][tb]);
+        if (tb < 2 * ks + 2) dk[j][tb] = mma(qt, frag_tr(S.p, LDP, 16 * tb, 32 * ks, l), dk[j][tb]);
+      }
+    }
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) {
+      const int t = 16 * tb + r, n = n0 + 4 * g;
+      if (t >= rows || n >= a.N) continue;
+      const size_t at = (((size_t)b * a.n + t0 + t) * a.G + grp) * a.N + n;
+      const float vk[4] = {dk[j][tb][0], dk[j][tb][1], dk[j][tb][2], dk[j][tb][3]};
+      const float vq[4] = {dq[j][tb][0], dq[j][tb][1], dq[j][tb][2], dq[j][tb][3]};
+      if (a.hs == 1) {
+        uint2 o[1];
+        pieces4<1>(vk, o);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dk) + at) = o[0];
+        pieces4<1>(vq, o);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dq) + at) = o[0];
+      } else {
+        const size_t all = (size_t)a.B * a.n * a.G * a.N;
+        *reinterpret_cast<float4*>(static_cast<float*>(a.dk) + hs * all + at) = make_float4(vk[0], vk[1], vk[2], vk[3]);
+        *reinterpret_cast<float4*>(static_cast<float*>(a.dq) + hs * all + at) = make_float4(vq[0], vq[1], vq[2], vq[3]);
+      }
+    }
+  }
+}
+
+// The first H blocks sum a head's parameters over sequences and tiles; the
+// others the head subsets' dB and dC, four values a thread.
+struct FinishArgs {
+  const float* par;
+  float *dA, *dD, *db;
+  const float *dk, *dq;
+  uint16_t *dBm, *dCm;
+  size_t all;
+  int B, H, tiles, hs;
+};
+__global__ __launch_bounds__(256) void k_ssm_finish(FinishArgs a) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < a.H) {
+    const int head = blockIdx.x;
+    double s[3] = {0.0, 0.0, 0.0};
+    for (int i = tid; i < a.B * a.tiles; i += 256) {
+      const int b = i / a.tiles, tile = i - b * a.tiles;
+      const float* p = a.par + (((size_t)b * a.H + head) * a.tiles + tile) * 3;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) s[j] += p[j];
+    }
+    __shared__ double red[3][256];
+#pragma unroll
+    for (int j = 0; j < 3; ++j) red[j][tid] = s[j];
+    __syncthreads();
+    for (int m = 128; m > 0; m /= 2) {
+      if (tid < m)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) red[j][tid] += red[j][tid + m];
+      __syncthreads();
+    }
+    if (tid == 0) {
+      a.dA[head] = (float)red[0][0];
+      if (a.dD) a.dD[head] = (float)red[1][0];
+      if (a.db) a.db[head] = (float)red[2][0];
+    }
+    return;
+  }
+  const size_t i = ((size_t)(blockIdx.x - a.H) * 256 + tid) * 4;
+  if (i >= a.all) return;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float* p = j ? a.dq : a.dk;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int h = 0; h < a.hs; ++h) {
+      const float4 u = *reinterpret_cast<const float4*>(p + h * a.all + i);
+      v[0] += u.x;
+      v[1] += u.y;
+      v[2] += u.z;
+      v[3] += u.w;
+    }
+    uint2 o[1];
+    pieces4<1>(v, o);
+    *reinterpret_cast<uint2*>((j ? a.dCm : a.dBm) + i) = o[0];
+  }
+}
+
+template <int PP, int NN>
+hipError_t grads(const GradArgs& a, hipStream_t s) {
+  constexpr size_t lds = sizeof(GradLds<PP, NN>);
+  static_assert(lds <= 160 * 1024, "fits a CU's LDS");
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ssm_grads<PP, NN>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  return HLA_TIMED("ssm_grads", (k_ssm_grads<PP, NN>), dim3((unsigned)(a.B * a.tiles * a.G * a.hs)), dim3(256), lds, s,
+                   a);
+}
+template <int PP>
+hipError_t grads_n(const GradArgs& a, hipStream_t s) {
+  if (a.N <= 32) return grads<PP, 32>(a, s);
+  if (a.N <= 64) return grads<PP, 64>(a, s);
+  return grads<PP, 128>(a, s);
+}
+
+// Head subsets a group: workgroups for two a CU, each of at least one head.
+int head_subsets(int B, int tiles, int G, int share) {
+  const long long wgs = (long long)B * tiles * G;
+  long long hs = wgs >= 512 ? 1 : (512 + wgs - 1) / wgs;
+  if (hs > share) hs = share;
+  const int per = (int)((share + hs - 1) / hs);
+  return (share + per - 1) / per;
+}
+
+struct GradWs {
+  Step* tab;
+  float *tot, *par, *ends[2], *segdec[2], *carry[2], *bc[2];
+  size_t bytes;
+};
+GradWs carve(void* ws, int B, int n, int H, int P, int G, int N) {
+  const int BH = B * H;
+  const SsmPlan p = ssm_plan(BH, n, kGQ);
+  const size_t tok = (size_t)(n + 63) / 64 * 64;
+  char* c = static_cast<char*>(ws);
+  size_t o = 0;
+  GradWs r;
+  auto take = [&](size_t floats) {
+    float* q = reinterpret_cast<float*>(c + o);
+    o += align256(sizeof(float) * floats);
+    return q;
+  };
+  r.tab = reinterpret_cast<Step*>(take(4 * tok * BH));
+  r.tot = take((size_t)p.tiles * BH);
+  r.par = take((size_t)p.tiles * BH * 3);
+  const int hs = head_subsets(B, p.tiles, G, H / G);
+  for (int i = 0; i < 2; ++i) {
+    r.segdec[i] = take((size_t)p.segs * BH);
+    r.ends[i] = take(p.segs > 1 ? (size_t)p.segs * BH * padded(P) * padded(N) : 0);
+    r.carry[i] = take((size_t)BH * p.tiles * N * P);
+    r.bc[i] = take(hs > 1 ? (size_t)hs * B * n * G * N : 0);
+  }
+  r.bytes = o;
+  return r;
+}
+
+}  // namespace
+
+size_t ssm_backward_ws(int B, int n, int H, int P, int G, int N) { return carve(nullptr, B, n, H, P, G, N).bytes; }
+
+hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {
+  const GradWs c = carve(ws, a.B, a.n, a.H, a.P, a.G, a.N);
+  hipError_t e = launch_steps(a, c.tab, c.tot, kGQ, s);
+  if (e != hipSuccess) return e;
+  WalkPair pair{};
+  for (int i = 0; i < 2; ++i) {
+    WalkArgs& w = pair.a[i];
+    w.x = i ? a.dy : a.x;
+    w.k = i ? a.Cm : a.Bm;
+    w.tab = c.tab; w.tot = c.tot; w.ends = c.ends[i]; w.segdec = c.segdec[i]; w.carry = c.carry[i];
+    w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
+    w.plan = ssm_plan(a.B * a.H, a.n, kGQ);
+    w.segs_run = w.plan.segs - 1;
+    w.rev = i;
+  }
+  if (pair.a[0].segs_run > 0) {
+    e = walk_pn<bf16, kEnds, 3>(pair, 2, a.B, s);
+    if (e != hipSuccess) return e;
+  }
+  pair.a[0].segs_run = pair.a[1].segs_run = pair.a[0].plan.segs;
+  e = walk_pn<bf16, kStates, 3>(pair, 2, a.B, s);
+  if (e != hipSuccess) return e;
+
+  GradArgs d{};
+  d.x = a.x; d.dy = a.dy; d.k = a.Bm; d.q = a.Cm;
+  d.tab = c.tab; d.tot = c.tot; d.h0 = c.carry[0]; d.g1 = c.carry[1];
+  d.A = a.A; d.D = a.D; d.dx = a.dx; d.ddt = a.ddt; d.par = c.par;
+  d.B = a.B; d.n = a.n; d.H = a.H; d.P = a.P; d.G = a.G; d.N = a.N; d.tok = (a.n + 63) / 64 * 64;
+  d.tiles = pair.a[0].plan.tiles;
+  d.hs = head_subsets(a.B, d.tiles, a.G, a.H / a.G);
+  d.softplus = a.softplus; d.dt_dtype = a.dt_dtype;
+  d.dk = d.hs > 1 ? c.bc[0] : a.dBm;
+  d.dq = d.hs > 1 ? c.bc[1] : a.dCm;
+  e = a.P <= 32 ? grads_n<32>(d, s) : a.P <= 64 ? grads_n<64>(d, s) : grads_n<128>(d, s);
+  if (e != hipSuccess) return e;
+
+  FinishArgs f{};
+  f.par = c.par; f.dA = a.dA; f.dD = a.dD; f.db = a.ddt_bias;
+  f.dk = c.bc[0]; f.dq = c.bc[1];
+  f.dBm = static_cast<uint16_t*>(a.dBm); f.dCm = static_cast<uint16_t*>(a.dCm);
+  f.all = d.hs > 1 ? (size_t)a.B * a.n * a.G * a.N : 0;
+  f.B = a.B; f.H = a.H; f.tiles = d.tiles; f.hs = d.hs;
+  return HLA_TIMED("ssm_finish", k_ssm_finish, dim3((unsigned)(a.H + (f.all / 4 + 255) / 256)), dim3(256), 0, s, f);
+}
+
+}  // namespace hla

@@ -17,58 +17,11 @@
 namespace hla {
 namespace {
 
-// A wave: 64 tokens of one (sequence, head).  Sums in fp64: L reaches the
-// hundreds, where fp32 sums would put 1e-5 into the weights of neighbours.
-template <int Q>
-__global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab, float* __restrict__ tot, int tok,
-                                                   int tiles) {
-  const int wv = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
-  const int head = wv % a.H, blk = (wv / a.H) % (tok / 64), b = wv / a.H / (tok / 64);
-  if (b >= a.B) return;
-  const int t = blk * 64 + lane, bh = b * a.H + head;
-  float dt = 0.f;
-  double la = 0.0;
-  if (t < a.n) {
-    dt = load_any(a.dt.p, a.dt_dtype, (size_t)(b * a.dt.bs + t * a.dt.ts + head));
-    if (a.dt_bias) dt += a.dt_bias[head];
-    if (a.softplus) dt = dt > 20.f ? dt : log1pf(expf(dt));
-    la = (double)dt * (double)a.A[head] * 1.4426950408889634;
-  }
-  double L = la;
-#pragma unroll
-  for (int m = 1; m < Q; m *= 2) {
-    const double o = __shfl_up(L, m, Q);
-    if ((lane & (Q - 1)) >= m) L += o;
-  }
-  const double end = __shfl(L, Q - 1, Q);
-  Step s;
-  s.Lh = (float)L;
-  s.Ll = (float)(L - (double)s.Lh);
-  s.dt = dt;
-  s.w = dt * exp2_((float)(end - L));
-  tab[(size_t)bh * tok + t] = s;
-  if ((lane & (Q - 1)) == Q - 1 && t / Q < tiles) tot[(size_t)bh * tiles + t / Q] = (float)end;
-}
-
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
 int tile_of(int dtype) { return dtype == 1 ? Kind<bf16>::Q : Kind<float>::Q; }
 
 }  // namespace
 
 bool ssm_sizes_ok(int P, int N) { return P >= 16 && P <= 128 && P % 16 == 0 && N >= 16 && N <= 128 && N % 16 == 0; }
-
-// Segments a head: walks for two workgroups a CU, each of at least four tiles.
-SsmPlan ssm_plan(int BH, int n, int Q) {
-  SsmPlan p;
-  p.tiles = (n + Q - 1) / Q;
-  int segs = BH >= 512 ? 1 : (512 + BH - 1) / BH;
-  if (segs > p.tiles / 4) segs = p.tiles / 4;
-  if (segs < 1) segs = 1;
-  p.per = (p.tiles + segs - 1) / segs;
-  p.segs = (p.tiles + p.per - 1) / p.per;
-  return p;
-}
 
 struct SsmWs {
   Step* tab;
@@ -97,21 +50,14 @@ size_t ssm_forward_ws(int B, int n, int H, int P, int N, int dtype) {
   return carve(nullptr, B * H, n, P, N, tile_of(dtype)).bytes;
 }
 
-static hipError_t launch_steps(const Ssm& a, Step* tab, float* tot, int Q, hipStream_t s) {
-  const int tok = (a.n + 63) / 64 * 64, tiles = (a.n + Q - 1) / Q;
-  const long long waves = (long long)a.B * a.H * (tok / 64);
-  const dim3 grid((unsigned)((waves + 3) / 4));
-  if (Q == 64) return HLA_TIMED("ssm_steps", k_ssm_steps<64>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
-  return HLA_TIMED("ssm_steps", k_ssm_steps<32>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
-}
-
 template <typename T, int NU>
 static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
   constexpr int Q = Kind<T>::Q;
   const SsmWs c = carve(ws, a.B * a.H, a.n, a.P, a.N, Q);
   hipError_t e = launch_steps(a, c.tab, c.tot, Q, s);
   if (e != hipSuccess) return e;
-  WalkArgs w{};
+  WalkPair pair{};
+  WalkArgs& w = pair.a[0];
   w.x = a.x; w.k = a.Bm; w.q = a.Cm;
   w.D = a.D; w.tab = c.tab; w.tot = c.tot; w.ends = c.ends; w.segdec = c.segdec;
   w.state = a.state; w.y = a.y;
@@ -119,11 +65,11 @@ static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
   w.plan = ssm_plan(a.B * a.H, a.n, Q);
   if (w.plan.segs > 1) {
     w.segs_run = w.plan.segs - 1;
-    e = walk_pn<T, kEnds, NU, false>(w, a.B, s);
+    e = walk_pn<T, kEnds, NU>(pair, 1, a.B, s);
     if (e != hipSuccess) return e;
   }
   w.segs_run = w.plan.segs;
-  return walk_pn<T, kOutputs, NU, false>(w, a.B, s);
+  return walk_pn<T, kOutputs, NU>(pair, 1, a.B, s);
 }
 
 // The scaled inputs go into the state in three pieces where the state is an

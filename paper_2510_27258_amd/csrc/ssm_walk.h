@@ -24,6 +24,12 @@ struct WalkArgs {
   int n, H, P, G, N, tok;
   SsmPlan plan;
   int segs_run;               // segments of this launch
+  int rev;                    // from the last tile to the first, weights 2^L
+};
+
+// Up to two walks of the same sizes in a launch (the gradients' states, both ways).
+struct WalkPair {
+  WalkArgs a[2];
 };
 
 template <int PP>
@@ -44,10 +50,12 @@ struct WalkLds {
 // One workgroup walks one segment of one head; wave w owns 16 CB columns of
 // the state, h[n = 16 nb + 4g + i][p = 16 (w CB + cb) + r], in accumulators.
 // NU pieces carry the scaled inputs into the state; the readout's rounding
-// (one piece of the state and of the scores for bf16 outputs, 2^-9 of each
+// (one piece of the state and of the scores for bf16 outputs, 2^-8 of each
 // term, as large as the output's own rounding; three for fp32) is NX.
-template <typename T, int PP, int NN, int MODE, int NU, bool REV>
-__global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkArgs a) {
+template <typename T, int PP, int NN, int MODE, int NU>
+__global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkPair pair) {
+  const WalkArgs& a = pair.a[blockIdx.y];
+  const bool REV = a.rev;
   using W = Waves<PP>;
   using L_ = WalkLds<T, PP, NN, MODE>;
   constexpr int NW = W::NW, THR = W::THR, CB = W::CB, NX = L_::NX, Q = L_::Q, NB = NN / 16, KN = NN / 32;
@@ -345,34 +353,88 @@ __global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkArgs a) {
   }
 }
 
-template <typename T, int PP, int NN, int MODE, int NU, bool REV>
-hipError_t walk(const WalkArgs& a, int B, hipStream_t s) {
+template <typename T, int PP, int NN, int MODE, int NU>
+hipError_t walk(const WalkPair& a, int count, int B, hipStream_t s) {
   constexpr size_t lds = sizeof(WalkLds<T, PP, NN, MODE>);
   static_assert(lds <= 160 * 1024, "fits a CU's LDS");
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ssm_walk<T, PP, NN, MODE, NU, REV>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ssm_walk<T, PP, NN, MODE, NU>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
   constexpr const char* name = MODE == kEnds ? "ssm_ends" : MODE == kOutputs ? "ssm_outputs" : "ssm_states";
-  return HLA_TIMED(name, (k_ssm_walk<T, PP, NN, MODE, NU, REV>), dim3((unsigned)(B * a.H * a.segs_run)),
+  return HLA_TIMED(name, (k_ssm_walk<T, PP, NN, MODE, NU>), dim3((unsigned)(B * a.a[0].H * a.a[0].segs_run), count),
                    dim3(Waves<PP>::THR), lds, s, a);
 }
 
-template <typename T, int PP, int MODE, int NU, bool REV>
-hipError_t walk_n(const WalkArgs& a, int B, hipStream_t s) {
-  if (a.N <= 32) return walk<T, PP, 32, MODE, NU, REV>(a, B, s);
-  if (a.N <= 64) return walk<T, PP, 64, MODE, NU, REV>(a, B, s);
-  return walk<T, PP, 128, MODE, NU, REV>(a, B, s);
+template <typename T, int PP, int MODE, int NU>
+hipError_t walk_n(const WalkPair& a, int count, int B, hipStream_t s) {
+  if (a.a[0].N <= 32) return walk<T, PP, 32, MODE, NU>(a, count, B, s);
+  if (a.a[0].N <= 64) return walk<T, PP, 64, MODE, NU>(a, count, B, s);
+  return walk<T, PP, 128, MODE, NU>(a, count, B, s);
 }
-template <typename T, int MODE, int NU, bool REV>
-hipError_t walk_pn(const WalkArgs& a, int B, hipStream_t s) {
-  if (a.P <= 32) return walk_n<T, 32, MODE, NU, REV>(a, B, s);
-  if (a.P <= 64) return walk_n<T, 64, MODE, NU, REV>(a, B, s);
-  return walk_n<T, 128, MODE, NU, REV>(a, B, s);
+template <typename T, int MODE, int NU>
+hipError_t walk_pn(const WalkPair& a, int count, int B, hipStream_t s) {
+  if (a.a[0].P <= 32) return walk_n<T, 32, MODE, NU>(a, count, B, s);
+  if (a.a[0].P <= 64) return walk_n<T, 64, MODE, NU>(a, count, B, s);
+  return walk_n<T, 128, MODE, NU>(a, count, B, s);
 }
 
-constexpr int walk_waves(int P) { return P <= 32 ? 2 : 4; }
+// A wave: 64 tokens of one (sequence, head).  Sums in fp64: L reaches the
+// hundreds, where fp32 sums would put 1e-5 into the weights of neighbours.
+template <int Q>
+__global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab, float* __restrict__ tot, int tok,
+                                                   int tiles) {
+  const int wv = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
+  const int head = wv % a.H, blk = (wv / a.H) % (tok / 64), b = wv / a.H / (tok / 64);
+  if (b >= a.B) return;
+  const int t = blk * 64 + lane, bh = b * a.H + head;
+  float dt = 0.f;
+  double la = 0.0;
+  if (t < a.n) {
+    dt = load_any(a.dt.p, a.dt_dtype, (size_t)(b * a.dt.bs + t * a.dt.ts + head));
+    if (a.dt_bias) dt += a.dt_bias[head];
+    if (a.softplus) dt = dt > 20.f ? dt : log1pf(expf(dt));
+    la = (double)dt * (double)a.A[head] * 1.4426950408889634;
+  }
+  double L = la;
+#pragma unroll
+  for (int m = 1; m < Q; m *= 2) {
+    const double o = __shfl_up(L, m, Q);
+    if ((lane & (Q - 1)) >= m) L += o;
+  }
+  const double end = __shfl(L, Q - 1, Q);
+  Step s;
+  s.Lh = (float)L;
+  s.Ll = (float)(L - (double)s.Lh);
+  s.dt = dt;
+  s.w = dt * exp2_((float)(end - L));
+  tab[(size_t)bh * tok + t] = s;
+  if ((lane & (Q - 1)) == Q - 1 && t / Q < tiles) tot[(size_t)bh * tiles + t / Q] = (float)end;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Segments a head: walks for two workgroups a CU, each of at least four tiles.
+inline SsmPlan ssm_plan(int BH, int n, int Q) {
+  SsmPlan p;
+  p.tiles = (n + Q - 1) / Q;
+  int segs = BH >= 512 ? 1 : (512 + BH - 1) / BH;
+  if (segs > p.tiles / 4) segs = p.tiles / 4;
+  if (segs < 1) segs = 1;
+  p.per = (p.tiles + segs - 1) / segs;
+  p.segs = (p.tiles + p.per - 1) / p.per;
+  return p;
+}
+
+inline hipError_t launch_steps(const Ssm& a, Step* tab, float* tot, int Q, hipStream_t s) {
+  const int tok = (a.n + 63) / 64 * 64, tiles = (a.n + Q - 1) / Q;
+  const long long waves = (long long)a.B * a.H * (tok / 64);
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (Q == 64) return HLA_TIMED("ssm_steps", k_ssm_steps<64>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
+  return HLA_TIMED("ssm_steps", k_ssm_steps<32>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
+}
+
 constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
 }  // namespace

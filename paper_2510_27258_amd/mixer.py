@@ -340,3 +340,38 @@ def ssm_step(state, x_t, dt_t, A, B_t, C_t, D=None, dt_bias=None, softplus=True,
         capi.hla_ssm_step(state.data_ptr(), *rx[:2], *rt[:2], A.data_ptr(), *rb[:2], *rc[:2], _ptr(D), _ptr(dt_bias),
                           out.data_ptr(), B, H, P, G, N, int(bool(softplus)), *codes, stream)
     return out
+
+
+def ssm_backward(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus=True):
+    """Gradients (dx, ddt, dA, dBm, dCm, dD, ddt_bias) of ssm_forward for dy
+    [B, n, H, P], bf16 inputs; None for a D or dt_bias not given."""
+    (rx, rt, rb, rc), sizes, codes = _ssm_args(x, dt, A, Bm, Cm, D, dt_bias)
+    _same("dy", dy, x.shape, x.dtype, x.device)
+    ry = _rows("dy", dy, 2)
+    dx, ddt, dB, dC = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (x, dt, Bm, Cm))
+    dA, dD, db = (None if t is None else torch.empty_like(t) for t in (A, D, dt_bias))
+    ws, nb = _space(capi.hla_ssm_backward_workspace_bytes(*sizes, codes[0]), x.device)
+    with _Device(x) as stream:
+        capi.hla_ssm_backward(*rx, *rt, A.data_ptr(), *rb, *rc, _ptr(D), _ptr(dt_bias), *ry, dx.data_ptr(),
+                              ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), _ptr(dD), _ptr(db), *sizes,
+                              int(bool(softplus)), *codes, ws.data_ptr(), nb, stream)
+    return dx, ddt, dA, dB, dC, dD, db
+
+
+class SSMScan(torch.autograd.Function):
+    """ssm_forward as a differentiable op (bf16 inputs)."""
+
+    @staticmethod
+    def forward(ctx, x, dt, A, Bm, Cm, D, dt_bias, softplus):
+        ctx.save_for_backward(x, dt, A, Bm, Cm, D, dt_bias)
+        ctx.softplus = softplus
+        return ssm_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus)
+
+    @staticmethod
+    def backward(ctx, dy):
+        return (*ssm_backward(*ctx.saved_tensors, dy.contiguous(), ctx.softplus), None)
+
+
+def ssm_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus=True):
+    """Differentiable ssm_forward."""
+    return SSMScan.apply(x, dt, A, Bm, Cm, D, dt_bias, softplus)
