@@ -531,15 +531,9 @@ hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {
     w.tab = c.tab; w.tot = c.tot; w.ends = c.ends[i]; w.segdec = c.segdec[i]; w.carry = c.carry[i];
     w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
     w.plan = ssm_plan(a.B * a.H, a.n, kGQ);
-    w.segs_run = w.plan.segs - 1;
     w.rev = i;
   }
-  if (pair.a[0].segs_run > 0) {
-    e = walk_pn<bf16, kEnds, 3>(pair, 2, a.B, s);
-    if (e != hipSuccess) return e;
-  }
-  pair.a[0].segs_run = pair.a[1].segs_run = pair.a[0].plan.segs;
-  e = walk_pn<bf16, kStates, 3>(pair, 2, a.B, s);
+  e = walk_all<bf16, kStates, 3>(pair, 2, a.B, s);
   if (e != hipSuccess) return e;
 
   GradArgs d{};

@@ -63,13 +63,7 @@ static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
   w.state = a.state; w.y = a.y;
   w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
   w.plan = ssm_plan(a.B * a.H, a.n, Q);
-  if (w.plan.segs > 1) {
-    w.segs_run = w.plan.segs - 1;
-    e = walk_pn<T, kEnds, NU>(pair, 1, a.B, s);
-    if (e != hipSuccess) return e;
-  }
-  w.segs_run = w.plan.segs;
-  return walk_pn<T, kOutputs, NU>(pair, 1, a.B, s);
+  return walk_all<T, kOutputs, NU>(pair, 1, a.B, s);
 }
 
 // The scaled inputs go into the state in three pieces where the state is an

@@ -153,49 +153,39 @@ struct Tile {
     for (int i = 0; i < CNT; ++i) {
       const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
       uint16_t* to = X + row * LD + c;
-      const uint32_t a[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
       if constexpr (NX == 1) {
         // an exponent of all ones carries into the bit above it
-#pragma unroll
-        for (int k = 0; k < 4; ++k) bad |= (a[k] & 0x7f807f80u) + 0x00800080u;
+        bad |= (r[i].x & 0x7f807f80u) + 0x00800080u;
+        bad |= (r[i].y & 0x7f807f80u) + 0x00800080u;
+        bad |= (r[i].z & 0x7f807f80u) + 0x00800080u;
+        bad |= (r[i].w & 0x7f807f80u) + 0x00800080u;
         *reinterpret_cast<uint4*>(to) = r[i];
       } else {
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          bad |= (a[k] & 0x7f800000u) + 0x00800000u;
-          v[k] = __uint_as_float(a[k]);
-        }
+        const float v[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z),
+                            __uint_as_float(r[i].w)};
         uint2 p[NX];
         pieces4<NX>(v, p);
+        bad |= (p[0].x & 0x7f807f80u) + 0x00800080u;
+        bad |= (p[0].y & 0x7f807f80u) + 0x00800080u;
 #pragma unroll
         for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(to + k * PLANE) = p[k];
       }
     }
-    return (bad & (NX == 1 ? 0x80008000u : 0x80000000u)) != 0;
+    return (bad & 0x80008000u) != 0;
   }
 
-  // After store() found one: such values become zeros in the tile, and the
-  // first token that held one goes to first[column] (per column) or first[0].
+  // After a store() found one: such values of the tile become zeros, and the
+  // first token that held one goes to first[column] (COLS) or first[0].
   template <bool COLS>
-  __device__ __forceinline__ void mend(uint16_t* X, int* first, int tid) const {
+  static __device__ __forceinline__ void mend(uint16_t* X, int* first, int tid) {
+#pragma unroll 1
+    for (int e = tid; e < Q * W; e += THR) {
+      const int row = e / W, c = e % W;
+      uint16_t* x = X + row * LD + c;
+      if ((*x & 0x7f80u) != 0x7f80u) continue;
 #pragma unroll
-    for (int i = 0; i < CNT; ++i) {
-      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
-      const uint32_t a[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        bool bad;
-        if constexpr (NX == 1)
-          bad = ((k & 1 ? a[k / 2] >> 16 : a[k / 2]) & 0x7f80u) == 0x7f80u;
-        else
-          bad = (a[k] & 0x7f800000u) == 0x7f800000u;
-        if (bad) {
-#pragma unroll
-          for (int p = 0; p < NX; ++p) X[p * PLANE + row * LD + c + k] = 0;
-          atomicMin(first + (COLS ? c + k : 0), row);
-        }
-      }
+      for (int k = 0; k < NX; ++k) x[k * PLANE] = 0;
+      atomicMin(first + (COLS ? c : 0), row);
     }
   }
 };

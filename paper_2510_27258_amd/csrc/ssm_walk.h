@@ -24,6 +24,7 @@ struct WalkArgs {
   int n, H, P, G, N, tok;
   SsmPlan plan;
   int segs_run;               // segments of this launch
+  int summed;                 // ends[s] is the state after segment s
   int rev;                    // from the last tile to the first, weights 2^L
 };
 
@@ -47,13 +48,39 @@ struct WalkLds {
   int first[PP], first_all, bad[2];
 };
 
+// ends[s] += decay ends[s - 1], s = 1 .. segs - 2: the state after each segment.
+// Beyond kOwnSums earlier segments (the sum is then longer than a launch), so
+// that no walk reads more than one.  V: float4s a slot.
+constexpr int kOwnSums = 3;
+__global__ __launch_bounds__(256) void k_ssm_carry(WalkPair pair, int V) {
+  const WalkArgs& a = pair.a[blockIdx.z];
+  const int i = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y, segs = a.plan.segs;
+  if (i >= V) return;
+  f32x4* e = reinterpret_cast<f32x4*>(a.ends) + (size_t)bh * segs * V + i;
+  const float* d = a.segdec + (size_t)bh * segs;
+  f32x4 sum = e[0];
+  constexpr int U = 8;
+  for (int s = 1; s < segs - 1; s += U) {
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u < segs - 1) x[u] = e[(size_t)(s + u) * V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u < segs - 1) {
+        sum = sum * d[s + u] + x[u];
+        e[(size_t)(s + u) * V] = sum;
+      }
+  }
+}
+
 // One workgroup walks one segment of one head; wave w owns 16 CB columns of
 // the state, h[n = 16 nb + 4g + i][p = 16 (w CB + cb) + r], in accumulators.
 // NU pieces carry the scaled inputs into the state; the readout's rounding
 // (one piece of the state and of the scores for bf16 outputs, 2^-8 of each
 // term, as large as the output's own rounding; three for fp32) is NX.
 template <typename T, int PP, int NN, int MODE, int NU>
-__global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkPair pair) {
+__global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_walk(WalkPair pair) {
   const WalkArgs& a = pair.a[blockIdx.y];
   const bool REV = a.rev;
   using W = Waves<PP>;
@@ -142,9 +169,9 @@ __global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkPair pair) {
       }
     }
   } else {
-    // segment 0's end state holds the first state
-    for (int s = 0; s < seg; ++s) {
-      const float d = a.segdec[(size_t)bh * a.plan.segs + s];
+    // segment 0's end state holds the first state; summed slots (k_ssm_carry) hold all before them
+    for (int s = a.summed ? seg - 1 : 0; s < seg; ++s) {
+      const float d = a.summed ? 0.f : a.segdec[(size_t)bh * a.plan.segs + s];
       const f32x4* from = slot(s);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -183,8 +210,8 @@ __global__ __launch_bounds__(Waves<PP>::THR) void k_ssm_walk(WalkPair pair) {
       // an infinite or NaN input must not reach the tile's earlier tokens
       // through a zero weight: it is taken out here and its column (k: every
       // column) set to NaN from its token on
-      tk.template mend<false>(S.k, &S.first_all, tid);
-      tx.template mend<true>(S.x, S.first, tid);
+      Tile<T, NN, THR>::template mend<false>(S.k, &S.first_all, tid);
+      Tile<T, PP, THR>::template mend<true>(S.x, S.first, tid);
       lds_barrier();
     }
     if (i + 1 < i1) fetch(i + 1);
@@ -436,6 +463,27 @@ inline hipError_t launch_steps(const Ssm& a, Step* tab, float* tot, int Q, hipSt
 }
 
 constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+
+// The walks of `pair` in full: ends, their sums, then MODE.
+template <typename T, int MODE, int NU>
+hipError_t walk_all(WalkPair& pair, int count, int B, hipStream_t s) {
+  const WalkArgs& a = pair.a[0];
+  const int segs = a.plan.segs;
+  if (segs > 1) {
+    for (int i = 0; i < count; ++i) pair.a[i].segs_run = segs - 1;
+    hipError_t e = walk_pn<T, kEnds, NU>(pair, count, B, s);
+    if (e != hipSuccess) return e;
+    if (segs - 1 > kOwnSums) {
+      const int V = padded(a.P) * padded(a.N) / 4;
+      e = HLA_TIMED("ssm_carry", k_ssm_carry, dim3((V + 255) / 256, B * a.H, count), dim3(256), 0, s, pair, V);
+      if (e != hipSuccess) return e;
+      for (int i = 0; i < count; ++i) pair.a[i].summed = 1;
+    }
+  }
+  for (int i = 0; i < count; ++i) pair.a[i].segs_run = segs;
+  return walk_pn<T, MODE, NU>(pair, count, B, s);
+}
 
 }  // namespace
 }  // namespace hla
