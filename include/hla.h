@@ -438,7 +438,8 @@ int hla_qk_norm_rope_backward(const void *q, long long q_bs, long long q_ts, con
  * the last; without it the scan starts from zero.
  * P and N: multiples of 16 from 16 to 128; G divides H; B*H <= 65535;
  * B*H*n < 2^31.  A <= 0 is meant (a growing state may overflow).  x, Bm, Cm:
- * 16-byte aligned, strides of whole 16-byte pieces.  bf16 inputs: scores and
+ * 16-byte aligned, strides of whole 16-byte pieces, the rows of a sequence not
+ * overlapping.  bf16 inputs: scores and
  * the state that the outputs read are rounded to bf16 (2^-8 of a term, as the
  * outputs are), the state itself is kept in fp32.  An infinite or NaN input
  * gives NaN in every output that depends on it, and in no other.

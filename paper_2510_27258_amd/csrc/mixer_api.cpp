@@ -138,22 +138,28 @@ int ssm_sizes(int B, int n, int H, int P, int G, int N) {
   return HLA_OK;
 }
 
-int ssm_rows(const hla::Rows& r, int dtype, const char* name) {
+// Rows of w elements, n of them a sequence.  The kernels' tiles end where the
+// next row would begin, so rows must not overlap; the stride of a single row
+// is not used and set to one that does not.
+int ssm_rows(hla::Rows& r, int n, int w, int dtype, const char* name) {
+  if (n == 1) r.ts = w;
   const int rc = check_rows(r, dtype, name);
   if (rc) return rc;
+  if (r.ts < w)
+    return fail(HLA_ERR_INVALID, "%s: a token stride of %lld elements makes rows of %d overlap", name, r.ts, w);
   // a tile's rows are addressed with 32-bit byte offsets
   if (r.ts * 64 * esize(dtype) >= (1LL << 30))
     return fail(HLA_ERR_UNSUPPORTED, "%s: a token stride of %lld elements is too long", name, r.ts);
   return HLA_OK;
 }
 
-int ssm_check(const hla::Ssm& a) {
+int ssm_check(hla::Ssm& a) {
   int rc;
   if ((rc = ssm_sizes(a.B, a.n, a.H, a.P, a.G, a.N)) || (rc = check_flag(a.softplus, "softplus")) ||
       (rc = check_type(a.dtype, "dtype")) || (rc = check_type(a.dt_dtype, "dt_dtype")))
     return rc;
-  if ((rc = ssm_rows(a.x, a.dtype, "x")) || (rc = ssm_rows(a.Bm, a.dtype, "Bm")) ||
-      (rc = ssm_rows(a.Cm, a.dtype, "Cm")) || (rc = check_own(a.dt.p, esize(a.dt_dtype), "dt")) ||
+  if ((rc = ssm_rows(a.x, a.n, a.H * a.P, a.dtype, "x")) || (rc = ssm_rows(a.Bm, a.n, a.G * a.N, a.dtype, "Bm")) ||
+      (rc = ssm_rows(a.Cm, a.n, a.G * a.N, a.dtype, "Cm")) || (rc = check_own(a.dt.p, esize(a.dt_dtype), "dt")) ||
       (rc = check_stride(a.dt.bs, a.dt.ts, "dt")) || (rc = check_own(a.A, 4, "A")) ||
       (rc = check_own(a.D, 4, "D", false)) || (rc = check_own(a.dt_bias, 4, "dt_bias", false)))
     return rc;
@@ -320,7 +326,7 @@ int hla_ssm_backward(const void* x, long long x_bs, long long x_ts, const void* 
   int rc;
   if ((rc = ssm_check(a)) != HLA_OK) return rc;
   if (dtype != HLA_BF16) return fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
-  if ((rc = ssm_rows(a.dy, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
+  if ((rc = ssm_rows(a.dy, n, H * P, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
       (rc = check_own(ddt, esize(dt_dtype), "ddt")) || (rc = check_own(dA, 4, "dA")) || (rc = check_16(dBm, "dBm")) ||
       (rc = check_16(dCm, "dCm")) || (rc = check_own(dD, 4, "dD", false)) ||
       (rc = check_own(ddt_bias, 4, "ddt_bias", false)) ||

@@ -42,7 +42,7 @@ struct GradArgs {
 
 template <int PP, int NN>
 struct GradLds {
-  static constexpr int LDK = NN + kSsmPad, LDX = PP + kSsmPad, LDP = kGQ + kSsmPad;
+  static constexpr int LDK = ld_of(NN), LDX = ld_of(PP), LDP = ld_of(kGQ);
   uint16_t k[kGQ * LDK];
   union {
     uint16_t q[kGQ * LDK];
@@ -93,17 +93,21 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   const uint16_t* xp = static_cast<const uint16_t*>(a.x.p) + b * a.x.bs + t0 * a.x.ts;
   const uint16_t* yp = static_cast<const uint16_t*>(a.dy.p) + b * a.dy.bs + t0 * a.dy.ts;
 
-  Tile<bf16, NN, 256> tn;
-  Tile<bf16, PP, 256> tx, ty;
+  using TN = Tile<bf16, NN, 256>;
+  using TP = Tile<bf16, PP, 256>;
+  TN tn;
+  TP tx, ty;
+  const uint32_t x1 = TP::first(a.x.ts, a.P, tid), xby = TP::step(a.x.ts);
+  const uint32_t y1 = TP::first(a.dy.ts, a.P, tid), yby = TP::step(a.dy.ts);
   Step st{};
   auto fetch = [&](int head) {
-    tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, a.x.ts, a.P, tid);
-    ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, a.dy.ts, a.P, tid);
+    tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, a.x.ts, a.P, x1, xby);
+    ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, a.dy.ts, a.P, y1, yby);
     if (tid < kGQ) st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + tid];
   };
-  tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, tid);
+  tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, TN::first(a.k.ts, a.N, tid), TN::step(a.k.ts));
   tn.store(S.k, tid);
-  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, tid);
+  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.store(S.q, tid);
   if (heads > 0) fetch(head0);
   lds_barrier();
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   }
 
   // the tile's own part of dB and dC: the heads' sum z[t][s] with C and B
-  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, tid);
+  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.store(S.q, tid);
 #pragma unroll
   for (int sb = 0; sb < TB; ++sb)
@@ -528,7 +532,7 @@ hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {
     WalkArgs& w = pair.a[i];
     w.x = i ? a.dy : a.x;
     w.k = i ? a.Cm : a.Bm;
-    w.tab = c.tab; w.tot = c.tot; w.ends = c.ends[i]; w.segdec = c.segdec[i]; w.carry = c.carry[i];
+    w.tab = c.tab; w.ends = c.ends[i]; w.segdec = c.segdec[i]; w.carry = c.carry[i];
     w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
     w.plan = ssm_plan(a.B * a.H, a.n, kGQ);
     w.rev = i;

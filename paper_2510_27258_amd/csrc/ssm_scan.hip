@@ -59,7 +59,7 @@ static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
   WalkPair pair{};
   WalkArgs& w = pair.a[0];
   w.x = a.x; w.k = a.Bm; w.q = a.Cm;
-  w.D = a.D; w.tab = c.tab; w.tot = c.tot; w.ends = c.ends; w.segdec = c.segdec;
+  w.D = a.D; w.tab = c.tab; w.ends = c.ends; w.segdec = c.segdec;
   w.state = a.state; w.y = a.y;
   w.n = a.n; w.H = a.H; w.P = a.P; w.G = a.G; w.N = a.N; w.tok = (a.n + 63) / 64 * 64;
   w.plan = ssm_plan(a.B * a.H, a.n, Q);

@@ -19,7 +19,11 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kSsmPad = 16;   // bf16 elements of padding a row: transposed and row reads both spread over the banks
+// Row stride of an LDS tile of W bf16 values, a dwords: a/4 is odd modulo 16, so
+// that 16 rows' 8- or 16-byte reads at one column fall into different banks
+// (of 64), and 0, a, 2a, 3a are 8 banks apart or more, so that the four rows a
+// transposed read takes do too: a = 28, 36, 76 for W = 32, 64, 128.
+__host__ __device__ constexpr int ld_of(int W) { return W == 64 ? 72 : W + 24; }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float nan_() { return __builtin_nanf(""); }
@@ -30,6 +34,24 @@ __device__ __forceinline__ rsrc_t rows_rsrc(const void* p, long long bytes) {
 __device__ __forceinline__ uint4 load16(rsrc_t r, uint32_t off) {
   const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
   return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+__device__ __forceinline__ void store8(rsrc_t r, uint32_t off, const uint2& v) {
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2{v.x, v.y}, r, (int)off, 0, 0);
+}
+__device__ __forceinline__ void store16(rsrc_t r, uint32_t off, const float (&v)[4]) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(
+      u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, r, (int)off, 0,
+      0);
+}
+
+// x through an empty asm statement: what is computed from it is computed where
+// it is used, not hoisted out of the walk and kept in registers (or spilled) through it.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // v_mfma_f32_16x16x32_bf16, lane l = 16 g + r:
@@ -132,18 +154,29 @@ template <typename T, int W, int THR>
 struct Tile {
   static constexpr int Q = Kind<T>::Q, V = Kind<T>::V, NX = Kind<T>::NX;
   static constexpr int PR = W / V, TOT = Q * PR, CNT = (TOT + THR - 1) / THR;
-  static_assert(TOT % THR == 0, "whole pieces a thread");
-  static constexpr int LD = W + kSsmPad, PLANE = Q * LD;
+  static_assert(TOT % THR == 0 && THR % PR == 0, "whole pieces a thread, all of one column");
+  static constexpr uint32_t kOut = 0x80000000u;    // past any tile: reads zeros
+  static constexpr int LD = ld_of(W), PLANE = Q * LD;
   uint4 r[CNT];
 
-  // base: the tile's first row; rows valid rows; ts elements between them; w values each
-  __device__ __forceinline__ void load(const T* base, int rows, long long ts, int w, int tid) {
-    const rsrc_t rs = rows_rsrc(base, rows > 0 ? ((long long)(rows - 1) * ts + w) * (long long)sizeof(T) : 0);
+  // This thread's first piece and the bytes between its pieces, for rows ts >= w elements apart, w values each.
+  static __device__ __forceinline__ uint32_t first(long long ts, int w, int tid) {
+    const int row = tid / PR, c = (tid % PR) * V;
+    return c < w ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : kOut;
+  }
+  static __device__ __forceinline__ uint32_t step(long long ts) { return (THR / PR) * (uint32_t)ts * sizeof(T); }
+  // The tile from its first row on, of which `rows` are valid: the others lie past the resource's end.
+  __device__ __forceinline__ void load(const T* base, int rows, long long ts, int w, uint32_t off, uint32_t by) {
+    const rsrc_t rs = rows_rsrc(base, ((long long)(rows - 1) * ts + w) * (long long)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < CNT; ++i) {
-      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
-      r[i] = load16(rs, row < rows && c < w ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : 0x80000000u);
-    }
+    for (int i = 0; i < CNT; ++i) r[i] = load16(rs, off + i * by);
+  }
+
+  // The largest magnitudes of the low and the high halves so far, as bit patterns.
+  static __device__ __forceinline__ void note(uint32_t& most, uint32_t pair) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 a = __builtin_bit_cast(u16x2, pair & 0x7fff7fffu), m = __builtin_bit_cast(u16x2, most);
+    most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, m));
   }
 
   // The tile as NX planes of Q rows.  Returns whether a value of this thread's is infinite or NaN.
@@ -154,24 +187,23 @@ struct Tile {
       const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
       uint16_t* to = X + row * LD + c;
       if constexpr (NX == 1) {
-        // an exponent of all ones carries into the bit above it
-        bad |= (r[i].x & 0x7f807f80u) + 0x00800080u;
-        bad |= (r[i].y & 0x7f807f80u) + 0x00800080u;
-        bad |= (r[i].z & 0x7f807f80u) + 0x00800080u;
-        bad |= (r[i].w & 0x7f807f80u) + 0x00800080u;
+        note(bad, r[i].x);
+        note(bad, r[i].y);
+        note(bad, r[i].z);
+        note(bad, r[i].w);
         *reinterpret_cast<uint4*>(to) = r[i];
       } else {
         const float v[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z),
                             __uint_as_float(r[i].w)};
         uint2 p[NX];
         pieces4<NX>(v, p);
-        bad |= (p[0].x & 0x7f807f80u) + 0x00800080u;
-        bad |= (p[0].y & 0x7f807f80u) + 0x00800080u;
+        note(bad, p[0].x);
+        note(bad, p[0].y);
 #pragma unroll
         for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(to + k * PLANE) = p[k];
       }
     }
-    return (bad & 0x80008000u) != 0;
+    return (bad & 0xffffu) >= 0x7f80u || bad >= 0x7f800000u;
   }
 
   // After a store() found one: such values of the tile become zeros, and the

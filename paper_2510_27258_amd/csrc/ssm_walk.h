@@ -15,7 +15,6 @@ struct WalkArgs {
   Rows x, k, q;               // x [B, n, H, P]; k, q [B, n, G, N] (backwards: dy and C in x's and k's place)
   const float* D;             // [H] or null
   const Step* tab;            // [B H][tok]
-  const float* tot;           // [B H][tiles]
   float* ends;                // [B H][segs] end states in the walk's own order; slot segs - 1: the first state
   float* segdec;              // [B H][segs] decay over a segment
   float* state;               // [B, H, N, P] or null
@@ -41,10 +40,11 @@ struct Waves {
 template <typename T, int PP, int NN, int MODE>
 struct WalkLds {
   static constexpr int NX = Kind<T>::NX, Q = Kind<T>::Q;
-  static constexpr int LDK = NN + kSsmPad, LDX = PP + kSsmPad, LDS_ = Q + kSsmPad;
+  static constexpr int LDK = ld_of(NN), LDX = ld_of(PP), LDS_ = ld_of(Q);
   uint16_t k[NX * Q * LDK], x[NX * Q * LDX];
   uint16_t q[MODE == kOutputs ? NX * Q * LDK : 8], s[MODE == kOutputs ? NX * Q * LDS_ : 8];
   float Lh[Q], Ll[Q], dt[Q], w[Q];
+  float cf[Q], end[Q / 16];     // dt_s 2^(L of its 16 tokens' last - L_s), and those L
   int first[PP], first_all, bad[2];
 };
 
@@ -105,18 +105,41 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
   const T* qp = MODE == kOutputs ? static_cast<const T*>(a.q.p) + b * a.q.bs + (long long)(head / (a.H / a.G)) * a.N
                                  : nullptr;
   const Step* tab = a.tab + (size_t)bh * a.tok;
+  // outputs: row r of a 16-token block, columns pw + 4g .. + 3 of a column block
+  T* yp = MODE == kOutputs ? static_cast<T*>(a.y) + (size_t)b * a.n * a.H * a.P : nullptr;
+  const int ystep = 16 * a.H * a.P * (int)sizeof(T);
+  const uint32_t yoff = (uint32_t)((r * a.H * a.P + head * a.P + pw + 4 * g) * (int)sizeof(T));
 
   Tile<T, NN, THR> tk, tq;
   Tile<T, PP, THR> tx;
   Step st{};
+  const long long kts = a.k.ts, xts = a.x.ts, qts = a.q.ts;
+  const uint32_t k1 = Tile<T, NN, THR>::first(kts, a.N, tid), kby = Tile<T, NN, THR>::step(kts);
+  const uint32_t x1 = Tile<T, PP, THR>::first(xts, a.P, tid), xby = Tile<T, PP, THR>::step(xts);
+  const uint32_t q1 = Tile<T, NN, THR>::first(qts, a.N, tid), qby = Tile<T, NN, THR>::step(qts);
+  // no branches here: a wait after one would be for every load in flight
   auto fetch = [&](int i) {
     const int t0 = (REV ? M - 1 - i : i) * Q, rows = min(Q, a.n - t0);
-    tk.load(kp + t0 * a.k.ts, rows, a.k.ts, a.N, tid);
-    tx.load(xp + t0 * a.x.ts, rows, a.x.ts, a.P, tid);
-    if (MODE == kOutputs) tq.load(qp + t0 * a.q.ts, rows, a.q.ts, a.N, tid);
-    if (tid < Q) st = tab[t0 + tid];
+    st = tab[t0 + (tid & (Q - 1))];
+    tk.load(kp + t0 * kts, rows, kts, a.N, k1, kby);
+    tx.load(xp + t0 * xts, rows, xts, a.P, x1, xby);
+    if (MODE == kOutputs) tq.load(qp + t0 * qts, rows, qts, a.N, q1, qby);
   };
   fetch(i0);
+  if (MODE == kOutputs) {
+    // as many stores (dropped: an empty resource) as a tile has, so that the
+    // loop's waits for its loads count the stores behind them on every path and need not drain them
+    const rsrc_t none = rows_rsrc(yp, 0);
+#pragma unroll
+    for (int e = 0; e < TB * CB; ++e) {
+      if constexpr (NX == 1) {
+        store8(none, 0, make_uint2(0, 0));
+      } else {
+        const float z[4] = {0.f, 0.f, 0.f, 0.f};
+        store16(none, 0, z);
+      }
+    }
+  }
 
   f32x4 h[NB][CB];
   // the [N][P] record of a head
@@ -191,8 +214,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
   float segL = 0.f;
   for (int i = i0; i < i1; ++i) {
     const int tile = REV ? M - 1 - i : i, t0 = tile * Q, par = i & 1;
-    const float Ltile = a.tot[(size_t)bh * M + tile];
-    segL += Ltile;
+    const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
     bool bad = tk.store(S.k, tid);
     bad |= tx.store(S.x, tid);
     if (MODE == kOutputs) tq.store(S.q, tid);
@@ -201,6 +223,11 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
       S.Ll[tid] = st.Ll;
       S.dt[tid] = st.dt;
       S.w[tid] = REV ? exp2_(st.Lh + st.Ll) : st.w;
+      if (MODE == kOutputs) {
+        const float eh = __shfl(st.Lh, tid | 15), el = __shfl(st.Ll, tid | 15);
+        S.cf[tid] = st.dt * exp2_((eh - st.Lh) + (el - st.Ll));
+        if ((tid & 15) == 15) S.end[tid / 16] = eh + el;
+      }
     }
     if (bad) S.bad[par] = 1;
     lds_barrier();
@@ -221,73 +248,110 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
 
     bf16x8 xf[KS][CB][NX];
     if (MODE == kOutputs) {
-      // scores, transposed (rows s, columns t), weighted and stored as s[t][s]
-      constexpr int WPT = NW > TB ? NW / TB : 1;
+      // scores, transposed (rows s, columns t), weighted and stored as s[t][s].
+      // Below the diagonal blocks M_ts dt_s = 2^(L_t - L_end) (dt_s 2^(L_end - L_s))
+      // with L_end at s's block's last token: both factors at most 1, one
+      // exponential a block and lane.  Blocks above it are zeros, as far as
+      // the products over 32 tokens read them.
+      auto block = [&](int tb, int sb, const bf16x8 (&cf)[KN][NX]) {
+        const int t = 16 * tb + r, s0 = 16 * sb + 4 * g;
+        uint2 p[NX];
 #pragma unroll
-      for (int u0 = 0; u0 < TB * WPT; u0 += NW) {
-        const int u = u0 + w, tb = u / WPT;
-        if (u < TB * WPT) {
-          bf16x8 cf[KN][NX];
+        for (int k = 0; k < NX; ++k) p[k] = make_uint2(0, 0);
+        if (sb <= tb) {
+          f32x4 acc = zero4();
 #pragma unroll
-          for (int k = 0; k < KN; ++k) load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
-          const int t = 16 * tb + r;
-          const float Lt = S.Lh[t], Ltl = S.Ll[t];
-          for (int sb = u % WPT; sb <= (tb | 1); sb += WPT) {
-            f32x4 acc = zero4();
-            if (sb <= tb) {
+          for (int k = 0; k < KN; ++k) {
+            bf16x8 bf[NX];
+            load_frags<NX>(S.k, PK, LDK, 16 * sb, 32 * k, l, bf);
+            mma_pieces<NX, NX>(bf, cf[k], acc);
+          }
+          float v[4];
+          if (sb < tb) {
+            const f32x4 c = *reinterpret_cast<const f32x4*>(S.cf + s0);
+            const float rf = exp2_(S.Lh[t] + S.Ll[t] - S.end[sb]);
 #pragma unroll
-              for (int k = 0; k < KN; ++k) {
-                bf16x8 bf[NX];
-                load_frags<NX>(S.k, PK, LDK, 16 * sb, 32 * k, l, bf);
-                mma_pieces<NX, NX>(bf, cf[k], acc);
-              }
-            }
-            const int s0 = 16 * sb + 4 * g;
-            const float4 Ls = *reinterpret_cast<const float4*>(S.Lh + s0), ds = *reinterpret_cast<const float4*>(S.dt + s0);
-            const float lh[4] = {Ls.x, Ls.y, Ls.z, Ls.w}, dd[4] = {ds.x, ds.y, ds.z, ds.w};
-            float v[4];
+            for (int e = 0; e < 4; ++e) v[e] = acc[e] * (c[e] * rf);
+          } else {
+            const f32x4 lh = *reinterpret_cast<const f32x4*>(S.Lh + s0), ll = *reinterpret_cast<const f32x4*>(S.Ll + s0);
+            const f32x4 dd = *reinterpret_cast<const f32x4*>(S.dt + s0);
+            const float Lt = S.Lh[t], Ltl = S.Ll[t];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float d = Lt - lh[e];
-              if (NX == 3) d += Ltl - S.Ll[s0 + e];
-              v[e] = s0 + e <= t ? acc[e] * (exp2_(d) * dd[e]) : 0.f;
-            }
-            uint2 p[NX];
-            pieces4<NX>(v, p);
+            for (int e = 0; e < 4; ++e)
+              v[e] = s0 + e <= t ? acc[e] * (exp2_((Lt - lh[e]) + (Ltl - ll[e])) * dd[e]) : 0.f;
+          }
+          pieces4<NX>(v, p);
+        }
 #pragma unroll
-            for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(S.s + k * PS + t * LDQ + s0) = p[k];
+        for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(S.s + k * PS + t * LDQ + s0) = p[k];
+      };
+      auto rows_of = [&](int tb, bf16x8 (&cf)[KN][NX]) {
+#pragma unroll
+        for (int k = 0; k < KN; ++k) load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
+      };
+      bf16x8 cfr[KN][NX];
+      if constexpr (TB == 4 && NW == 4) {
+        // ten blocks and two of zeros over four waves: three each at most
+        if (w < 2) {
+          rows_of(3, cfr);
+          block(3, 2 * w, cfr);
+          block(3, 2 * w + 1, cfr);
+          rows_of(w, cfr);
+          block(w, 0, cfr);
+          if (w == 0) block(0, 1, cfr);
+        } else {
+          rows_of(2, cfr);
+          block(2, w == 2 ? 0 : 2, cfr);
+          block(2, w == 2 ? 1 : 3, cfr);
+          if (w == 2) {
+            rows_of(1, cfr);
+            block(1, 1, cfr);
+          }
+        }
+      } else {
+        constexpr int WPT = NW > TB ? NW / TB : 1;
+#pragma unroll
+        for (int u0 = 0; u0 < TB * WPT; u0 += NW) {
+          const int u = u0 + w, tb = u / WPT;
+          if (u < TB * WPT) {
+            rows_of(tb, cfr);
+            for (int sb = u % WPT; sb <= (tb | 1); sb += WPT) block(tb, sb, cfr);
           }
         }
       }
       // the state's part, y^T[p][t] = 2^L_t sum_n h[n][p] q[t][n]
       f32x4 y[TB][CB];
-      bf16x8 hf[KN][CB][NX];
 #pragma unroll
-      for (int k = 0; k < KN; ++k)
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) frag_from_acc<NX>(h[2 * k][cb], h[2 * k + 1][cb], hf[k][cb]);
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb) {
+      for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) y[tb][cb] = zero4();
 #pragma unroll
-        for (int k = 0; k < KN; ++k) {
+      for (int k = 0; k < KN; ++k) {
+        bf16x8 hf[CB][NX];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) frag_from_acc<NX>(h[2 * k][cb], h[2 * k + 1][cb], hf[cb]);
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) {
           bf16x8 cf[NX];
           load_frags_acc<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf);
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NX>(hf[k][cb], cf, y[tb][cb]);
+          for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NX>(hf[cb], cf, y[tb][cb]);
         }
+      }
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
         const float e = exp2_(S.Lh[16 * tb + r] + S.Ll[16 * tb + r]);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) y[tb][cb] *= e;
       }
       lds_barrier();
       // the tile's own part, and the outputs
+      const int l = opaque(tid) & 63, r = l & 15, g = l >> 4;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) load_frags_tr<NX>(S.x, PX, LDX, pw + 16 * cb, 32 * ks, l, xf[ks][cb]);
-      const int rows = min(Q, a.n - t0);
+      const rsrc_t yr = rows_rsrc(yp + (long long)t0 * a.H * a.P, (long long)min(Q, a.n - t0) * a.H * a.P * sizeof(T));
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb) {
 #pragma unroll
@@ -314,17 +378,19 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             v[e] = y[tb][cb][e] + Dh * v[e];
-            if (flagged && t >= min(S.first[c + e], S.first_all)) v[e] = nan_();
           }
-          if (t < rows && c < a.P) {
-            T* to = static_cast<T*>(a.y) + (((size_t)b * a.n + t0 + t) * a.H + head) * a.P + c;
-            if constexpr (NX == 1) {
-              uint2 p[1];
-              pieces4<1>(v, p);
-              *reinterpret_cast<uint2*>(to) = p[0];
-            } else {
-              *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-            }
+          if (flagged) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (t >= min(S.first[c + e], S.first_all)) v[e] = nan_();
+          }
+          const uint32_t off = c < a.P ? yoff + (uint32_t)(tb * ystep) + 16 * cb * sizeof(T) : 0x80000000u;
+          if constexpr (NX == 1) {
+            uint2 p[1];
+            pieces4<1>(v, p);
+            store8(yr, off, p[0]);
+          } else {
+            store16(yr, off, v);
           }
         }
       }
@@ -336,7 +402,8 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
     }
 
     // h <- 2^Ltile h + sum_s k_s (w_s x_s)^T
-    const float dec = exp2_(Ltile);
+    const float Ltile = S.Lh[Q - 1] + S.Ll[Q - 1], dec = exp2_(Ltile);
+    segL += Ltile;
     bf16x8 u[KS][CB][NU];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
