@@ -106,9 +106,9 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
     if (tid < kGQ) st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + tid];
   };
   tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, TN::first(a.k.ts, a.N, tid), TN::step(a.k.ts));
-  tn.store(S.k, tid);
+  tn.template store<false>(S.k, tid);
   tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
-  tn.store(S.q, tid);
+  tn.template store<false>(S.q, tid);
   if (heads > 0) fetch(head0);
   lds_barrier();
 
@@ -143,8 +143,8 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   for (int hh = 0; hh < heads; ++hh) {
     const int head = head0 + hh, bh = b * a.H + head;
     const float Lend = a.tot[(size_t)bh * a.tiles + tile];
-    tx.store(S.x, tid);
-    ty.store(S.dy, tid);
+    tx.template store<false>(S.x, tid);
+    ty.template store<false>(S.dy, tid);
     if (tid < kGQ) {
       S.Lh[tid] = st.Lh;
       S.Ll[tid] = st.Ll;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
 
   // the tile's own part of dB and dC: the heads' sum z[t][s] with C and B
   tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
-  tn.store(S.q, tid);
+  tn.template store<false>(S.q, tid);
 #pragma unroll
   for (int sb = 0; sb < TB; ++sb)
     if (sb <= (w | 1)) {

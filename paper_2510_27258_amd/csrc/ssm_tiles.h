@@ -154,7 +154,8 @@ template <typename T, int W, int THR>
 struct Tile {
   static constexpr int Q = Kind<T>::Q, V = Kind<T>::V, NX = Kind<T>::NX;
   static constexpr int PR = W / V, TOT = Q * PR, CNT = (TOT + THR - 1) / THR;
-  static_assert(TOT % THR == 0 && THR % PR == 0, "whole pieces a thread, all of one column");
+  static_assert((TOT % THR == 0 || TOT < THR) && THR % PR == 0, "whole pieces a thread, all of one column");
+  static constexpr bool kAll = TOT >= THR;         // else the threads past TOT have none
   static constexpr uint32_t kOut = 0x80000000u;    // past any tile: reads zeros
   static constexpr int LD = ld_of(W), PLANE = Q * LD;
   uint4 r[CNT];
@@ -162,7 +163,7 @@ struct Tile {
   // This thread's first piece and the bytes between its pieces, for rows ts >= w elements apart, w values each.
   static __device__ __forceinline__ uint32_t first(long long ts, int w, int tid) {
     const int row = tid / PR, c = (tid % PR) * V;
-    return c < w ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : kOut;
+    return c < w && (kAll || tid < TOT) ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : kOut;
   }
   static __device__ __forceinline__ uint32_t step(long long ts) { return (THR / PR) * (uint32_t)ts * sizeof(T); }
   // The tile from its first row on, of which `rows` are valid: the others lie past the resource's end.
@@ -179,37 +180,42 @@ struct Tile {
     most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, m));
   }
 
-  // The tile as NX planes of Q rows.  Returns whether a value of this thread's is infinite or NaN.
+  // The tile as NX planes of Q rows.  CHECK: returns whether a value of this thread's is infinite or NaN.
+  template <bool CHECK>
   __device__ __forceinline__ bool store(uint16_t* X, int tid) const {
-    uint32_t bad = 0;
+    uint32_t most = 0;
+    if (!kAll && tid >= TOT) return false;
 #pragma unroll
     for (int i = 0; i < CNT; ++i) {
       const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
       uint16_t* to = X + row * LD + c;
       if constexpr (NX == 1) {
-        note(bad, r[i].x);
-        note(bad, r[i].y);
-        note(bad, r[i].z);
-        note(bad, r[i].w);
+        if (CHECK) {
+          note(most, r[i].x);
+          note(most, r[i].y);
+          note(most, r[i].z);
+          note(most, r[i].w);
+        }
         *reinterpret_cast<uint4*>(to) = r[i];
       } else {
         const float v[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z),
                             __uint_as_float(r[i].w)};
         uint2 p[NX];
         pieces4<NX>(v, p);
-        note(bad, p[0].x);
-        note(bad, p[0].y);
+        if (CHECK) {
+          note(most, p[0].x);
+          note(most, p[0].y);
+        }
 #pragma unroll
         for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(to + k * PLANE) = p[k];
       }
     }
-    return (bad & 0xffffu) >= 0x7f80u || bad >= 0x7f800000u;
+    return (most & 0xffffu) >= 0x7f80u || most >= 0x7f800000u;
   }
 
   // After a store() found one: such values of the tile become zeros, and the
-  // first token that held one goes to first[column] (COLS) or first[0].
-  template <bool COLS>
-  static __device__ __forceinline__ void mend(uint16_t* X, int* first, int tid) {
+  // first token that held one goes to first[column] and, unless null, *any.
+  static __device__ __forceinline__ void mend(uint16_t* X, int* first, int* any, int tid) {
 #pragma unroll 1
     for (int e = tid; e < Q * W; e += THR) {
       const int row = e / W, c = e % W;
@@ -217,7 +223,8 @@ struct Tile {
       if ((*x & 0x7f80u) != 0x7f80u) continue;
 #pragma unroll
       for (int k = 0; k < NX; ++k) x[k * PLANE] = 0;
-      atomicMin(first + (COLS ? c : 0), row);
+      atomicMin(first + c, row);
+      if (any) atomicMin(any, row);
     }
   }
 };

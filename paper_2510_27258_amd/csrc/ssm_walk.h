@@ -34,7 +34,7 @@ struct WalkPair {
 
 template <int PP>
 struct Waves {
-  static constexpr int NW = PP / 16 < 4 ? PP / 16 : 4, THR = 64 * NW, CB = PP / 16 / NW;
+  static constexpr int NW = PP / 16, THR = 64 * NW, CB = PP / 16 / NW;
 };
 
 template <typename T, int PP, int NN, int MODE>
@@ -44,8 +44,7 @@ struct WalkLds {
   uint16_t k[NX * Q * LDK], x[NX * Q * LDX];
   uint16_t q[MODE == kOutputs ? NX * Q * LDK : 8], s[MODE == kOutputs ? NX * Q * LDS_ : 8];
   float Lh[Q], Ll[Q], dt[Q], w[Q];
-  float cf[Q], end[Q / 16];     // dt_s 2^(L of its 16 tokens' last - L_s), and those L
-  int first[PP], first_all, bad[2];
+  int firstx[PP], firstk[NN], first_all, bad[2];
 };
 
 // ends[s] += decay ends[s - 1], s = 1 .. segs - 2: the state after each segment.
@@ -80,7 +79,7 @@ __global__ __launch_bounds__(256) void k_ssm_carry(WalkPair pair, int V) {
 // (one piece of the state and of the scores for bf16 outputs, 2^-8 of each
 // term, as large as the output's own rounding; three for fp32) is NX.
 template <typename T, int PP, int NN, int MODE, int NU>
-__global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_walk(WalkPair pair) {
+__global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2) : 1) void k_ssm_walk(WalkPair pair) {
   const WalkArgs& a = pair.a[blockIdx.y];
   const bool REV = a.rev;
   using W = Waves<PP>;
@@ -203,43 +202,46 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
     }
   }
 
-  for (int c = tid; c < PP; c += THR) S.first[c] = Q;
-  if (tid == 0) {
-    S.first_all = Q;
-    S.bad[0] = S.bad[1] = 0;
+  auto forget = [&]() {
+    for (int c = tid; c < PP; c += THR) S.firstx[c] = Q;
+    for (int c = tid; c < NN; c += THR) S.firstk[c] = Q;
+    if (tid == 0) S.first_all = Q;
+  };
+  if (MODE == kOutputs) {
+    forget();
+    if (tid == 0) S.bad[0] = S.bad[1] = 0;
+    __syncthreads();
   }
-  __syncthreads();
 
   const float Dh = MODE == kOutputs && a.D ? a.D[head] : 0.f;
   float segL = 0.f;
   for (int i = i0; i < i1; ++i) {
     const int tile = REV ? M - 1 - i : i, t0 = tile * Q, par = i & 1;
     const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
-    bool bad = tk.store(S.k, tid);
-    bad |= tx.store(S.x, tid);
-    if (MODE == kOutputs) tq.store(S.q, tid);
+    bool bad = tk.template store<MODE == kOutputs>(S.k, tid);
+    bad |= tx.template store<MODE == kOutputs>(S.x, tid);
+    if (MODE == kOutputs) tq.template store<false>(S.q, tid);
     if (tid < Q) {
       S.Lh[tid] = st.Lh;
       S.Ll[tid] = st.Ll;
       S.dt[tid] = st.dt;
       S.w[tid] = REV ? exp2_(st.Lh + st.Ll) : st.w;
-      if (MODE == kOutputs) {
-        const float eh = __shfl(st.Lh, tid | 15), el = __shfl(st.Ll, tid | 15);
-        S.cf[tid] = st.dt * exp2_((eh - st.Lh) + (el - st.Ll));
-        if ((tid & 15) == 15) S.end[tid / 16] = eh + el;
-      }
     }
-    if (bad) S.bad[par] = 1;
+    if (MODE == kOutputs && bad) S.bad[par] = 1;
     lds_barrier();
-    const bool flagged = __builtin_amdgcn_readfirstlane(S.bad[par]) != 0;
-    if (tid == 0) S.bad[par ^ 1] = 0;
-    if (flagged) {
-      // an infinite or NaN input must not reach the tile's earlier tokens
-      // through a zero weight: it is taken out here and its column (k: every
-      // column) set to NaN from its token on
-      Tile<T, NN, THR>::template mend<false>(S.k, &S.first_all, tid);
-      Tile<T, PP, THR>::template mend<true>(S.x, S.first, tid);
-      lds_barrier();
+    // An infinite or NaN input spoils the state by itself, its column (x) or
+    // its row (k).  The outputs of the tile's earlier tokens it must not reach
+    // through a zero weight: it is taken out of the tile, and the outputs and
+    // the state that depend on it are set to NaN.
+    bool flagged = false;
+    if (MODE == kOutputs) {
+      flagged = __builtin_amdgcn_readfirstlane(S.bad[par]) != 0;
+      if (tid == 0) S.bad[par ^ 1] = 0;
+      if (flagged) {
+        Tile<T, NN, THR>::mend(S.k, S.firstk, &S.first_all, tid);
+        Tile<T, PP, THR>::mend(S.x, S.firstx, nullptr, tid);
+        lds_barrier();
+      }
     }
     if (i + 1 < i1) fetch(i + 1);
 
@@ -248,74 +250,56 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
 
     bf16x8 xf[KS][CB][NX];
     if (MODE == kOutputs) {
-      // scores, transposed (rows s, columns t), weighted and stored as s[t][s].
-      // Below the diagonal blocks M_ts dt_s = 2^(L_t - L_end) (dt_s 2^(L_end - L_s))
-      // with L_end at s's block's last token: both factors at most 1, one
-      // exponential a block and lane.  Blocks above it are zeros, as far as
-      // the products over 32 tokens read them.
-      auto block = [&](int tb, int sb, const bf16x8 (&cf)[KN][NX]) {
-        const int t = 16 * tb + r, s0 = 16 * sb + 4 * g;
-        uint2 p[NX];
-#pragma unroll
-        for (int k = 0; k < NX; ++k) p[k] = make_uint2(0, 0);
-        if (sb <= tb) {
-          f32x4 acc = zero4();
-#pragma unroll
-          for (int k = 0; k < KN; ++k) {
-            bf16x8 bf[NX];
-            load_frags<NX>(S.k, PK, LDK, 16 * sb, 32 * k, l, bf);
-            mma_pieces<NX, NX>(bf, cf[k], acc);
-          }
-          float v[4];
-          if (sb < tb) {
-            const f32x4 c = *reinterpret_cast<const f32x4*>(S.cf + s0);
-            const float rf = exp2_(S.Lh[t] + S.Ll[t] - S.end[sb]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = acc[e] * (c[e] * rf);
-          } else {
-            const f32x4 lh = *reinterpret_cast<const f32x4*>(S.Lh + s0), ll = *reinterpret_cast<const f32x4*>(S.Ll + s0);
-            const f32x4 dd = *reinterpret_cast<const f32x4*>(S.dt + s0);
-            const float Lt = S.Lh[t], Ltl = S.Ll[t];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] = s0 + e <= t ? acc[e] * (exp2_((Lt - lh[e]) + (Ltl - ll[e])) * dd[e]) : 0.f;
-          }
-          pieces4<NX>(v, p);
-        }
-#pragma unroll
-        for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(S.s + k * PS + t * LDQ + s0) = p[k];
-      };
+      // scores, transposed (rows s, columns t), weighted and stored as s[t][s];
+      // blocks above the diagonal ones as far as the products over 32 tokens
+      // read them (all of their weights are zeros).  No branches: a wave's
+      // loads and products of all its blocks are in flight together.
       auto rows_of = [&](int tb, bf16x8 (&cf)[KN][NX]) {
 #pragma unroll
         for (int k = 0; k < KN; ++k) load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
       };
-      bf16x8 cfr[KN][NX];
-      if constexpr (TB == 4 && NW == 4) {
-        // ten blocks and two of zeros over four waves: three each at most
-        if (w < 2) {
-          rows_of(3, cfr);
-          block(3, 2 * w, cfr);
-          block(3, 2 * w + 1, cfr);
-          rows_of(w, cfr);
-          block(w, 0, cfr);
-          if (w == 0) block(0, 1, cfr);
-        } else {
-          rows_of(2, cfr);
-          block(2, w == 2 ? 0 : 2, cfr);
-          block(2, w == 2 ? 1 : 3, cfr);
-          if (w == 2) {
-            rows_of(1, cfr);
-            block(1, 1, cfr);
-          }
+      auto product = [&](int sb, const bf16x8 (&cf)[KN][NX]) {
+        f32x4 acc = zero4();
+#pragma unroll
+        for (int k = 0; k < KN; ++k) {
+          bf16x8 bf[NX];
+          load_frags<NX>(S.k, PK, LDK, 16 * sb, 32 * k, l, bf);
+          mma_pieces<NX, NX>(bf, cf[k], acc);
         }
+        return acc;
+      };
+      auto weigh = [&](int tb, int sb, const f32x4& acc) {
+        const int t = 16 * tb + r, s0 = 16 * sb + 4 * g;
+        const f32x4 lh = *reinterpret_cast<const f32x4*>(S.Lh + s0), dd = *reinterpret_cast<const f32x4*>(S.dt + s0);
+        f32x4 d = S.Lh[t] - lh;
+        if (NX == 3) d += S.Ll[t] - *reinterpret_cast<const f32x4*>(S.Ll + s0);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = s0 + e <= t ? acc[e] * (exp2_(d[e]) * dd[e]) : 0.f;
+        uint2 p[NX];
+        pieces4<NX>(v, p);
+#pragma unroll
+        for (int k = 0; k < NX; ++k) *reinterpret_cast<uint2*>(S.s + k * PS + t * LDQ + s0) = p[k];
+      };
+      if constexpr (TB == 4 && NW == 4) {
+        // twelve blocks over four waves: (3; 0 1) (0; 0), (3; 2 3) (1; 0), (2; 0 1) (1; 1), (2; 2 3) (0; 1)
+        const int ta = w < 2 ? 3 : 2, sa = 2 * (w & 1), tb = w == 1 || w == 2 ? 1 : 0, sb = w >> 1;
+        bf16x8 ca[KN][NX], cb[KN][NX];
+        rows_of(ta, ca);
+        rows_of(tb, cb);
+        const f32x4 x0 = product(sa, ca), x1 = product(sa + 1, ca), x2 = product(sb, cb);
+        weigh(ta, sa, x0);
+        weigh(ta, sa + 1, x1);
+        weigh(tb, sb, x2);
       } else {
         constexpr int WPT = NW > TB ? NW / TB : 1;
+        bf16x8 cf[KN][NX];
 #pragma unroll
         for (int u0 = 0; u0 < TB * WPT; u0 += NW) {
           const int u = u0 + w, tb = u / WPT;
           if (u < TB * WPT) {
-            rows_of(tb, cfr);
-            for (int sb = u % WPT; sb <= (tb | 1); sb += WPT) block(tb, sb, cfr);
+            rows_of(tb, cf);
+            for (int sb = u % WPT; sb <= (tb | 1); sb += WPT) weigh(tb, sb, product(sb, cf));
           }
         }
       }
@@ -366,25 +350,31 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
           const int c = pw + 16 * cb + 4 * g;
-          float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = NX - 1; k >= 0; --k) {
             const uint2 u = *reinterpret_cast<const uint2*>(S.x + k * PX + t * LDX + c);
-            v[0] += __uint_as_float(u.x << 16);
-            v[1] += __uint_as_float(u.x & 0xffff0000u);
-            v[2] += __uint_as_float(u.y << 16);
-            v[3] += __uint_as_float(u.y & 0xffff0000u);
+            y[tb][cb][0] += Dh * __uint_as_float(u.x << 16);
+            y[tb][cb][1] += Dh * __uint_as_float(u.x & 0xffff0000u);
+            y[tb][cb][2] += Dh * __uint_as_float(u.y << 16);
+            y[tb][cb][3] += Dh * __uint_as_float(u.y & 0xffff0000u);
           }
+        }
+      }
+      if (flagged) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = y[tb][cb][e] + Dh * v[e];
-          }
-          if (flagged) {
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (t >= min(S.first[c + e], S.first_all)) v[e] = nan_();
-          }
-          const uint32_t off = c < a.P ? yoff + (uint32_t)(tb * ystep) + 16 * cb * sizeof(T) : 0x80000000u;
+              if (16 * tb + r >= min(S.firstx[pw + 16 * cb + 4 * g + e], S.first_all)) y[tb][cb][e] = nan_();
+      }
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const float v[4] = {y[tb][cb][0], y[tb][cb][1], y[tb][cb][2], y[tb][cb][3]};
+          const uint32_t off = pw + 16 * cb + 4 * g < a.P ? yoff + (uint32_t)(tb * ystep) + 16 * cb * sizeof(T) : 0x80000000u;
           if constexpr (NX == 1) {
             uint2 p[1];
             pieces4<1>(v, p);
@@ -393,7 +383,6 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
             store16(yr, off, v);
           }
         }
-      }
     } else {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
@@ -423,14 +412,14 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? 2 : 1) void k_ssm_
     }
     if (flagged) {
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-        if (min(S.first[pw + 16 * cb + r], S.first_all) < Q) {
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) h[nb][cb] = f32x4{nan_(), nan_(), nan_(), nan_()};
-        }
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (min(S.firstx[pw + 16 * cb + r], S.firstk[16 * nb + 4 * g + e]) < Q) h[nb][cb][e] = nan_();
       lds_barrier();
-      for (int c = tid; c < PP; c += THR) S.first[c] = Q;
-      if (tid == 0) S.first_all = Q;
+      forget();
     }
     lds_barrier();
   }
