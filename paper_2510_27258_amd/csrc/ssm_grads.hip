@@ -27,11 +27,11 @@ namespace hla {
 namespace {
 
 constexpr int kGQ = 64;   // Kind<bf16>::Q
+constexpr int kGW = 8, kGThreads = 64 * kGW;   // waves
 
 struct GradArgs {
   Rows x, dy, k, q;
   const Step* tab;
-  const float* tot;
   const float *h0, *g1;       // [B H][tiles][N][P]
   const float *A, *D;
   void *dx, *ddt;
@@ -50,7 +50,7 @@ struct GradLds {
   };
   uint16_t x[kGQ * LDX], dy[kGQ * LDX], p[kGQ * LDP];
   float Lh[kGQ], Ll[kGQ], dt[kGQ], el[kGQ], wq[kGQ];
-  float R[kGQ], own[kGQ], K[4][kGQ], E[4][kGQ], F[4][kGQ], one[4][2];
+  float R[kGW][kGQ], own[kGQ], K[kGW][kGQ], E[kGW][kGQ], F[kGW][kGQ], one[kGW][2];
 };
 
 __device__ __forceinline__ float sum_groups(float v) {        // over the four lane groups of 16
@@ -69,16 +69,31 @@ __device__ __forceinline__ void unpack4(const uint2& u, float (&v)[4]) {
   v[3] = __uint_as_float(u.y & 0xffff0000u);
 }
 
+// sum over the 16 lanes of a row, in every one of them
+__device__ __forceinline__ float sum_row(float v) {
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xf, 0xf, false));   // row_ror:8
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x124, 0xf, 0xf, false));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x122, 0xf, 0xf, false));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x121, 0xf, 0xf, false));
+  return v;
+}
+
+// Eight waves.  Scores: wave w takes the 16 tokens t of block w / 2 and the
+// blocks s of w's parity.  h and g: NN / 16 blocks of 16 rows n, the four
+// token blocks dealt to the waves that share one.  dx: PP / 16 blocks of
+// columns, the token blocks dealt likewise.
 template <int PP, int NN>
-__global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
+__global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   using L_ = GradLds<PP, NN>;
   constexpr int LDK = L_::LDK, LDX = L_::LDX, LDP = L_::LDP, KN = NN / 32, KP = PP / 32, TB = 4;
-  constexpr int NBT = NN / 16, NBW = NBT >= 4 ? NBT / 4 : 1, PBT = PP / 16, PBW = PBT >= 4 ? PBT / 4 : 1;
+  constexpr int NBT = NN / 16, NT = TB * NBT / kGW;          // token blocks a wave takes of its n block
+  constexpr int PBT = PP / 16, PT = TB * PBT / kGW;          // and of its p block
+  static_assert(NT >= 1 && PT >= 1, "every wave has a block");
   extern __shared__ __align__(16) char smem[];
   L_& S = *reinterpret_cast<L_*>(smem);
   const int tid = threadIdx.x, l = tid & 63, r = l & 15, g = l >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool has_n = w * NBW < NBT, has_p = w * PBW < PBT;
+  const int n0 = 16 * (w % NBT), nt0 = NT * (w / NBT), p0 = 16 * (w % PBT), pt0 = PT * (w / PBT);
 
   int lin = blockIdx.x;
   const int hs = lin % a.hs; lin /= a.hs;
@@ -93,8 +108,8 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   const uint16_t* xp = static_cast<const uint16_t*>(a.x.p) + b * a.x.bs + t0 * a.x.ts;
   const uint16_t* yp = static_cast<const uint16_t*>(a.dy.p) + b * a.dy.bs + t0 * a.dy.ts;
 
-  using TN = Tile<bf16, NN, 256>;
-  using TP = Tile<bf16, PP, 256>;
+  using TN = Tile<bf16, NN, kGThreads>;
+  using TP = Tile<bf16, PP, kGThreads>;
   TN tn;
   TP tx, ty;
   const uint32_t x1 = TP::first(a.x.ts, a.P, tid), xby = TP::step(a.x.ts);
@@ -103,236 +118,248 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   auto fetch = [&](int head) {
     tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, a.x.ts, a.P, x1, xby);
     ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, a.dy.ts, a.P, y1, yby);
-    if (tid < kGQ) st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + tid];
+    st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + (tid & (kGQ - 1))];
   };
   tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, TN::first(a.k.ts, a.N, tid), TN::step(a.k.ts));
   tn.template store<false>(S.k, tid);
   tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.template store<false>(S.q, tid);
-  if (heads > 0) fetch(head0);
+  fetch(head0);
   lds_barrier();
 
-  // (C B^T)^T of the wave's 16 tokens t, rows s; and B and C where dB and dC will be
-  f32x4 s_[TB], z[TB];
+  // (C B^T)^T of the wave's tokens t, its two blocks of rows s; and B and C where dB and dC will be
+  const int ts = w / 2, s1 = w & 1;
+  f32x4 s_[2], z[2];
   {
     bf16x8 cf[KN];
 #pragma unroll
-    for (int k = 0; k < KN; ++k) cf[k] = frag(S.q, LDK, 16 * w, 32 * k, l);
+    for (int k = 0; k < KN; ++k) cf[k] = frag(S.q, LDK, 16 * ts, 32 * k, l);
 #pragma unroll
-    for (int sb = 0; sb < TB; ++sb) {
-      s_[sb] = z[sb] = zero4();
-      if (sb <= w) {
+    for (int i = 0; i < 2; ++i) {
+      s_[i] = z[i] = zero4();
 #pragma unroll
-        for (int k = 0; k < KN; ++k) s_[sb] = mma(frag(S.k, LDK, 16 * sb, 32 * k, l), cf[k], s_[sb]);
-      }
+      for (int k = 0; k < KN; ++k) s_[i] = mma(frag(S.k, LDK, 16 * (s1 + 2 * i), 32 * k, l), cf[k], s_[i]);
     }
   }
-  f32x4 dk[NBW][TB], dq[NBW][TB];
-  uint2 kn[NBW][TB], qn[NBW][TB];
+  f32x4 dk[NT], dq[NT];
+  uint2 kn[NT], qn[NT];
 #pragma unroll
-  for (int j = 0; j < NBW; ++j)
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
-      dk[j][tb] = dq[j][tb] = zero4();
-      const int at = (16 * tb + r) * LDK + (has_n ? 16 * (w * NBW + j) + 4 * g : 0);
-      kn[j][tb] = *reinterpret_cast<const uint2*>(S.k + at);
-      qn[j][tb] = *reinterpret_cast<const uint2*>(S.q + at);
-    }
+  for (int j = 0; j < NT; ++j) {
+    dk[j] = dq[j] = zero4();
+    const int at = (16 * (nt0 + j) + r) * LDK + n0 + 4 * g;
+    kn[j] = *reinterpret_cast<const uint2*>(S.k + at);
+    qn[j] = *reinterpret_cast<const uint2*>(S.q + at);
+  }
   lds_barrier();
 
+#pragma unroll 1
   for (int hh = 0; hh < heads; ++hh) {
     const int head = head0 + hh, bh = b * a.H + head;
-    const float Lend = a.tot[(size_t)bh * a.tiles + tile];
+    const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
     tx.template store<false>(S.x, tid);
     ty.template store<false>(S.dy, tid);
-    if (tid < kGQ) {
-      S.Lh[tid] = st.Lh;
-      S.Ll[tid] = st.Ll;
-      S.dt[tid] = st.dt;
-      S.el[tid] = exp2_(st.Lh + st.Ll);
-      S.wq[tid] = exp2_(Lend - st.Lh - st.Ll);
+    {
+      const float eh = __shfl(st.Lh, kGQ - 1), el = __shfl(st.Ll, kGQ - 1);
+      if (tid < kGQ) {
+        S.Lh[tid] = st.Lh;
+        S.Ll[tid] = st.Ll;
+        S.dt[tid] = st.dt;
+        S.el[tid] = exp2_(st.Lh + st.Ll);
+        S.wq[tid] = exp2_((eh - st.Lh) + (el - st.Ll));
+      }
+    }
+    // h and g of the wave's rows n, on their way while the scores are made
+    f32x4 hv[KP][2], gv[KP][2];
+    {
+      const size_t rec = ((size_t)bh * a.tiles + tile) * a.N * a.P;
+      const rsrc_t hr = rows_rsrc(a.h0 + rec, (long long)a.N * a.P * 4), gr = rows_rsrc(a.g1 + rec, (long long)a.N * a.P * 4);
+#pragma unroll
+      for (int k = 0; k < KP; ++k) {
+        const int c = 32 * k + 8 * g;
+        const uint32_t off = c < a.P ? (uint32_t)((n0 + r) * a.P + c) * 4 : 0x80000000u;   // rows past N lie past the end
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          hv[k][i] = __builtin_bit_cast(f32x4, load16(hr, off + 16 * i));
+          gv[k][i] = __builtin_bit_cast(f32x4, load16(gr, off + 16 * i));
+        }
+      }
     }
     lds_barrier();
-    if (hh + 1 < heads) fetch(head + 1);
 
     // (dy x^T)^T, the weighted scores for dx, and their sums
     {
-      const int t = 16 * w + r;
+      const int t = 16 * ts + r;
       const float Lt = S.Lh[t], Ltl = S.Ll[t];
       bf16x8 yf[KP];
 #pragma unroll
-      for (int k = 0; k < KP; ++k) yf[k] = frag(S.dy, LDX, 16 * w, 32 * k, l);
+      for (int k = 0; k < KP; ++k) yf[k] = frag(S.dy, LDX, 16 * ts, 32 * k, l);
       float rsum = 0.f, diag = 0.f;
 #pragma unroll
-      for (int sb = 0; sb < TB; ++sb) {
-        float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
-        const int s0 = 16 * sb + 4 * g;
-        if (sb <= w) {
-          f32x4 v = zero4();
+      for (int i = 0; i < 2; ++i) {
+        const int s0 = 16 * (s1 + 2 * i) + 4 * g;
+        f32x4 v = zero4();
 #pragma unroll
-          for (int k = 0; k < KP; ++k) v = mma(frag(S.x, LDX, 16 * sb, 32 * k, l), yf[k], v);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool in = s0 + e <= t;
-            const float m = in ? exp2_((Lt - S.Lh[s0 + e]) + (Ltl - S.Ll[s0 + e])) : 0.f, dts = S.dt[s0 + e];
-            p[e] = in ? m * s_[sb][e] : 0.f;
-            // q's diagonal has no part in da: left out of the sums that would cancel it
-            q[e] = s0 + e < t ? p[e] * v[e] : 0.f;
-            z[sb][e] += in ? m * v[e] * dts : 0.f;
-            rsum += q[e] * dts;
-            if (s0 + e == t) {
-              diag = v[e];
-              S.own[t] = p[e] * v[e];
-            }
-          }
-        }
-        if (sb <= (w | 1)) {
-          uint2 o[1];
-          pieces4<1>(p, o);
-          *reinterpret_cast<uint2*>(S.p + t * LDP + s0) = o[0];
-        }
+        for (int k = 0; k < KP; ++k) v = mma(frag(S.x, LDX, 16 * (s1 + 2 * i), 32 * k, l), yf[k], v);
+        const f32x4 lh = *reinterpret_cast<const f32x4*>(S.Lh + s0), ll = *reinterpret_cast<const f32x4*>(S.Ll + s0);
+        const f32x4 dd = *reinterpret_cast<const f32x4*>(S.dt + s0);
+        float p[4], q[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (sb <= w) {
-#pragma unroll
-            for (int m = 1; m < 16; m *= 2) q[e] += __shfl_xor(q[e], m);
+          const bool in = s0 + e <= t;
+          const float m = exp2_((Lt - lh[e]) + (Ltl - ll[e]));
+          p[e] = in ? m * s_[i][e] : 0.f;
+          // q's diagonal has no part in da: left out of the sums that would cancel it
+          q[e] = s0 + e < t ? p[e] * v[e] : 0.f;
+          z[i][e] += in ? m * v[e] * dd[e] : 0.f;
+          rsum += q[e] * dd[e];
+          if (s0 + e == t) {
+            diag = v[e];
+            S.own[t] = p[e] * v[e];
           }
-          if (r == 0) S.K[w][s0 + e] = q[e];
+        }
+        uint2 o[1];
+        pieces4<1>(p, o);
+        *reinterpret_cast<uint2*>(S.p + t * LDP + s0) = o[0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          q[e] = sum_row(q[e]);
+          if (r == 0) S.K[ts][s0 + e] = q[e];
         }
       }
       rsum = sum_groups(rsum);
-      if (g == 0) S.R[t] = rsum;
+      if (g == 0) S.R[s1][t] = rsum;
       diag = sum_wave(diag);
       if (l == 0) S.one[w][0] = diag;
     }
 
-    // h dy_t and g x_s for the wave's rows n
-    float zz = 0.f, E[TB] = {0.f, 0.f, 0.f, 0.f}, F[TB] = {0.f, 0.f, 0.f, 0.f};
-    if (has_n) {
-      const size_t rec = ((size_t)bh * a.tiles + tile) * a.N * a.P;
+    // h dy_t and g x_s for the wave's rows n and token blocks
+    float zz = 0.f;
+    {
 #pragma unroll
-      for (int j = 0; j < NBW; ++j) {
-        const int n = 16 * (w * NBW + j) + r;
-        float hv[KP][8], gv[KP][8];
+      for (int k = 0; k < KP; ++k)
 #pragma unroll
-        for (int k = 0; k < KP; ++k) {
-          const int c = 32 * k + 8 * g;
-          const bool in = n < a.N && c < a.P;
-          const float4* hp = reinterpret_cast<const float4*>(a.h0 + rec + (size_t)n * a.P + c);
-          const float4* gp = reinterpret_cast<const float4*>(a.g1 + rec + (size_t)n * a.P + c);
-          const float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          const float4 h_0 = in ? hp[0] : o, h_1 = in ? hp[1] : o, g_0 = in ? gp[0] : o, g_1 = in ? gp[1] : o;
-          const float hq[8] = {h_0.x, h_0.y, h_0.z, h_0.w, h_1.x, h_1.y, h_1.z, h_1.w};
-          const float gq[8] = {g_0.x, g_0.y, g_0.z, g_0.w, g_1.x, g_1.y, g_1.z, g_1.w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            hv[k][i] = hq[i];
-            gv[k][i] = gq[i];
-            zz += hq[i] * gq[i];
-          }
-        }
-        bf16x8 hf[KP][3], gf[KP][3];
+        for (int i = 0; i < 8; ++i) zz += hv[k][i / 4][i % 4] * gv[k][i / 4][i % 4];
+      if (nt0 != 0) zz = 0.f;
+      // one after the other, held apart: both operands' pieces at once do not fit the registers
+      auto pieces = [&](const f32x4 (&v)[KP][2], bf16x8 (&f)[KP][3]) {
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
-          pieces8<3>(hv[k], hf[k]);
-          pieces8<3>(gv[k], gf[k]);
-          *reinterpret_cast<uint4*>(S.g + n * LDX + 32 * k + 8 * g) = __builtin_bit_cast(uint4, gf[k][0]);
+          float q[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) q[i] = v[k][i / 4][i % 4];
+          pieces8<3>(q, f[k]);
         }
+      };
+      auto times = [&](const bf16x8 (&f)[KP][3], const uint16_t* X, int j) {
+        f32x4 c = zero4();
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb) {
-          f32x4 c0 = zero4(), b0 = zero4();
+        for (int k = 0; k < KP; ++k) {
+          const bf16x8 xf = frag(X, LDX, 16 * (nt0 + j), 32 * k, l);
 #pragma unroll
-          for (int k = 0; k < KP; ++k) {
-            const bf16x8 yf = frag(S.dy, LDX, 16 * tb, 32 * k, l), xf = frag(S.x, LDX, 16 * tb, 32 * k, l);
-            c0 = mma(hf[k][2], yf, c0);
-            b0 = mma(gf[k][2], xf, b0);
-            c0 = mma(hf[k][1], yf, c0);
-            b0 = mma(gf[k][1], xf, b0);
-            c0 = mma(hf[k][0], yf, c0);
-            b0 = mma(gf[k][0], xf, b0);
-          }
-          const int t = 16 * tb + r;
-          const float el = S.el[t], wq = S.wq[t], wd = wq * S.dt[t];
-          float kv[4], qv[4];
-          unpack4(kn[j][tb], kv);
-          unpack4(qn[j][tb], qv);
-          float e_ = 0.f, f_ = 0.f;
+          for (int i = 2; i >= 0; --i) c = mma(f[k][i], xf, c);
+        }
+        return c;
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      {
+        bf16x8 hf[KP][3];
+        pieces(hv, hf);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            e_ += qv[i] * c0[i];
-            f_ += kv[i] * b0[i];
-            dq[j][tb][i] += el * c0[i];
-            dk[j][tb][i] += wd * b0[i];
-          }
-          E[tb] += el * e_;
-          F[tb] += wq * f_;
+        for (int j = 0; j < NT; ++j) {
+          const int t = 16 * (nt0 + j) + r;
+          const f32x4 c0 = times(hf, S.dy, j);
+          const float el = S.el[t];
+          float qv[4], e_ = 0.f;
+          unpack4(qn[j], qv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e_ += qv[i] * c0[i];
+          dq[j] += el * c0;
+          e_ = sum_groups(el * e_);
+          if (g == 0) S.E[w % NBT][t] = e_;
         }
       }
-    }
+      __builtin_amdgcn_sched_barrier(0);
+      {
+        bf16x8 gf[KP][3];
+        pieces(gv, gf);
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
-      const float e_ = sum_groups(E[tb]), f_ = sum_groups(F[tb]);
-      if (g == 0) {
-        S.E[w][16 * tb + r] = e_;
-        S.F[w][16 * tb + r] = f_;
+        for (int k = 0; k < KP; ++k)
+          if (nt0 == 0) *reinterpret_cast<uint4*>(S.g + (n0 + r) * LDX + 32 * k + 8 * g) = __builtin_bit_cast(uint4, gf[k][0]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const int t = 16 * (nt0 + j) + r;
+          const f32x4 b0 = times(gf, S.x, j);
+          const float wq = S.wq[t], wd = wq * S.dt[t];
+          float kv[4], f_ = 0.f;
+          unpack4(kn[j], kv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f_ += kv[i] * b0[i];
+          dk[j] += wd * b0;
+          f_ = sum_groups(wq * f_);
+          if (g == 0) S.F[w % NBT][t] = f_;
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     zz = sum_wave(zz);
     if (l == 0) S.one[w][1] = zz;
+    if (hh + 1 < heads) fetch(head + 1);
     lds_barrier();
 
-    // dx^T for the wave's columns p
-    if (has_p) {
+    // dx^T for the wave's columns p and token blocks
+    {
+      const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
       const float Dh = a.D ? a.D[head] : 0.f;
+      f32x4 acc[PT];
 #pragma unroll
-      for (int j = 0; j < PBW; ++j) {
-        const int p0 = 16 * (w * PBW + j);
-        f32x4 acc[TB];
+      for (int j = 0; j < PT; ++j) acc[j] = zero4();
 #pragma unroll
-        for (int sb = 0; sb < TB; ++sb) acc[sb] = zero4();
+      for (int k = 0; k < KN; ++k) {
+        const bf16x8 gt = frag_tr(S.g, LDX, p0, 32 * k, l);
 #pragma unroll
-        for (int k = 0; k < KN; ++k) {
-          const bf16x8 gt = frag_tr(S.g, LDX, p0, 32 * k, l);
+        for (int j = 0; j < PT; ++j) acc[j] = mma(gt, frag(S.k, LDK, 16 * (pt0 + j), 32 * k, l), acc[j]);
+      }
 #pragma unroll
-          for (int sb = 0; sb < TB; ++sb) acc[sb] = mma(gt, frag(S.k, LDK, 16 * sb, 32 * k, l), acc[sb]);
-        }
+      for (int j = 0; j < PT; ++j) acc[j] *= S.wq[16 * (pt0 + j) + r];
+      // tokens s of block sb need t from 32 (sb / 2) on
 #pragma unroll
-        for (int sb = 0; sb < TB; ++sb) acc[sb] *= S.wq[16 * sb + r];
+      for (int ks = 0; ks < 2; ++ks) {
+        const bf16x8 yt = frag_tr(S.dy, LDX, p0, 32 * ks, l);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const bf16x8 yt = frag_tr(S.dy, LDX, p0, 32 * ks, l);
+        for (int j = 0; j < PT; ++j)
+          if (pt0 + j < 2 * ks + 2) acc[j] = mma(yt, frag_tr(S.p, LDP, 16 * (pt0 + j), 32 * ks, l), acc[j]);
+      }
 #pragma unroll
-          for (int sb = 0; sb < TB; ++sb)
-            if (sb < 2 * ks + 2) acc[sb] = mma(yt, frag_tr(S.p, LDP, 16 * sb, 32 * ks, l), acc[sb]);
-        }
+      for (int j = 0; j < PT; ++j) {
+        const int s = 16 * (pt0 + j) + r, c = p0 + 4 * g;
+        float v[4];
+        unpack4(*reinterpret_cast<const uint2*>(S.dy + s * LDX + c), v);
+        const float dts = S.dt[s];
 #pragma unroll
-        for (int sb = 0; sb < TB; ++sb) {
-          const int s = 16 * sb + r, c = p0 + 4 * g;
-          float v[4];
-          unpack4(*reinterpret_cast<const uint2*>(S.dy + s * LDX + c), v);
-          const float dts = S.dt[s];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = dts * acc[sb][e] + Dh * v[e];
-          if (s < rows && c < a.P) {
-            uint2 o[1];
-            pieces4<1>(v, o);
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dx) + (((size_t)b * a.n + t0 + s) * a.H + head) * a.P + c) =
-                o[0];
-          }
+        for (int e = 0; e < 4; ++e) v[e] = dts * acc[j][e] + Dh * v[e];
+        if (s < rows && c < a.P) {
+          uint2 o[1];
+          pieces4<1>(v, o);
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dx) + (((size_t)b * a.n + t0 + s) * a.H + head) * a.P + c) = o[0];
         }
       }
     }
     // the gradients of dt and the per-head parameters: one wave, a token a lane
-    if (w == (hh & 3)) {
-      const float dt = S.dt[l], R = S.R[l];
-      float K = 0.f, Et = 0.f, Fs = 0.f;
+    if (w == (hh & (kGW - 1))) {
+      const float dt = S.dt[l], R = S.R[0][l] + S.R[1][l], Lend = S.Lh[kGQ - 1] + S.Ll[kGQ - 1];
+      float K = 0.f, Et = 0.f, Fs = 0.f, hg = 0.f, dD = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        K += S.K[i][l];
+      for (int i = 0; i < TB; ++i) K += S.K[i][l];
+#pragma unroll
+      for (int i = 0; i < NBT; ++i) {
         Et += S.E[i][l];
         Fs += S.F[i][l];
       }
-      const float hg = S.one[0][1] + S.one[1][1] + S.one[2][1] + S.one[3][1];
+#pragma unroll
+      for (int i = 0; i < kGW; ++i) {
+        dD += S.one[i][0];
+        hg += S.one[i][1];
+      }
       double suf = (double)R - (double)dt * K + Et, pre = (double)dt * Fs;
       const double own = pre;
 #pragma unroll
@@ -349,7 +376,7 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
       if (l == 0) {
         float* o = a.par + ((size_t)bh * a.tiles + tile) * 3;
         o[0] = dA;
-        o[1] = S.one[0][0] + S.one[1][0] + S.one[2][0] + S.one[3][0];
+        o[1] = dD;
         o[2] = db;
       }
     }
@@ -360,45 +387,39 @@ __global__ __launch_bounds__(256) void k_ssm_grads(GradArgs a) {
   tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.template store<false>(S.q, tid);
 #pragma unroll
-  for (int sb = 0; sb < TB; ++sb)
-    if (sb <= (w | 1)) {
-      const float v[4] = {z[sb][0], z[sb][1], z[sb][2], z[sb][3]};
-      uint2 o[1];
-      pieces4<1>(v, o);
-      *reinterpret_cast<uint2*>(S.p + (16 * w + r) * LDP + 16 * sb + 4 * g) = o[0];
-    }
+  for (int i = 0; i < 2; ++i) {
+    const float v[4] = {z[i][0], z[i][1], z[i][2], z[i][3]};
+    uint2 o[1];
+    pieces4<1>(v, o);
+    *reinterpret_cast<uint2*>(S.p + (16 * ts + r) * LDP + 16 * (s1 + 2 * i) + 4 * g) = o[0];
+  }
   lds_barrier();
-  if (!has_n) return;
 #pragma unroll
-  for (int j = 0; j < NBW; ++j) {
-    const int n0 = 16 * (w * NBW + j);
+  for (int ks = 0; ks < 2; ++ks) {
+    const bf16x8 kt = frag_tr(S.k, LDK, n0, 32 * ks, l), qt = frag_tr(S.q, LDK, n0, 32 * ks, l);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 kt = frag_tr(S.k, LDK, n0, 32 * ks, l), qt = frag_tr(S.q, LDK, n0, 32 * ks, l);
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb) {
-        if (tb >= 2 * ks) dq[j][tb] = mma(kt, frag(S.p, LDP, 16 * tb, 32 * ks, l), dq[j][tb]);
-        if (tb < 2 * ks + 2) dk[j][tb] = mma(qt, frag_tr(S.p, LDP, 16 * tb, 32 * ks, l), dk[j][tb]);
-      }
+    for (int j = 0; j < NT; ++j) {
+      const int tb = nt0 + j;
+      if (tb >= 2 * ks) dq[j] = mma(kt, frag(S.p, LDP, 16 * tb, 32 * ks, l), dq[j]);
+      if (tb < 2 * ks + 2) dk[j] = mma(qt, frag_tr(S.p, LDP, 16 * tb, 32 * ks, l), dk[j]);
     }
+  }
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
-      const int t = 16 * tb + r, n = n0 + 4 * g;
-      if (t >= rows || n >= a.N) continue;
-      const size_t at = (((size_t)b * a.n + t0 + t) * a.G + grp) * a.N + n;
-      const float vk[4] = {dk[j][tb][0], dk[j][tb][1], dk[j][tb][2], dk[j][tb][3]};
-      const float vq[4] = {dq[j][tb][0], dq[j][tb][1], dq[j][tb][2], dq[j][tb][3]};
-      if (a.hs == 1) {
-        uint2 o[1];
-        pieces4<1>(vk, o);
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dk) + at) = o[0];
-        pieces4<1>(vq, o);
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dq) + at) = o[0];
-      } else {
-        const size_t all = (size_t)a.B * a.n * a.G * a.N;
-        *reinterpret_cast<float4*>(static_cast<float*>(a.dk) + hs * all + at) = make_float4(vk[0], vk[1], vk[2], vk[3]);
-        *reinterpret_cast<float4*>(static_cast<float*>(a.dq) + hs * all + at) = make_float4(vq[0], vq[1], vq[2], vq[3]);
-      }
+  for (int j = 0; j < NT; ++j) {
+    const int t = 16 * (nt0 + j) + r, n = n0 + 4 * g;
+    if (t >= rows || n >= a.N) continue;
+    const size_t at = (((size_t)b * a.n + t0 + t) * a.G + grp) * a.N + n;
+    const float vk[4] = {dk[j][0], dk[j][1], dk[j][2], dk[j][3]}, vq[4] = {dq[j][0], dq[j][1], dq[j][2], dq[j][3]};
+    if (a.hs == 1) {
+      uint2 o[1];
+      pieces4<1>(vk, o);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dk) + at) = o[0];
+      pieces4<1>(vq, o);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dq) + at) = o[0];
+    } else {
+      const size_t all = (size_t)a.B * a.n * a.G * a.N;
+      *reinterpret_cast<float4*>(static_cast<float*>(a.dk) + hs * all + at) = make_float4(vk[0], vk[1], vk[2], vk[3]);
+      *reinterpret_cast<float4*>(static_cast<float*>(a.dq) + hs * all + at) = make_float4(vq[0], vq[1], vq[2], vq[3]);
     }
   }
 }
@@ -469,7 +490,7 @@ hipError_t grads(const GradArgs& a, hipStream_t s) {
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  return HLA_TIMED("ssm_grads", (k_ssm_grads<PP, NN>), dim3((unsigned)(a.B * a.tiles * a.G * a.hs)), dim3(256), lds, s,
+  return HLA_TIMED("ssm_grads", (k_ssm_grads<PP, NN>), dim3((unsigned)(a.B * a.tiles * a.G * a.hs)), dim3(kGThreads), lds, s,
                    a);
 }
 template <int PP>
@@ -542,7 +563,7 @@ hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {
 
   GradArgs d{};
   d.x = a.x; d.dy = a.dy; d.k = a.Bm; d.q = a.Cm;
-  d.tab = c.tab; d.tot = c.tot; d.h0 = c.carry[0]; d.g1 = c.carry[1];
+  d.tab = c.tab; d.h0 = c.carry[0]; d.g1 = c.carry[1];
   d.A = a.A; d.D = a.D; d.dx = a.dx; d.ddt = a.ddt; d.par = c.par;
   d.B = a.B; d.n = a.n; d.H = a.H; d.P = a.P; d.G = a.G; d.N = a.N; d.tok = (a.n + 63) / 64 * 64;
   d.tiles = pair.a[0].plan.tiles;
