@@ -43,39 +43,59 @@ struct GradArgs {
 template <int PP, int NN>
 struct GradLds {
   static constexpr int LDK = ld_of(NN), LDX = ld_of(PP), LDP = ld_of(kGQ);
-  uint16_t k[kGQ * LDK];
-  union {
-    uint16_t q[kGQ * LDK];
-    uint16_t g[NN * LDX];
-  };
+  uint16_t k[kGQ * LDK], q[kGQ * LDK], g[NN * LDX];
   uint16_t x[kGQ * LDX], dy[kGQ * LDX], p[kGQ * LDP];
   float Lh[kGQ], Ll[kGQ], dt[kGQ], el[kGQ], wq[kGQ];
   float R[kGW][kGQ], own[kGQ], K[kGW][kGQ], E[kGW][kGQ], F[kGW][kGQ], one[kGW][2];
 };
 
-__device__ __forceinline__ float sum_groups(float v) {        // over the four lane groups of 16
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+// Sums across lanes without the LDS unit.  A swap of halves (rows 0 1 with 2 3,
+// or 0 with 1 and 2 with 3) of a value with itself leaves both halves' sum in
+// the two results' sum, in every lane.
+__device__ __forceinline__ float sum_groups(float v) {        // over the four rows of 16 lanes
+  auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  h = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
-__device__ __forceinline__ float sum_wave(float v) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
-  return v;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float v) {               // 0 where the lane has no source
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// over the 16 lanes of a row, in every one of them (rotations by 8, 4, 2, 1)
+__device__ __forceinline__ float sum_row(float v) {
+  v += dpp<0x128, 0xf>(v);
+  v += dpp<0x124, 0xf>(v);
+  v += dpp<0x122, 0xf>(v);
+  return v + dpp<0x121, 0xf>(v);
+}
+__device__ __forceinline__ float sum_wave(float v) { return sum_groups(sum_row(v)); }
+// sums over the lanes up to and with this one: shifts by 1, 2, 4, 8 in a row, then a row's last lane to the rows behind
+__device__ __forceinline__ double sums_to(double v) {
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);
+  return v + dpp<0x143, 0xc>(v);
+}
+__device__ __forceinline__ double last_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ __forceinline__ void unpack4(const uint2& u, float (&v)[4]) {
   v[0] = __uint_as_float(u.x << 16);
   v[1] = __uint_as_float(u.x & 0xffff0000u);
   v[2] = __uint_as_float(u.y << 16);
   v[3] = __uint_as_float(u.y & 0xffff0000u);
-}
-
-// sum over the 16 lanes of a row, in every one of them
-__device__ __forceinline__ float sum_row(float v) {
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xf, 0xf, false));   // row_ror:8
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x124, 0xf, 0xf, false));
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x122, 0xf, 0xf, false));
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x121, 0xf, 0xf, false));
-  return v;
 }
 
 // Eight waves.  Scores: wave w takes the 16 tokens t of block w / 2 and the
@@ -91,7 +111,7 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   static_assert(NT >= 1 && PT >= 1, "every wave has a block");
   extern __shared__ __align__(16) char smem[];
   L_& S = *reinterpret_cast<L_*>(smem);
-  const int tid = threadIdx.x, l = tid & 63, r = l & 15, g = l >> 4;
+  const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n0 = 16 * (w % NBT), nt0 = NT * (w / NBT), p0 = 16 * (w % PBT), pt0 = PT * (w / PBT);
 
@@ -124,13 +144,34 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   tn.template store<false>(S.k, tid);
   tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.template store<false>(S.q, tid);
+  // rows n0 + r of the states; each is loaded anew, for the next head, as soon
+  // as its pieces are made.  At P > 64 both do not fit the registers beside
+  // the pieces: h comes with its head, g once h is in pieces.
+  constexpr bool kAhead = PP <= 64;
+  f32x4 hv[KP][2], gv[KP][2];
+  auto rows_of = [&](const float* states, int head, f32x4 (&v)[KP][2]) {
+    const int l = opaque(threadIdx.x) & 63;
+    const rsrc_t rs = rows_rsrc(states + ((size_t)(b * a.H + head) * a.tiles + tile) * a.N * a.P, (long long)a.N * a.P * 4);
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+      const int c = 32 * k + 8 * (l >> 4);
+      const uint32_t off = c < a.P ? (uint32_t)((n0 + (l & 15)) * a.P + c) * 4 : 0x80000000u;   // rows past N lie past the end
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[k][i] = __builtin_bit_cast(f32x4, load16(rs, off + 16 * i));
+    }
+  };
   fetch(head0);
+  if (kAhead) {
+    rows_of(a.h0, head0, hv);
+    rows_of(a.g1, head0, gv);
+  }
   lds_barrier();
 
-  // (C B^T)^T of the wave's tokens t, its two blocks of rows s; and B and C where dB and dC will be
+  // (C B^T)^T of the wave's tokens t, its two blocks of rows s
   const int ts = w / 2, s1 = w & 1;
   f32x4 s_[2], z[2];
   {
+    const int l = tid & 63;
     bf16x8 cf[KN];
 #pragma unroll
     for (int k = 0; k < KN; ++k) cf[k] = frag(S.q, LDK, 16 * ts, 32 * k, l);
@@ -142,15 +183,8 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
     }
   }
   f32x4 dk[NT], dq[NT];
-  uint2 kn[NT], qn[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    dk[j] = dq[j] = zero4();
-    const int at = (16 * (nt0 + j) + r) * LDK + n0 + 4 * g;
-    kn[j] = *reinterpret_cast<const uint2*>(S.k + at);
-    qn[j] = *reinterpret_cast<const uint2*>(S.q + at);
-  }
-  lds_barrier();
+  for (int j = 0; j < NT; ++j) dk[j] = dq[j] = zero4();
 
 #pragma unroll 1
   for (int hh = 0; hh < heads; ++hh) {
@@ -168,23 +202,9 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         S.wq[tid] = exp2_((eh - st.Lh) + (el - st.Ll));
       }
     }
-    // h and g of the wave's rows n, on their way while the scores are made
-    f32x4 hv[KP][2], gv[KP][2];
-    {
-      const size_t rec = ((size_t)bh * a.tiles + tile) * a.N * a.P;
-      const rsrc_t hr = rows_rsrc(a.h0 + rec, (long long)a.N * a.P * 4), gr = rows_rsrc(a.g1 + rec, (long long)a.N * a.P * 4);
-#pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        const int c = 32 * k + 8 * g;
-        const uint32_t off = c < a.P ? (uint32_t)((n0 + r) * a.P + c) * 4 : 0x80000000u;   // rows past N lie past the end
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          hv[k][i] = __builtin_bit_cast(f32x4, load16(hr, off + 16 * i));
-          gv[k][i] = __builtin_bit_cast(f32x4, load16(gr, off + 16 * i));
-        }
-      }
-    }
+    if (!kAhead) rows_of(a.h0, head, hv);
     lds_barrier();
+    fetch(min(head + 1, head0 + heads - 1));
 
     // (dy x^T)^T, the weighted scores for dx, and their sums
     {
@@ -235,11 +255,12 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
     // h dy_t and g x_s for the wave's rows n and token blocks
     float zz = 0.f;
     {
+      if (kAhead) {
 #pragma unroll
-      for (int k = 0; k < KP; ++k)
+        for (int k = 0; k < KP; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) zz += hv[k][i / 4][i % 4] * gv[k][i / 4][i % 4];
-      if (nt0 != 0) zz = 0.f;
+          for (int i = 0; i < 8; ++i) zz += hv[k][i / 4][i % 4] * gv[k][i / 4][i % 4];
+      }
       // one after the other, held apart: both operands' pieces at once do not fit the registers
       auto pieces = [&](const f32x4 (&v)[KP][2], bf16x8 (&f)[KP][3]) {
 #pragma unroll
@@ -261,27 +282,42 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         return c;
       };
       __builtin_amdgcn_sched_barrier(0);
+      bf16x8 hf[KP][3];
+      pieces(hv, hf);
+      if (kAhead)
+        rows_of(a.h0, min(head + 1, head0 + heads - 1), hv);
+      else
+        rows_of(a.g1, head, gv);
       {
-        bf16x8 hf[KP][3];
-        pieces(hv, hf);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           const int t = 16 * (nt0 + j) + r;
           const f32x4 c0 = times(hf, S.dy, j);
           const float el = S.el[t];
           float qv[4], e_ = 0.f;
-          unpack4(qn[j], qv);
+          unpack4(*reinterpret_cast<const uint2*>(S.q + t * LDK + n0 + 4 * g), qv);
 #pragma unroll
           for (int i = 0; i < 4; ++i) e_ += qv[i] * c0[i];
           dq[j] += el * c0;
           e_ = sum_groups(el * e_);
           if (g == 0) S.E[w % NBT][t] = e_;
+          if (j & 1) __builtin_amdgcn_sched_barrier(0);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
       {
+        if (!kAhead) {
+#pragma unroll
+          for (int k = 0; k < KP; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              zz += (((float)hf[k][2][i] + (float)hf[k][1][i]) + (float)hf[k][0][i]) * gv[k][i / 4][i % 4];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (nt0 != 0) zz = 0.f;
         bf16x8 gf[KP][3];
         pieces(gv, gf);
+        if (kAhead) rows_of(a.g1, min(head + 1, head0 + heads - 1), gv);
 #pragma unroll
         for (int k = 0; k < KP; ++k)
           if (nt0 == 0) *reinterpret_cast<uint4*>(S.g + (n0 + r) * LDX + 32 * k + 8 * g) = __builtin_bit_cast(uint4, gf[k][0]);
@@ -291,19 +327,19 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
           const f32x4 b0 = times(gf, S.x, j);
           const float wq = S.wq[t], wd = wq * S.dt[t];
           float kv[4], f_ = 0.f;
-          unpack4(kn[j], kv);
+          unpack4(*reinterpret_cast<const uint2*>(S.k + t * LDK + n0 + 4 * g), kv);
 #pragma unroll
           for (int i = 0; i < 4; ++i) f_ += kv[i] * b0[i];
           dk[j] += wd * b0;
           f_ = sum_groups(wq * f_);
           if (g == 0) S.F[w % NBT][t] = f_;
+          if (j & 1) __builtin_amdgcn_sched_barrier(0);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     zz = sum_wave(zz);
     if (l == 0) S.one[w][1] = zz;
-    if (hh + 1 < heads) fetch(head + 1);
     lds_barrier();
 
     // dx^T for the wave's columns p and token blocks
@@ -360,15 +396,9 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         dD += S.one[i][0];
         hg += S.one[i][1];
       }
-      double suf = (double)R - (double)dt * K + Et, pre = (double)dt * Fs;
-      const double own = pre;
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) {
-        const double u = __shfl_down(suf, m), v = __shfl_up(pre, m);
-        if (l + m < 64) suf += u;
-        if (l >= m) pre += v;
-      }
-      const float da = (float)(suf + (pre - own) + (double)exp2_(Lend) * hg);
+      const double back = (double)R - (double)dt * K + Et, ahead = (double)dt * Fs;
+      const double upto = sums_to(back), suf = last_lane(upto) - upto + back, pre = sums_to(ahead) - ahead;
+      const float da = (float)(suf + pre + (double)exp2_(Lend) * hg);
       float d = a.A[head] * da + (K + S.own[l] + Fs);
       if (a.softplus) d *= -expm1f(-dt);
       if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, d);
@@ -384,8 +414,7 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   }
 
   // the tile's own part of dB and dC: the heads' sum z[t][s] with C and B
-  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
-  tn.template store<false>(S.q, tid);
+  const int l = opaque(threadIdx.x) & 63, r = l & 15, g = l >> 4;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float v[4] = {z[i][0], z[i][1], z[i][2], z[i][3]};
