@@ -9,7 +9,11 @@ namespace {
 
 // What a walk does: the end state of a segment from zero, the outputs, or the
 // state before every tile (after every tile, backwards).
-enum WalkMode { kEnds = 0, kOutputs = 1, kStates = 2 };
+// For the gradients' states the accumulators hold the state transposed, four
+// neighbours of a row of [N][P] a lane, so that its stores are 16 bytes wide;
+// the readout needs it as it is.
+enum WalkMode { kEnds = 0, kOutputs = 1, kStates = 2, kEndsOfStates = 3 };
+constexpr bool transposed(int mode) { return mode == kStates || mode == kEndsOfStates; }
 
 struct WalkArgs {
   Rows x, k, q;               // x [B, n, H, P]; k, q [B, n, G, N] (backwards: dy and C in x's and k's place)
@@ -74,7 +78,8 @@ __global__ __launch_bounds__(256) void k_ssm_carry(WalkPair pair, int V) {
 }
 
 // One workgroup walks one segment of one head; wave w owns 16 CB columns of
-// the state, h[n = 16 nb + 4g + i][p = 16 (w CB + cb) + r], in accumulators.
+// the state, h[n = 16 nb + 4g + i][p = 16 (w CB + cb) + r], in accumulators
+// (transposed: h[n = 16 nb + r][p = 16 (w CB + cb) + 4g + i]).
 // NU pieces carry the scaled inputs into the state; the readout's rounding
 // (one piece of the state and of the scores for bf16 outputs, 2^-8 of each
 // term, as large as the output's own rounding; three for fp32) is NX.
@@ -169,8 +174,8 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) h[nb][cb] = zero4();
-  if (MODE == kEnds) {
-    if (seg == 0 && a.state && !REV) {
+  if (MODE == kEnds || MODE == kEndsOfStates) {
+    if (MODE == kEnds && seg == 0 && a.state) {
       load_state(a.state + (size_t)bh * a.N * a.P);
       f32x4* to = slot(a.plan.segs - 1);          // the outputs' last segment overwrites a.state
 #pragma unroll
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
         for (int cb = 0; cb < CB; ++cb) to[(nb * CB + cb) * THR + tid] = h[nb][cb];
     }
   } else if (seg == 0) {
-    if (a.state && !REV) {
+    if (MODE == kOutputs && a.state) {
       if (a.plan.segs == 1) {
         load_state(a.state + (size_t)bh * a.N * a.P);
       } else {
@@ -245,8 +250,16 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     }
     if (i + 1 < i1) fetch(i + 1);
 
-    if (MODE == kStates)
-      store_state(a.carry + ((size_t)bh * M + tile) * a.N * a.P);
+    if (MODE == kStates) {
+      float* to = a.carry + ((size_t)bh * M + tile) * a.N * a.P;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const int n = 16 * nb + r, c = pw + 16 * cb + 4 * g;
+          if (n < a.N && c < a.P) *reinterpret_cast<f32x4*>(to + n * a.P + c) = h[nb][cb];
+        }
+    }
 
     bf16x8 xf[KS][CB][NX];
     if (MODE == kOutputs) {
@@ -407,7 +420,12 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
         bf16x8 bt[NX];
         load_frags_tr<NX>(S.k, PK, LDK, 16 * nb, 32 * ks, l, bt);
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NU>(bt, u[ks][cb], h[nb][cb]);
+        for (int cb = 0; cb < CB; ++cb) {
+          if constexpr (transposed(MODE))
+            mma_pieces<NU, NX>(u[ks][cb], bt, h[nb][cb]);
+          else
+            mma_pieces<NX, NU>(bt, u[ks][cb], h[nb][cb]);
+        }
       }
     }
     if (flagged) {
@@ -424,7 +442,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     lds_barrier();
   }
 
-  if (MODE == kEnds) {
+  if (MODE == kEnds || MODE == kEndsOfStates) {
     f32x4* to = slot(seg);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -445,7 +463,7 @@ hipError_t walk(const WalkPair& a, int count, int B, hipStream_t s) {
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  constexpr const char* name = MODE == kEnds ? "ssm_ends" : MODE == kOutputs ? "ssm_outputs" : "ssm_states";
+  constexpr const char* name = MODE == kEnds || MODE == kEndsOfStates ? "ssm_ends" : MODE == kOutputs ? "ssm_outputs" : "ssm_states";
   return HLA_TIMED(name, (k_ssm_walk<T, PP, NN, MODE, NU>), dim3((unsigned)(B * a.a[0].H * a.a[0].segs_run), count),
                    dim3(Waves<PP>::THR), lds, s, a);
 }
@@ -528,7 +546,7 @@ hipError_t walk_all(WalkPair& pair, int count, int B, hipStream_t s) {
   const int segs = a.plan.segs;
   if (segs > 1) {
     for (int i = 0; i < count; ++i) pair.a[i].segs_run = segs - 1;
-    hipError_t e = walk_pn<T, kEnds, NU>(pair, count, B, s);
+    hipError_t e = walk_pn<T, MODE == kStates ? kEndsOfStates : kEnds, NU>(pair, count, B, s);
     if (e != hipSuccess) return e;
     if (segs - 1 > kOwnSums) {
       const int V = padded(a.P) * padded(a.N) / 4;
