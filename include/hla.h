@@ -381,8 +381,8 @@ int ahla_forward(const void *q, const void *k, const void *v, float *out,
  * oldest first; replaced by the last K-1 inputs of [state; x].  Without it
  * they are zeros.  One call with n = 1 is a decode step.
  * K in {2, 3, 4}, any D, n <= 2^22, B <= 65535.  Pointers need the alignment
- * of their type; rows in whole 16-byte pieces (base, strides and D) are
- * faster. */
+ * of their type; four channels kept together (D and the strides multiples of
+ * four, addresses of four values' alignment) are faster. */
 int hla_conv_forward(const void *x, long long x_bs, long long x_ts, const void *weight, const void *bias,
                      void *state, void *y, int B, int n, int D, int K, int silu, int dtype, int w_dtype,
                      void *stream);

@@ -5,10 +5,12 @@
 //   dx_t = sum_j w_j dz_{t+K-1-j},  dw_j = sum_t dz_t x_{t-K+1+j},  dbias = sum_t dz_t
 //
 // 2K + a few operations an element: bound by memory.  A thread walks a run of
-// tokens of 16 bytes of channels (one channel where the width, a stride or an
-// address is no multiple of 16 bytes) with the last K - 1 inputs in
-// registers, so each input is read once, plus K - 1 rows a run; four rows'
-// loads are in flight at a time.  Sums are fp32, rounded once on the store.
+// tokens of four channels (one where the width, a stride or an address does
+// not keep four together) with the last K - 1 inputs in registers, so each
+// input is read once, plus K - 1 rows a run.  Four channels, 8 bytes of bf16,
+// rather than 16 bytes: half the registers a thread, so that twice the waves
+// hide the loads.  A chunk of rows loads while the one before it is
+// computed.  Sums are fp32, rounded once on the store.
 #include "common.h"
 #include "mixer.h"
 #include "profile.h"
@@ -22,30 +24,21 @@ constexpr int kConvBackRun = 16;   // tokens a thread of the gradients walks
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-template <int V>
-struct Fv {
-  float v[V];
-};
-
-template <typename T, int V>
-__device__ __forceinline__ Fv<V> row(const T* p, bool there) {
-  Fv<V> r;
-  if (there) {
-    load_vec<T, V>(p, r.v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) r.v[i] = 0.f;
-  }
-  return r;
-}
-
 template <int V, int K>
 __device__ __forceinline__ void taps(const Conv& a, int c, float (&w)[K][V], float (&b)[V]) {
+  float all[V * K];
+  if (a.w_dtype == 1) {
+    load_many<bf16, V, V * K>(a.w, (size_t)c * K, all);
+    if (a.bias) load_many<bf16, V, V>(a.bias, c, b);
+  } else {
+    load_many<float, V, V * K>(a.w, (size_t)c * K, all);
+    if (a.bias) load_many<float, V, V>(a.bias, c, b);
+  }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) w[j][i] = load_any(a.w, a.w_dtype, (size_t)(c + i) * K + j);
-    b[i] = a.bias ? load_any(a.bias, a.w_dtype, c + i) : 0.f;
+    for (int j = 0; j < K; ++j) w[j][i] = all[i * K + j];
+    if (!a.bias) b[i] = 0.f;
   }
 }
 
@@ -59,10 +52,15 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a, int CV, int runs,
   const int run = (int)(idx / CV), c = (int)(idx - (long long)run * CV) * V, b = blockIdx.y;
   const T* x = static_cast<const T*>(a.x.p) + b * a.x.bs + c;
   T* y = static_cast<T*>(a.y) + (size_t)b * a.n * a.D + c;
-  float w[K][V], bias[V];
-  taps<V, K>(a, c, w, bias);
   const int t0 = run * run_len, t1 = min(a.n, t0 + run_len);
-  float win[K - 1][V];
+  constexpr int U = 4;
+  Raw<T, V> next[U];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u].load(x + min(t + u, a.n - 1) * a.x.ts);   // past the run: not used
+  };
+  fetch(t0);
+  float w[K][V], bias[V], win[K - 1][V];
   if (run == 0) {
     if (a.state) {
       T* st = static_cast<T*>(a.state) + (size_t)b * (K - 1) * a.D + c;
@@ -85,47 +83,45 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a, int CV, int runs,
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) load_vec<T, V>(x + (t0 - (K - 1) + j) * a.x.ts, win[j]);
   }
-  constexpr int U = 4;
+  taps<V, K>(a, c, w, bias);
   for (int t = t0; t < t1; t += U) {
-    Fv<V> in[U];
+    Raw<T, V> in[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) in[u] = row<T, V>(x + (t + u) * a.x.ts, t + u < t1);
+    for (int u = 0; u < U; ++u) in[u] = next[u];
+    fetch(t + U);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float z[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
+        const float x_t = in[u].at(i);
         z[i] = bias[i];
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) z[i] += w[j][i] * win[j][i];
-        z[i] += w[K - 1][i] * in[u].v[i];
+        z[i] += w[K - 1][i] * x_t;
         if (a.silu) z[i] *= sigmoid(z[i]);
 #pragma unroll
         for (int j = 0; j + 1 < K - 1; ++j) win[j][i] = win[j + 1][i];
-        win[K - 2][i] = in[u].v[i];
+        win[K - 2][i] = x_t;
       }
       if (t + u < t1) store_vec<T, V>(y + (size_t)(t + u) * a.D, z);
     }
   }
 }
 
-// Gradients.  A block is CL channel pieces by RL runs; a thread walks its run
+// Gradients.  A block is kConvCL channel pieces by kConvRL runs; a thread walks its run
 // and K - 1 tokens past it with the last K inputs and the last K values of dz
 // in registers, and sums its tokens' share of dw and dbias.  The runs of a
 // block are summed in the wave and over the waves in a fixed order, a row of
 // partials [D (K + 1)] a block, and k_conv_sum adds the rows: no atomics, so
 // the same inputs give the same bits.
-template <int V>
-struct ConvBlock {
-  static constexpr int CL = V == 1 ? 64 : 16, RL = kConvThreads / CL, RW = 64 / CL;
-};
+constexpr int kConvCL = 32, kConvRL = kConvThreads / kConvCL;
 
 template <typename T, int V, int K>
-__global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part, int run_len) {
-  using Bk = ConvBlock<V>;
-  const int cl = threadIdx.x % Bk::CL, rl = threadIdx.x / Bk::CL, b = blockIdx.z;
-  const int c = (blockIdx.x * Bk::CL + cl) * V;
-  const int t0 = (blockIdx.y * Bk::RL + rl) * run_len, t1 = min(a.n, t0 + run_len);
+__global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part) {
+  const int cl = threadIdx.x % kConvCL, rl = threadIdx.x / kConvCL, b = blockIdx.z;
+  const int c = (blockIdx.x * kConvCL + cl) * V;
+  const int t0 = (blockIdx.y * kConvRL + rl) * kConvBackRun, t1 = min(a.n, t0 + kConvBackRun);
   float dw[K + 1][V];
 #pragma unroll
   for (int j = 0; j <= K; ++j)
@@ -135,28 +131,39 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part,
     const T* x = static_cast<const T*>(a.x.p) + b * a.x.bs + c;
     const T* dy = static_cast<const T*>(a.dy.p) + b * a.dy.bs + c;
     T* dx = static_cast<T*>(a.dx) + (size_t)b * a.n * a.D + c;
-    float w[K][V], bias[V];
-    taps<V, K>(a, c, w, bias);
-    float win[K][V], dz[K][V];
+    constexpr int U = 4;
+    Raw<T, V> nx[U], ng[U];
+    // rows past the sequence: no part in anything (there is tested below)
+    auto fetch = [&](int t) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        nx[u].load(x + min(t + u, a.n - 1) * a.x.ts);
+        ng[u].load(dy + min(t + u, a.n - 1) * a.dy.ts);
+      }
+    };
+    fetch(t0);
+    float w[K][V], bias[V], win[K][V], dz[K][V];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
       const int t = t0 - K + j;      // the first is shifted out at once
-      const Fv<V> r = row<T, V>(x + t * a.x.ts, j > 0 && t >= 0);
+      if (j > 0 && t >= 0) {
+        load_vec<T, V>(x + t * a.x.ts, win[j]);
+      } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        win[j][i] = r.v[i];
-        dz[j][i] = 0.f;
+        for (int i = 0; i < V; ++i) win[j][i] = 0.f;
       }
+#pragma unroll
+      for (int i = 0; i < V; ++i) dz[j][i] = 0.f;
     }
-    constexpr int U = 4;
+    taps<V, K>(a, c, w, bias);
     for (int t = t0; t < t1 + K - 1; t += U) {
-      Fv<V> in[U], g[U];
+      Raw<T, V> in[U], g[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const bool there = t + u < t1 + K - 1 && t + u < a.n;
-        in[u] = row<T, V>(x + (t + u) * a.x.ts, there);
-        g[u] = row<T, V>(dy + (t + u) * a.dy.ts, there);
+        in[u] = nx[u];
+        g[u] = ng[u];
       }
+      fetch(t + U);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const bool mine = t + u < t1;
@@ -169,8 +176,8 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part,
             win[j][i] = win[j + 1][i];
             dz[j][i] = dz[j + 1][i];
           }
-          win[K - 1][i] = in[u].v[i];
-          float d = g[u].v[i];
+          win[K - 1][i] = in[u].at(i);
+          float d = g[u].at(i);
           if (a.silu) {
             float z = bias[i];
 #pragma unroll
@@ -193,20 +200,18 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part,
       }
     }
   }
-  __shared__ float red[kConvThreads / 64][Bk::CL * V];
+  __shared__ float red[kConvThreads / 64][kConvCL * V];
   float* to = part + ((size_t)blockIdx.z * gridDim.y + blockIdx.y) * a.D * (K + 1);
 #pragma unroll
   for (int j = 0; j <= K; ++j) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float v = dw[j][i];
-#pragma unroll
-      for (int m = Bk::CL; m < 64; m *= 2) v += __shfl_xor(v, m);
-      if ((threadIdx.x & 63) < Bk::CL) red[threadIdx.x / 64][cl * V + i] = v;
+      const float v = dw[j][i] + __shfl_xor(dw[j][i], 32);
+      if ((threadIdx.x & 63) < kConvCL) red[threadIdx.x / 64][cl * V + i] = v;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < Bk::CL * V; e += kConvThreads) {
-      const int ch = blockIdx.x * Bk::CL * V + e;
+    for (int e = threadIdx.x; e < kConvCL * V; e += kConvThreads) {
+      const int ch = blockIdx.x * kConvCL * V + e;
       if (ch < a.D) to[(size_t)j * a.D + ch] = red[0][e] + red[1][e] + red[2][e] + red[3][e];
     }
     __syncthreads();
@@ -232,13 +237,16 @@ __global__ __launch_bounds__(64 * kSumRows) void k_conv_sum(Conv a, const float*
     store_any(a.dbias, a.w_dtype, c, s);
 }
 
-bool vec_ok(const Conv& c, int V) {
-  auto fits = [&](const Rows& r) {
-    return (reinterpret_cast<uintptr_t>(r.p) & 15) == 0 && r.bs % V == 0 && r.ts % V == 0;
-  };
-  return c.D % V == 0 && fits(c.x) && (!c.dy.p || fits(c.dy)) &&
-         ((reinterpret_cast<uintptr_t>(c.state) | reinterpret_cast<uintptr_t>(c.y) |
-           reinterpret_cast<uintptr_t>(c.dx)) & 15) == 0;
+// Blocks over the tokens of the gradients.
+int conv_back_blocks(int n) { return (n + kConvBackRun * kConvRL - 1) / (kConvBackRun * kConvRL); }
+
+// Whether four channels stay together: whole vectors of 4 values everywhere.
+bool vec_ok(const Conv& c) {
+  const int es = c.dtype == 1 ? 2 : 4, ws = c.w_dtype == 1 ? 2 : 4;
+  auto whole = [](const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0; };
+  auto fits = [&](const Rows& r) { return whole(r.p, es) && r.bs % 4 == 0 && r.ts % 4 == 0; };
+  return c.D % 4 == 0 && fits(c.x) && fits(c.dy) && whole(c.state, es) && whole(c.y, es) && whole(c.dx, es) &&
+         whole(c.w, ws) && whole(c.bias, ws);
 }
 
 template <typename T, int V, int K>
@@ -254,11 +262,9 @@ hipError_t forward(const Conv& c, hipStream_t s) {
 
 template <typename T, int V, int K>
 hipError_t backward(const Conv& c, float* part, hipStream_t s) {
-  using Bk = ConvBlock<V>;
-  const int len = kConvBackRun;
-  const int cb = (c.D / V + Bk::CL - 1) / Bk::CL, tb = (c.n + len * Bk::RL - 1) / (len * Bk::RL);
+  const int cb = (c.D / V + kConvCL - 1) / kConvCL, tb = conv_back_blocks(c.n);
   const hipError_t e = HLA_TIMED("conv_back", (k_conv_back<T, V, K>), dim3(cb, tb, c.B), dim3(kConvThreads), 0, s, c,
-                                 part, len);
+                                 part);
   if (e != hipSuccess) return e;
   const int cols = c.D * (K + 1);
   return HLA_TIMED("conv_sum", k_conv_sum, dim3((cols + 63) / 64), dim3(64 * kSumRows), 0, s, c, part, tb * c.B);
@@ -274,18 +280,17 @@ hipError_t by_k(const Conv& c, float* part, hipStream_t s) {
 }
 
 hipError_t by_type(const Conv& c, float* part, hipStream_t s) {
-  if (c.dtype == 1) return vec_ok(c, 8) ? by_k<bf16, 8>(c, part, s) : by_k<bf16, 1>(c, part, s);
-  return vec_ok(c, 4) ? by_k<float, 4>(c, part, s) : by_k<float, 1>(c, part, s);
+  const bool vec = vec_ok(c);
+  if (c.dtype == 1) return vec ? by_k<bf16, 4>(c, part, s) : by_k<bf16, 1>(c, part, s);
+  return vec ? by_k<float, 4>(c, part, s) : by_k<float, 1>(c, part, s);
 }
 
 }  // namespace
 
 hipError_t launch_conv_forward(const Conv& c, hipStream_t s) { return by_type(c, nullptr, s); }
 
-// the most blocks over time that any of the forms takes (the scalar form's four runs)
 size_t conv_backward_ws(int B, int n, int D, int K) {
-  const size_t tb = (n + kConvBackRun * 4 - 1) / (kConvBackRun * 4);
-  return sizeof(float) * tb * B * D * (K + 1);
+  return sizeof(float) * conv_back_blocks(n) * (size_t)B * D * (K + 1);
 }
 
 hipError_t launch_conv_backward(const Conv& c, void* ws, hipStream_t s) {

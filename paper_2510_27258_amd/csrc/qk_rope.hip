@@ -7,10 +7,14 @@
 //   dx = r (g w - xhat mean(g w xhat)),  dw = sum g xhat,  xhat = x r.
 //
 // Bound by memory: every row is read once and written once.  LP lanes hold a
-// head's row, 16 bytes each, the mean square goes over them by shuffles, and
-// the other half of a rotation pair comes from its lane.  A thread takes
-// several heads of one token, so that cos and sin are read once for them and
-// the heads' loads are in flight together; queries and keys share the launch.
+// head's row, 16 bytes each; the mean square goes over them by lane moves, and
+// the other half of a rotation pair comes, as it was loaded, from its lane.
+// A thread takes HP heads of one token and kind: cos, sin and the weight,
+// folded into one factor for the element itself and one for its pair's other
+// element, are made once for them, and the heads' loads are in flight
+// together.  A block takes 256 / LP neighbouring tokens of the same heads, so
+// that both its reads (HP rows of a token) and its writes (its tokens' rows of
+// a head) are contiguous; queries and keys share the launch.
 #include "common.h"
 #include "mixer.h"
 #include "profile.h"
@@ -21,25 +25,25 @@ namespace {
 
 constexpr int kQkThreads = 256;
 
-// Where the row of virtual head v (queries, then keys) of token (b, t) is.
-template <typename T>
-struct Head {
-  const T* x;
-  size_t out;      // row index in the [B, H, n, d] output of its kind
+// A block's share: tokens [tok0, tok0 + 256 / LP) of all B n, heads [h0, h0 + HP) of one kind.
+struct Share {
+  long long tok0;
+  int h0, heads;
   bool key;
 };
-template <typename T>
-__device__ __forceinline__ Head<T> head_at(const QkRope& a, int b, int t, int v) {
-  Head<T> h;
-  h.key = v >= a.H;
-  const Rows& r = h.key ? a.k : a.q;
-  const int i = h.key ? v - a.H : v;
-  h.x = static_cast<const T*>(r.p) + b * r.bs + t * r.ts + (size_t)i * a.d;
-  h.out = ((size_t)b * (h.key ? a.Hk : a.H) + i) * a.n + t;
-  return h;
+__device__ __forceinline__ Share share_of(const QkRope& a, long long unit, int HP, int tokens) {
+  const int gq = (a.H + HP - 1) / HP, gk = (a.Hk + HP - 1) / HP;
+  const int gr = (int)(unit % (gq + gk));
+  Share s;
+  s.tok0 = unit / (gq + gk) * tokens;
+  s.key = gr >= gq;
+  s.h0 = (s.key ? gr - gq : gr) * HP;
+  s.heads = min(HP, (s.key ? a.Hk : a.H) - s.h0);
+  return s;
 }
 
-// cos and sin of the lane's V dimensions (1 and 0 past rot).  A position
+// cos and sin of the lane's V dimensions (1 and 0 past rot), sin with the sign
+// it has for the pair's other element (- in the first half).  A position
 // outside the tables rotates by NaN: nothing is read there.
 template <int V>
 __device__ __forceinline__ void angles(const QkRope& a, int b, int t, int c, float (&cs)[V], float (&sn)[V]) {
@@ -50,236 +54,267 @@ __device__ __forceinline__ void angles(const QkRope& a, int b, int t, int c, flo
   const bool in = pos >= 0 && pos < a.positions;
   const int half = a.rot / 2;
   const size_t at = in ? (size_t)pos * half : 0;
+  if (!a.interleaved && half % V == 0) {
+    if (c < a.rot) {
+      const int p = c < half ? c : c - half;
+      load_many<float, 4, V>(a.cs, at + p, cs);
+      load_many<float, 4, V>(a.sn, at + p, sn);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float s = c < half ? -sn[i] : sn[i];
+      cs[i] = c >= a.rot ? 1.f : in ? cs[i] : __builtin_nanf("");
+      sn[i] = c >= a.rot ? 0.f : in ? s : __builtin_nanf("");
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int e = c + i;
+    cs[i] = 1.f;
+    sn[i] = 0.f;
     if (e < a.rot) {
       const int p = a.interleaved ? e / 2 : (e < half ? e : e - half);
+      const bool first = a.interleaved ? e % 2 == 0 : e < half;
       cs[i] = in ? a.cs[at + p] : __builtin_nanf("");
-      sn[i] = in ? a.sn[at + p] : __builtin_nanf("");
-    } else {
-      cs[i] = 1.f;
-      sn[i] = 0.f;
+      sn[i] = in ? (first ? -a.sn[at + p] : a.sn[at + p]) : __builtin_nanf("");
     }
   }
 }
 
-// out = u rotated by (cs, sign sn), u the lane's V dimensions from c on.  The
-// pair's other element is in the lane itself (interleaved), or `hop` lanes
-// on or back (hop > 0: rot/2 is a whole number of lanes), or, where a pair
-// straddles lanes, fetched element by element from its lane.
-template <int V>
-__device__ __forceinline__ void rotate(const QkRope& a, int c, int hop, float sign, const float (&u)[V],
-                                       const float (&cs)[V], const float (&sn)[V], float (&out)[V]) {
+// The other elements of the lane's pairs, v their own: from the lane itself
+// (interleaved), from the lane hop on or back (rot/2 a whole number of lanes),
+// or, where a pair straddles lanes, element by element.  Past rot: anything
+// finite times the 0 of angles() - the lane's own elements.
+template <typename T, int V>
+__device__ __forceinline__ void others(const QkRope& a, int c, int hop, const Raw<T, V>& v, float (&o)[V]) {
   const int half = a.rot / 2, lane = threadIdx.x & 63;
   if (a.interleaved || a.rot == 0) {
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-      const float s0 = sign * sn[i], s1 = sign * sn[i + 1];
-      out[i] = u[i] * cs[i] - u[i + 1] * s0;
-      out[i + 1] = u[i + 1] * cs[i + 1] + u[i] * s1;
-    }
+    for (int i = 0; i < V; ++i) o[i] = v.at(i ^ 1);
     return;
   }
-  const bool first = c < half;
   if (hop > 0) {
-    const int from = c >= a.rot ? lane : first ? lane + hop : lane - hop;
+    const int from = c >= a.rot ? lane : c < half ? lane + hop : lane - hop;
+    Raw<T, V> w;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float o = __shfl(u[i], from);
-      const float s = first ? -sign * sn[i] : sign * sn[i];
-      out[i] = c < a.rot ? u[i] * cs[i] + o * s : u[i];
-    }
+    for (int i = 0; i < Raw<T, V>::N; ++i) w.w[i] = __shfl((int)v.w[i], from);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = w.at(i);
     return;
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int e = c + i;
-    const int pe = e < half ? e + half : e - half;       // the pair's other element, for e < rot
-    const int from = lane + (e < a.rot ? pe / V - c / V : 0), slot = pe % V;
-    float o = 0.f;
+    const int pe = e >= a.rot ? e : e < half ? e + half : e - half;
+    const int from = lane + pe / V - c / V, slot = pe % V;
+    o[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float w = __shfl(u[j], from);
-      if (j == slot) o = w;
+      const float w = __shfl(v.at(j), from);
+      if (j == slot) o[i] = w;
     }
-    const float s = e < half ? -sign * sn[i] : sign * sn[i];
-    out[i] = e < a.rot ? u[i] * cs[i] + o * s : u[i];
   }
 }
 
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+// Sum over the LP lanes of a row, in each of them: neighbours, pairs of
+// neighbours, then mirrored halves of 8, 16, 32 and 64 lanes.
 template <int LP>
 __device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int m = 1; m < LP; m *= 2) v += __shfl_xor(v, m);
+  v += moved<0xb1>(v);                       // quad_perm 1 0 3 2
+  v += moved<0x4e>(v);                       // quad_perm 2 3 0 1
+  if (LP >= 8) v += moved<0x141>(v);         // row_half_mirror
+  if (LP >= 16) v += moved<0x140>(v);        // row_mirror
+  if (LP >= 32) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  if (LP >= 64) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
   return v;
 }
 
 template <int V>
-__device__ __forceinline__ void weight(const void* w, int dtype, int c, bool there, float (&v)[V]) {
+__device__ __forceinline__ void weight(const QkRope& a, bool key, int c, bool there, float (&v)[V]) {
+  const void* w = key ? a.kw : a.qw;
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = !there ? 0.f : w ? load_any(w, dtype, c + i) : 1.f;
+  for (int i = 0; i < V; ++i) v[i] = !there ? 0.f : w ? load_any(w, a.w_dtype, c + i) : 1.f;
 }
 
-// A row's lanes past d hold zeros.  Unit: HP virtual heads of one token.
+// A row's lanes past d hold zeros.
 template <typename T, int V, int LP, int HP>
-__global__ __launch_bounds__(kQkThreads) void k_qk_rope(QkRope a, int groups, long long units) {
-  const int lane = threadIdx.x % LP, c = lane * V;
-  const long long unit = (long long)blockIdx.x * (kQkThreads / LP) + threadIdx.x / LP;
-  if (unit >= units) return;                      // the LP lanes of a row leave together
-  const int gr = (int)(unit % groups);
-  const long long tok = unit / groups;
+__global__ __launch_bounds__(kQkThreads) void k_qk_rope(QkRope a) {
+  const int c = threadIdx.x % LP * V;
+  const Share s = share_of(a, blockIdx.x, HP, kQkThreads / LP);
+  const long long tok = s.tok0 + threadIdx.x / LP;
+  if (tok >= (long long)a.B * a.n) return;        // the LP lanes of a row leave together
   const int b = (int)(tok / a.n), t = (int)(tok - (long long)b * a.n);
   const bool there = c < a.d;
   const int hop = (a.rot / 2) % V == 0 ? a.rot / 2 / V : 0;
-  float x[HP][V];
+  const Rows& rows = s.key ? a.k : a.q;
+  const T* x = static_cast<const T*>(rows.p) + b * rows.bs + t * rows.ts + (size_t)s.h0 * a.d + c;
+  T* y = static_cast<T*>(s.key ? a.ko : a.qo) + (((size_t)b * (s.key ? a.Hk : a.H) + s.h0) * a.n + t) * a.d + c;
+  Raw<T, V> in[HP];
 #pragma unroll
   for (int k = 0; k < HP; ++k) {
-    const int v = min(gr * HP + k, a.H + a.Hk - 1);
-    if (there) {
-      load_vec<T, V>(head_at<T>(a, b, t, v).x + c, x[k]);
-    } else {
+    in[k].zero();
+    if (there) in[k].load(x + (size_t)min(k, s.heads - 1) * a.d);
+  }
+  // out_i = r (x_i w_i c_i + x_j w_j s_i), j the pair's other element
+  float own[V], pair[V];
+  {
+    float w[V], wo[V];
+    weight<V>(a, s.key, c, there, w);
+    angles<V>(a, b, t, c, own, pair);
+    Raw<float, V> wr;
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[k][i] = 0.f;
+    for (int i = 0; i < V; ++i) wr.w[i] = __float_as_uint(w[i]);
+    others<float, V>(a, c, hop, wr, wo);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      own[i] *= w[i];
+      pair[i] *= wo[i];
     }
   }
-  float cs[V], sn[V];
-  angles<V>(a, b, t, c, cs, sn);
 #pragma unroll
   for (int k = 0; k < HP; ++k) {
-    const int v = min(gr * HP + k, a.H + a.Hk - 1);
-    const Head<T> h = head_at<T>(a, b, t, v);
-    float w[V], u[V], o[V], ss = 0.f;
-    weight<V>(h.key ? a.kw : a.qw, a.w_dtype, c, there, w);
+    float o[V], ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) ss += x[k][i] * x[k][i];
+    for (int i = 0; i < V; ++i) ss += in[k].at(i) * in[k].at(i);
     const float r = 1.f / sqrtf(row_sum<LP>(ss) / a.d + a.eps);
+    others<T, V>(a, c, hop, in[k], o);
 #pragma unroll
-    for (int i = 0; i < V; ++i) u[i] = x[k][i] * r * w[i];
-    rotate<V>(a, c, hop, 1.f, u, cs, sn, o);
-    if (there && gr * HP + k < a.H + a.Hk)
-      store_vec<T, V>(static_cast<T*>(h.key ? a.ko : a.qo) + h.out * a.d + c, o);
+    for (int i = 0; i < V; ++i) o[i] = r * (in[k].at(i) * own[i] + (c + i < a.rot ? o[i] * pair[i] : 0.f));
+    if (there && k < s.heads) store_vec<T, V>(y + (size_t)k * a.n * a.d, o);
   }
 }
 
-// Gradients.  Blocks walk units by the grid's stride; a thread keeps its lane's
-// dimensions through all of them, so the two weights' gradients are summed in
-// registers, then over the block's rows in a fixed order, a row of partials
-// [2][d] a block; k_qk_sum adds the rows.
-constexpr int kQkBackBlocks = 2048;
+// Gradients.  Blocks walk the shares of one kind by the grid's stride; a
+// thread keeps its lane's dimensions through all of them, so the weight's
+// gradient is summed in registers, then over the block's rows in a fixed
+// order, a row of partials [d] a block; k_qk_sum adds the rows of each kind.
+constexpr int kQkBackBlocks = 1024;   // at most, of the two kinds together
 
 template <typename T, int V, int LP, int HP>
-__global__ __launch_bounds__(kQkThreads) void k_qk_rope_back(QkRope a, int groups, long long units,
-                                                             float* __restrict__ part) {
+__global__ __launch_bounds__(kQkThreads) void k_qk_rope_back(QkRope a, int qblocks, float* __restrict__ part) {
   constexpr int RB = kQkThreads / LP;
-  const int lane = threadIdx.x % LP, c = lane * V;
-  const bool there = c < a.d;
+  const int c = threadIdx.x % LP * V;
+  const bool there = c < a.d, key = (int)blockIdx.x >= qblocks;
   const int hop = (a.rot / 2) % V == 0 ? a.rot / 2 / V : 0;
-  float dw[2][V];
+  const int nb = key ? gridDim.x - qblocks : qblocks, me = key ? blockIdx.x - qblocks : blockIdx.x;
+  const int heads = key ? a.Hk : a.H, groups = (heads + HP - 1) / HP;
+  const long long toks = (long long)a.B * a.n, units = (toks + RB - 1) / RB * groups;
+  const Rows& rows = key ? a.k : a.q;
+  float dw[V], w[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) dw[0][i] = dw[1][i] = 0.f;
-  for (long long unit = (long long)blockIdx.x * RB + threadIdx.x / LP; unit < units;
-       unit += (long long)gridDim.x * RB) {
-    const int gr = (int)(unit % groups);
-    const long long tok = unit / groups;
-    const int b = (int)(tok / a.n), t = (int)(tok - (long long)b * a.n);
-    float x[HP][V], g[HP][V];
+  for (int i = 0; i < V; ++i) dw[i] = 0.f;
+  weight<V>(a, key, c, there, w);
+  for (long long unit = me; unit < units; unit += nb) {
+    const int h0 = (int)(unit % groups) * HP;
+    const long long tok = unit / groups * RB + threadIdx.x / LP;
+    if (tok >= toks) continue;
+    const int b = (int)(tok / a.n), t = (int)(tok - (long long)b * a.n), last = min(HP, heads - h0) - 1;
+    const T* x = static_cast<const T*>(rows.p) + b * rows.bs + t * rows.ts + (size_t)h0 * a.d + c;
+    const T* g = static_cast<const T*>(key ? a.gk : a.gq) + (((size_t)b * heads + h0) * a.n + t) * a.d + c;
+    T* dx = static_cast<T*>(key ? a.dk : a.dq) + (((size_t)b * a.n + t) * heads + h0) * a.d + c;
+    Raw<T, V> in[HP], up[HP];
 #pragma unroll
     for (int k = 0; k < HP; ++k) {
-      const int v = min(gr * HP + k, a.H + a.Hk - 1);
-      const Head<T> h = head_at<T>(a, b, t, v);
+      in[k].zero();
+      up[k].zero();
       if (there) {
-        load_vec<T, V>(h.x + c, x[k]);
-        load_vec<T, V>(static_cast<const T*>(h.key ? a.gk : a.gq) + h.out * a.d + c, g[k]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[k][i] = g[k][i] = 0.f;
+        in[k].load(x + (size_t)min(k, last) * a.d);
+        up[k].load(g + (size_t)min(k, last) * a.n * a.d);
       }
     }
     float cs[V], sn[V];
     angles<V>(a, b, t, c, cs, sn);
 #pragma unroll
     for (int k = 0; k < HP; ++k) {
-      const int v = min(gr * HP + k, a.H + a.Hk - 1);
-      const Head<T> h = head_at<T>(a, b, t, v);
-      float w[V], du[V], ss = 0.f, dot = 0.f;
-      weight<V>(h.key ? a.kw : a.qw, a.w_dtype, c, there, w);
-      rotate<V>(a, c, hop, -1.f, g[k], cs, sn, du);
-#pragma unroll
-      for (int i = 0; i < V; ++i) ss += x[k][i] * x[k][i];
-      const float r = 1.f / sqrtf(row_sum<LP>(ss) / a.d + a.eps);
+      // u: the gradient turned back, by the negative angle
+      float u[V], ss = 0.f, dot = 0.f;
+      others<T, V>(a, c, hop, up[k], u);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        x[k][i] *= r;
-        dot += du[i] * w[i] * x[k][i];
+        u[i] = up[k].at(i) * cs[i] - (c + i < a.rot ? u[i] * sn[i] : 0.f);
+        ss += in[k].at(i) * in[k].at(i);
+        dot += u[i] * w[i] * in[k].at(i);
       }
-      const float mean = row_sum<LP>(dot) / a.d;
-      if (there && gr * HP + k < a.H + a.Hk) {
-        float dx[V];
+      const float r = 1.f / sqrtf(row_sum<LP>(ss) / a.d + a.eps);
+      const float mean = row_sum<LP>(dot) / a.d * (r * r * r);
+      if (there && k <= last) {
+        float o[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          dx[i] = r * (du[i] * w[i] - x[k][i] * mean);
-          dw[0][i] += h.key ? 0.f : du[i] * x[k][i];
-          dw[1][i] += h.key ? du[i] * x[k][i] : 0.f;
+          o[i] = r * (u[i] * w[i]) - in[k].at(i) * mean;
+          dw[i] += u[i] * (in[k].at(i) * r);
         }
-        const int i = h.key ? v - a.H : v, heads = h.key ? a.Hk : a.H;
-        store_vec<T, V>(static_cast<T*>(h.key ? a.dk : a.dq) + (((size_t)b * a.n + t) * heads + i) * a.d + c, dx);
+        store_vec<T, V>(dx + (size_t)k * a.d, o);
       }
     }
   }
   __shared__ float red[RB][LP * V + 1];
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) red[threadIdx.x / LP][c + i] = dw[z][i];
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.d; e += kQkThreads) {
-      float s = 0.f;
-      for (int r = 0; r < RB; ++r) s += red[r][e];
-      part[((size_t)blockIdx.x * 2 + z) * a.d + e] = s;
-    }
-    __syncthreads();
+  for (int i = 0; i < V; ++i) red[threadIdx.x / LP][c + i] = dw[i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.d; e += kQkThreads) {
+    float s = 0.f;
+    for (int r = 0; r < RB; ++r) s += red[r][e];
+    part[(size_t)blockIdx.x * a.d + e] = s;
   }
 }
 
+// part [blocks][d], the queries' qblocks first -> the weights' gradients.  grid (columns, kinds).
 constexpr int kQkSumRows = 64, kQkSumCols = 16;
-__global__ __launch_bounds__(kQkSumRows * kQkSumCols) void k_qk_sum(QkRope a, const float* __restrict__ part,
-                                                                    int rows) {
+__global__ __launch_bounds__(kQkSumRows * kQkSumCols) void k_qk_sum(QkRope a, const float* __restrict__ part, int qblocks,
+                                                                    int blocks) {
   __shared__ float red[kQkSumRows][kQkSumCols];
   const int cl = threadIdx.x % kQkSumCols, rg = threadIdx.x / kQkSumCols, col = blockIdx.x * kQkSumCols + cl;
+  const bool key = blockIdx.y != 0;
   float s = 0.f;
-  if (col < 2 * a.d)
-    for (int r = rg; r < rows; r += kQkSumRows) s += part[(size_t)r * 2 * a.d + col];
+  if (col < a.d)
+    for (int r = (key ? qblocks : 0) + rg; r < (key ? blocks : qblocks); r += kQkSumRows) s += part[(size_t)r * a.d + col];
   red[rg][cl] = s;
   __syncthreads();
-  if (rg != 0 || col >= 2 * a.d) return;
+  if (rg != 0 || col >= a.d) return;
   for (int r = 1; r < kQkSumRows; ++r) s += red[r][cl];
-  void* to = col < a.d ? a.dqw : a.dkw;
-  if (to) store_any(to, a.w_dtype, col % a.d, s);
+  void* to = key ? a.dkw : a.dqw;
+  if (to) store_any(to, a.w_dtype, col, s);
 }
 
 template <typename T, int V, int LP, int HP>
 hipError_t launch(const QkRope& a, float* part, hipStream_t s) {
-  const int groups = (a.H + a.Hk + HP - 1) / HP;
-  const long long units = (long long)a.B * a.n * groups, per = kQkThreads / LP;
-  const long long blocks = (units + per - 1) / per;
+  constexpr int RB = kQkThreads / LP;
+  const long long tb = ((long long)a.B * a.n + RB - 1) / RB;
+  const int gq = (a.H + HP - 1) / HP, gk = (a.Hk + HP - 1) / HP;
   if (!part)
-    return HLA_TIMED("qk_norm_rope", (k_qk_rope<T, V, LP, HP>), dim3((unsigned)blocks), dim3(kQkThreads), 0, s, a,
-                     groups, units);
-  const int nb = (int)(blocks < kQkBackBlocks ? blocks : kQkBackBlocks);
-  const hipError_t e = HLA_TIMED("qk_norm_rope_back", (k_qk_rope_back<T, V, LP, HP>), dim3(nb), dim3(kQkThreads), 0, s,
-                                 a, groups, units, part);
+    return HLA_TIMED("qk_norm_rope", (k_qk_rope<T, V, LP, HP>), dim3((unsigned)(tb * (gq + gk))), dim3(kQkThreads), 0, s, a);
+  // each kind the blocks of its share of the rows
+  auto some = [&](int mine) {
+    const long long most = (long long)kQkBackBlocks * mine / (gq + gk), units = tb * mine;
+    return (int)(units < 1 || most < 1 ? 1 : units < most ? units : most);
+  };
+  const int qb = some(gq), kb = some(gk);
+  const hipError_t e = HLA_TIMED("qk_norm_rope_back", (k_qk_rope_back<T, V, LP, HP>), dim3(qb + kb), dim3(kQkThreads), 0, s,
+                                 a, qb, part);
   if (e != hipSuccess || (!a.dqw && !a.dkw)) return e;
-  return HLA_TIMED("qk_sum", k_qk_sum, dim3((2 * a.d + kQkSumCols - 1) / kQkSumCols), dim3(kQkSumRows * kQkSumCols), 0, s,
-                   a, part, nb);
+  return HLA_TIMED("qk_sum", k_qk_sum, dim3((a.d + kQkSumCols - 1) / kQkSumCols, 2), dim3(kQkSumRows * kQkSumCols), 0, s, a,
+                   part, qb, qb + kb);
 }
 
-// four heads a thread where that still leaves every CU eight waves, one otherwise (a few tokens)
+// HP heads a thread where that still leaves every CU eight waves, one otherwise (a few tokens).
+// Forward eight (a load each), gradients four (two loads each).
 template <typename T, int V, int LP>
 hipError_t by_heads(const QkRope& a, float* part, hipStream_t s) {
   const long long rows = (long long)a.B * a.n * (a.H + a.Hk);
-  if (rows * LP / 4 >= 256LL * 8 * 64) return launch<T, V, LP, 4>(a, part, s);
-  return launch<T, V, LP, 1>(a, part, s);
+  if (part) return rows * LP / 4 >= 256LL * 8 * 64 ? launch<T, V, LP, 4>(a, part, s) : launch<T, V, LP, 1>(a, part, s);
+  return rows * LP / 8 >= 256LL * 8 * 64 ? launch<T, V, LP, 8>(a, part, s) : launch<T, V, LP, 1>(a, part, s);
 }
 
 template <typename T, int V>
@@ -299,7 +334,7 @@ hipError_t by_type(const QkRope& a, float* part, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_qk_rope(const QkRope& a, hipStream_t s) { return by_type(a, nullptr, s); }
-size_t qk_rope_backward_ws(int d) { return sizeof(float) * kQkBackBlocks * 2 * (size_t)d; }
+size_t qk_rope_backward_ws(int d) { return sizeof(float) * (kQkBackBlocks + 2) * (size_t)d; }
 hipError_t launch_qk_rope_backward(const QkRope& a, void* ws, hipStream_t s) {
   return by_type(a, static_cast<float*>(ws), s);
 }

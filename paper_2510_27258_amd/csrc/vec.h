@@ -1,4 +1,4 @@
-// 16-byte vectors of bf16 or fp32 values for the streaming kernels, and
+// Vectors (16 bytes, or 8 of bf16) of bf16 or fp32 values for the streaming kernels, and
 // values whose type is known at run time only (weights).
 #pragma once
 #include "common.h"
@@ -11,49 +11,89 @@ struct bf16 {
 
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
+// The bits of V values in memory, and their values.
+template <typename T, int V>
+struct Raw {
+  static constexpr int N = sizeof(T) * V / 4;
+  static_assert(N % 4 == 0 || N == 2 || V == 1, "a vector is 8 bytes or whole 16, or one value");
+  uint32_t w[N ? N : 1];
+
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (N ? N : 1); ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[i / 4];
+        w[i] = u.x;
+        w[i + 1] = u.y;
+        w[i + 2] = u.z;
+        w[i + 3] = u.w;
+      }
+    } else if constexpr (N == 2) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      w[0] = u.x;
+      w[1] = u.y;
+    } else if constexpr (sizeof(T) == 2) {
+      w[0] = (uint32_t)p->bits << 16;
+    } else {
+      w[0] = __float_as_uint(*p);
+    }
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (V == 1 || sizeof(T) == 4)
+      return __uint_as_float(w[i]);
+    else
+      return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+
 template <typename T, int V>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[V]) {
-  if constexpr (sizeof(T) * V == 16) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t a[4] = {u.x, u.y, u.z, u.w};
-    if constexpr (V == 8) {
+  Raw<T, V> r;
+  r.load(p);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(a[i] << 16);
-        v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]);
-    }
-  } else {
-    static_assert(V == 1, "a vector is 16 bytes or one value");
-    if constexpr (sizeof(T) == 2)
-      v[0] = __uint_as_float((uint32_t)p->bits << 16);
-    else
-      v[0] = *p;
-  }
+  for (int i = 0; i < V; ++i) v[i] = r.at(i);
 }
 
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
-  if constexpr (sizeof(T) * V == 16) {
-    uint32_t a[4];
-    if constexpr (V == 8) {
-      typedef float f2 __attribute__((ext_vector_type(2)));
-      typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        a[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2 * i], v[2 * i + 1]}, b2));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]);
-    }
-    *reinterpret_cast<uint4*>(p) = make_uint4(a[0], a[1], a[2], a[3]);
-  } else if constexpr (sizeof(T) == 2) {
-    p->bits = to_bf16(v[0]);
+  constexpr int N = Raw<T, V>::N;
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 2)
+      p->bits = to_bf16(v[0]);
+    else
+      *p = v[0];
   } else {
-    *p = v[0];
+    uint32_t a[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        a[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2 * i], v[2 * i + 1]}, b2));
+      } else {
+        a[i] = __float_as_uint(v[i]);
+      }
+    }
+    if constexpr (N == 4)
+      *reinterpret_cast<uint4*>(p) = make_uint4(a[0], a[1], a[2], a[3]);
+    else
+      *reinterpret_cast<uint2*>(p) = make_uint2(a[0], a[1]);
+  }
+}
+
+// M values (a multiple of V) that start on a whole vector
+template <typename T, int V, int M>
+__device__ __forceinline__ void load_many(const void* p, size_t i, float (&v)[M]) {
+#pragma unroll
+  for (int j = 0; j < M / V; ++j) {
+    Raw<T, V> r;
+    r.load(static_cast<const T*>(p) + i + j * V);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[j * V + k] = r.at(k);
   }
 }
 
