@@ -60,22 +60,29 @@ def _on_gpu(t):
         raise ValueError("tensors must be on the GPU")
 
 
-class _Device:
-    """The current device is the tensor's within (a launch goes to the current device's context)."""
+# the device and stream of the calling thread, without torch.cuda's wrappers: they cost a decode call more than its kernel
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __init__(self, t):
-        self.index, self.back = t.device.index, None
 
-    def __enter__(self):
-        now = torch.cuda.current_device()
-        if now != self.index:
-            self.back = now
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream().cuda_stream
+def _launch(entry, t, *args):
+    """entry(*args, the current stream of t's device), with that device current:
+    a launch goes to the current device's context."""
+    index = t.device.index
+    now = _device()
+    if now == index:
+        entry(*args, _raw_stream(index))
+        return
+    torch.cuda.set_device(index)
+    try:
+        entry(*args, _raw_stream(index))
+    finally:
+        torch.cuda.set_device(now)
 
-    def __exit__(self, *_):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
+
+def _learns(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 def _out(out, shape, like, name="out"):
@@ -115,9 +122,8 @@ def _conv(x, weight, bias, silu, state, out, rank):
     _same("state", state, (B, K - 1, D), x.dtype, x.device, contiguous=True)
     rows = _rows("x", x, 1)
     out = _out(out, x.shape, x)
-    with _Device(x) as stream:
-        capi.hla_conv_forward(*rows, weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), B, n, D, K,
-                              int(bool(silu)), code, wcode, stream)
+    _launch(capi.hla_conv_forward, x, *rows, weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), B, n, D,
+            K, int(bool(silu)), code, wcode)
     return out
 
 
@@ -153,9 +159,8 @@ def conv_backward(x, weight, bias, dy, silu=True):
     dw = torch.empty_like(weight)
     db = None if bias is None else torch.empty_like(bias)
     ws, nb = _space(capi.hla_conv_backward_workspace_bytes(B, n, D, K), x.device)
-    with _Device(x) as stream:
-        capi.hla_conv_backward(*rows, weight.data_ptr(), _ptr(bias), *grows, dx.data_ptr(), dw.data_ptr(), _ptr(db),
-                               B, n, D, K, int(bool(silu)), code, wcode, ws.data_ptr(), nb, stream)
+    _launch(capi.hla_conv_backward, x, *rows, weight.data_ptr(), _ptr(bias), *grows, dx.data_ptr(), dw.data_ptr(),
+            _ptr(db), B, n, D, K, int(bool(silu)), code, wcode, ws.data_ptr(), nb)
     return dx, dw, db
 
 
@@ -178,6 +183,8 @@ class ShortConv(torch.autograd.Function):
 
 def short_conv(x, weight, bias=None, silu=True):
     """Differentiable conv_forward."""
+    if not _learns(x, weight, bias):
+        return conv_forward(x, weight, bias, silu)
     return ShortConv.apply(x, weight, bias, silu)
 
 
@@ -235,9 +242,8 @@ def qk_norm_rope_forward(q, k, q_weight=None, k_weight=None, cos=None, sin=None,
     B, n, H, Hk, d = sizes[:5]
     qo = torch.empty((B, H, n, d), dtype=q.dtype, device=q.device)
     ko = torch.empty((B, Hk, n, d), dtype=q.dtype, device=q.device)
-    with _Device(q) as stream:
-        capi.hla_qk_norm_rope(*lead, qo.data_ptr(), ko.data_ptr(), *sizes, int(bool(interleaved)), float(eps), *codes,
-                              stream)
+    _launch(capi.hla_qk_norm_rope, q, *lead, qo.data_ptr(), ko.data_ptr(), *sizes, int(bool(interleaved)),
+            float(eps), *codes)
     return qo, ko
 
 
@@ -252,10 +258,9 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, positions, dq_out,
     dk = torch.empty((B, n, Hk, d), dtype=q.dtype, device=q.device)
     dqw, dkw = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
     ws, nb = _space(capi.hla_qk_norm_rope_backward_workspace_bytes(d), q.device)
-    with _Device(q) as stream:
-        capi.hla_qk_norm_rope_backward(*lead, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-                                       _ptr(dqw), _ptr(dkw), *sizes, int(bool(interleaved)), float(eps), *codes,
-                                       ws.data_ptr(), nb, stream)
+    _launch(capi.hla_qk_norm_rope_backward, q, *lead, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(),
+            dk.data_ptr(), _ptr(dqw), _ptr(dkw), *sizes, int(bool(interleaved)), float(eps), *codes, ws.data_ptr(),
+            nb)
     return dq, dk, dqw, dkw
 
 
@@ -276,6 +281,8 @@ class QKNormRope(torch.autograd.Function):
 
 def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, positions=None, eps=1e-6, interleaved=False):
     """Differentiable qk_norm_rope_forward (in q, k and the weights)."""
+    if not _learns(q, k, q_weight, k_weight):
+        return qk_norm_rope_forward(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     return QKNormRope.apply(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
 
 
@@ -307,9 +314,8 @@ def _ssm(state, x, dt, A, Bm, Cm, D, dt_bias, softplus, out, workspace):
     _same("state", state, (B, H, N, P), torch.float32, x.device, contiguous=True)
     out = _out(out, x.shape, x)
     ws, nb = _space(capi.hla_ssm_workspace_bytes(*sizes, codes[0]), x.device, workspace)
-    with _Device(x) as stream:
-        capi.hla_ssm_forward(*rx, *rt, A.data_ptr(), *rb, *rc, _ptr(D), _ptr(dt_bias), _ptr(state), out.data_ptr(),
-                             *sizes, int(bool(softplus)), *codes, ws.data_ptr(), nb, stream)
+    _launch(capi.hla_ssm_forward, x, *rx, *rt, A.data_ptr(), *rb, *rc, _ptr(D), _ptr(dt_bias), _ptr(state),
+            out.data_ptr(), *sizes, int(bool(softplus)), *codes, ws.data_ptr(), nb)
     return out
 
 
@@ -336,9 +342,8 @@ def ssm_step(state, x_t, dt_t, A, B_t, C_t, D=None, dt_bias=None, softplus=True,
         raise ValueError("ssm_step needs a state")
     _same("state", state, (B, H, N, P), torch.float32, x_t.device, contiguous=True)
     out = _out(out, x_t.shape, x_t)
-    with _Device(x_t) as stream:
-        capi.hla_ssm_step(state.data_ptr(), *rx[:2], *rt[:2], A.data_ptr(), *rb[:2], *rc[:2], _ptr(D), _ptr(dt_bias),
-                          out.data_ptr(), B, H, P, G, N, int(bool(softplus)), *codes, stream)
+    _launch(capi.hla_ssm_step, x_t, state.data_ptr(), *rx[:2], *rt[:2], A.data_ptr(), *rb[:2], *rc[:2], _ptr(D),
+            _ptr(dt_bias), out.data_ptr(), B, H, P, G, N, int(bool(softplus)), *codes)
     return out
 
 
@@ -351,10 +356,9 @@ def ssm_backward(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus=True):
     dx, ddt, dB, dC = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (x, dt, Bm, Cm))
     dA, dD, db = (None if t is None else torch.empty_like(t) for t in (A, D, dt_bias))
     ws, nb = _space(capi.hla_ssm_backward_workspace_bytes(*sizes, codes[0]), x.device)
-    with _Device(x) as stream:
-        capi.hla_ssm_backward(*rx, *rt, A.data_ptr(), *rb, *rc, _ptr(D), _ptr(dt_bias), *ry, dx.data_ptr(),
-                              ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), _ptr(dD), _ptr(db), *sizes,
-                              int(bool(softplus)), *codes, ws.data_ptr(), nb, stream)
+    _launch(capi.hla_ssm_backward, x, *rx, *rt, A.data_ptr(), *rb, *rc, _ptr(D), _ptr(dt_bias), *ry, dx.data_ptr(),
+            ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), _ptr(dD), _ptr(db), *sizes,
+            int(bool(softplus)), *codes, ws.data_ptr(), nb)
     return dx, ddt, dA, dB, dC, dD, db
 
 
@@ -374,4 +378,6 @@ class SSMScan(torch.autograd.Function):
 
 def ssm_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus=True):
     """Differentiable ssm_forward."""
+    if not _learns(x, dt, A, Bm, Cm, D, dt_bias):
+        return ssm_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus)
     return SSMScan.apply(x, dt, A, Bm, Cm, D, dt_bias, softplus)
