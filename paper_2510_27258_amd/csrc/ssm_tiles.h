@@ -108,10 +108,14 @@ __device__ __forceinline__ void pieces4(const float (&v)[4], uint2 (&p)[NP]) {
 __device__ __forceinline__ bf16x8 frag(const uint16_t* X, int ld, int row0, int k0, int l) {
   return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(X + (row0 + (l & 15)) * ld + k0 + 8 * (l >> 4)));
 }
-// frag_acc: row row0 + r in the k order of two accumulator blocks, k0 + 4g .. + 3 and k0 + 16 + 4g .. + 3.
-__device__ __forceinline__ bf16x8 frag_acc(const uint16_t* X, int ld, int row0, int k0, int l) {
-  const uint16_t* p = X + (row0 + (l & 15)) * ld + k0 + 4 * (l >> 4);
-  const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + 16);
+// A tile whose rows are stored in the order of accumulator pairs: value 16 a +
+// 4 b + i of each 32 sits at 8 b + 4 a + i, so that frag() takes k0 + 4g .. + 3
+// and k0 + 16 + 4g .. + 3, the order of two accumulator blocks as one operand.
+// frag_plain: the 8 values k0 + 8g .. + 7 of row row0 + r of such a tile.
+__device__ __forceinline__ bf16x8 frag_plain(const uint16_t* X, int ld, int row0, int k0, int l) {
+  const int g = l >> 4;
+  const uint16_t* p = X + (row0 + (l & 15)) * ld + k0 + 16 * (g & 1) + 4 * (g >> 1);
+  const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + 8);
   return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y));
 }
 // frag_tr: column n0 + r, rows k0 + 8g .. + 7, through the LDS transpose unit:
@@ -128,7 +132,7 @@ __device__ __forceinline__ bf16x8 frag_tr(const uint16_t* Y, int ld, int n0, int
   return __builtin_bit_cast(bf16x8, make_uint4(ua.x, ua.y, ub.x, ub.y));
 }
 
-// Two accumulator blocks (rows 16 b + 4g + i of one column) as a fragment in frag_acc's k order.
+// Two accumulator blocks (rows 16 b + 4g + i of one column) as a fragment in the order of accumulator pairs.
 template <int NP>
 __device__ __forceinline__ void frag_from_acc(const f32x4& lo, const f32x4& hi, bf16x8 (&p)[NP]) {
   const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -180,8 +184,9 @@ struct Tile {
     most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, m));
   }
 
-  // The tile as NX planes of Q rows.  CHECK: returns whether a value of this thread's is infinite or NaN.
-  template <bool CHECK>
+  // The tile as NX planes of Q rows.  CHECK: returns whether a value of this
+  // thread's is infinite or NaN.  PAIRS: rows in the order of accumulator pairs.
+  template <bool CHECK, bool PAIRS = false>
   __device__ __forceinline__ bool store(uint16_t* X, int tid) const {
     uint32_t most = 0;
     if (!kAll && tid >= TOT) return false;
@@ -196,8 +201,15 @@ struct Tile {
           note(most, r[i].z);
           note(most, r[i].w);
         }
-        *reinterpret_cast<uint4*>(to) = r[i];
+        if constexpr (PAIRS) {
+          uint16_t* half = X + row * LD + (c & ~31) + 2 * (c & 8) + ((c & 16) >> 2);
+          *reinterpret_cast<uint2*>(half) = make_uint2(r[i].x, r[i].y);
+          *reinterpret_cast<uint2*>(half + 8) = make_uint2(r[i].z, r[i].w);
+        } else {
+          *reinterpret_cast<uint4*>(to) = r[i];
+        }
       } else {
+        if (PAIRS) to = X + row * LD + (c & ~31) + 2 * (c & 12) + ((c & 16) >> 2);
         const float v[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z),
                             __uint_as_float(r[i].w)};
         uint2 p[NX];
@@ -249,10 +261,10 @@ __device__ __forceinline__ void load_frags(const uint16_t* X, int plane, int ld,
   for (int k = 0; k < NP; ++k) f[k] = frag(X + k * plane, ld, row0, k0, l);
 }
 template <int NP>
-__device__ __forceinline__ void load_frags_acc(const uint16_t* X, int plane, int ld, int row0, int k0, int l,
-                                               bf16x8 (&f)[NP]) {
+__device__ __forceinline__ void load_frags_plain(const uint16_t* X, int plane, int ld, int row0, int k0, int l,
+                                                 bf16x8 (&f)[NP]) {
 #pragma unroll
-  for (int k = 0; k < NP; ++k) f[k] = frag_acc(X + k * plane, ld, row0, k0, l);
+  for (int k = 0; k < NP; ++k) f[k] = frag_plain(X + k * plane, ld, row0, k0, l);
 }
 template <int NP>
 __device__ __forceinline__ void load_frags_tr(const uint16_t* X, int plane, int ld, int n0, int k0, int l,

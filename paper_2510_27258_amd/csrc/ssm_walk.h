@@ -46,6 +46,8 @@ struct WalkLds {
   static constexpr int NX = Kind<T>::NX, Q = Kind<T>::Q;
   static constexpr int LDK = ld_of(NN), LDX = ld_of(PP), LDS_ = ld_of(Q);
   uint16_t k[NX * Q * LDK], x[NX * Q * LDX];
+  // q in the order of accumulator pairs: the readout takes it with the state's
+  // accumulators in 16-byte reads (as two 8-byte ones they met in the banks)
   uint16_t q[MODE == kOutputs ? NX * Q * LDK : 8], s[MODE == kOutputs ? NX * Q * LDS_ : 8];
   float Lh[Q], Ll[Q], dt[Q], w[Q];
   int firstx[PP], firstk[NN], first_all, bad[2];
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
     bool bad = tk.template store<MODE == kOutputs>(S.k, tid);
     bad |= tx.template store<MODE == kOutputs>(S.x, tid);
-    if (MODE == kOutputs) tq.template store<false>(S.q, tid);
+    if (MODE == kOutputs) tq.template store<false, true>(S.q, tid);
     if (tid < Q) {
       S.Lh[tid] = st.Lh;
       S.Ll[tid] = st.Ll;
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
       // loads and products of all its blocks are in flight together.
       auto rows_of = [&](int tb, bf16x8 (&cf)[KN][NX]) {
 #pragma unroll
-        for (int k = 0; k < KN; ++k) load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
+        for (int k = 0; k < KN; ++k) load_frags_plain<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf[k]);
       };
       auto product = [&](int sb, const bf16x8 (&cf)[KN][NX]) {
         f32x4 acc = zero4();
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
           bf16x8 cf[NX];
-          load_frags_acc<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf);
+          load_frags<NX>(S.q, PK, LDK, 16 * tb, 32 * k, l, cf);
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) mma_pieces<NX, NX>(hf[cb], cf, y[tb][cb]);
         }
