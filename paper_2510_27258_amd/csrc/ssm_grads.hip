@@ -398,11 +398,11 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
       }
       const double back = (double)R - (double)dt * K + Et, ahead = (double)dt * Fs;
       const double upto = sums_to(back), suf = last_lane(upto) - upto + back, pre = sums_to(ahead) - ahead;
-      const float da = (float)(suf + pre + (double)exp2_(Lend) * hg);
-      float d = a.A[head] * da + (K + S.own[l] + Fs);
+      const double da = suf + pre + (double)exp2_(Lend) * hg;
+      double d = (double)a.A[head] * da + ((double)K + S.own[l] + Fs);
       if (a.softplus) d *= -expm1f(-dt);
-      if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, d);
-      const float dA = sum_wave(l < rows ? dt * da : 0.f), db = sum_wave(l < rows ? d : 0.f);
+      if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, (float)d);
+      const float dA = (float)last_lane(sums_to(l < rows ? dt * da : 0.0)), db = (float)last_lane(sums_to(l < rows ? d : 0.0));
       if (l == 0) {
         float* o = a.par + ((size_t)bh * a.tiles + tile) * 3;
         o[0] = dA;
