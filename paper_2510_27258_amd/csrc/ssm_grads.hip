@@ -136,13 +136,13 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   const uint32_t y1 = TP::first(a.dy.ts, a.P, tid), yby = TP::step(a.dy.ts);
   Step st{};
   auto fetch = [&](int head) {
-    tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, a.x.ts, a.P, x1, xby);
-    ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, a.dy.ts, a.P, y1, yby);
+    tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, (int)a.x.ts * 2, a.P, x1, xby);
+    ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, (int)a.dy.ts * 2, a.P, y1, yby);
     st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + (tid & (kGQ - 1))];
   };
-  tn.load(reinterpret_cast<const bf16*>(kp), rows, a.k.ts, a.N, TN::first(a.k.ts, a.N, tid), TN::step(a.k.ts));
+  tn.load(reinterpret_cast<const bf16*>(kp), rows, (int)a.k.ts * 2, a.N, TN::first(a.k.ts, a.N, tid), TN::step(a.k.ts));
   tn.template store<false>(S.k, tid);
-  tn.load(reinterpret_cast<const bf16*>(qp), rows, a.q.ts, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
+  tn.load(reinterpret_cast<const bf16*>(qp), rows, (int)a.q.ts * 2, a.N, TN::first(a.q.ts, a.N, tid), TN::step(a.q.ts));
   tn.template store<false>(S.q, tid);
   // rows n0 + r of the states; each is loaded anew, for the next head, as soon
   // as its pieces are made.  At P > 64 both do not fit the registers beside

@@ -31,6 +31,9 @@ __device__ __forceinline__ float nan_() { return __builtin_nanf(""); }
 __device__ __forceinline__ rsrc_t rows_rsrc(const void* p, long long bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)(bytes > 0 ? bytes : 0), 0x00020000);
 }
+__device__ __forceinline__ rsrc_t tile_rsrc(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, 0x00020000);
+}
 __device__ __forceinline__ uint4 load16(rsrc_t r, uint32_t off) {
   const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
   return make_uint4(x[0], x[1], x[2], x[3]);
@@ -61,6 +64,19 @@ __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+
+// The order of the instructions before it: N products, each with V vector
+// operations and an LDS read.  A product occupies the matrix core four times
+// as long as it takes to issue; what the wave issues behind it is free.
+template <int N, int V>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  }
+}
 
 template <int NA, int NB>
 __device__ __forceinline__ void mma_pieces(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4& c) {
@@ -170,9 +186,10 @@ struct Tile {
     return c < w && (kAll || tid < TOT) ? (uint32_t)((row * (int)ts + c) * (int)sizeof(T)) : kOut;
   }
   static __device__ __forceinline__ uint32_t step(long long ts) { return (THR / PR) * (uint32_t)ts * sizeof(T); }
-  // The tile from its first row on, of which `rows` are valid: the others lie past the resource's end.
-  __device__ __forceinline__ void load(const T* base, int rows, long long ts, int w, uint32_t off, uint32_t by) {
-    const rsrc_t rs = rows_rsrc(base, ((long long)(rows - 1) * ts + w) * (long long)sizeof(T));
+  // The tile from its first row on, of which `rows` are valid: the others lie
+  // past the resource's end.  A tile's bytes fit 31 bits (checked on the host).
+  __device__ __forceinline__ void load(const void* base, int rows, int row_bytes, int w, uint32_t off, uint32_t by) {
+    const rsrc_t rs = tile_rsrc(base, (rows - 1) * row_bytes + w * (int)sizeof(T));
 #pragma unroll
     for (int i = 0; i < CNT; ++i) r[i] = load16(rs, off + i * by);
   }
@@ -190,10 +207,13 @@ struct Tile {
   __device__ __forceinline__ bool store(uint16_t* X, int tid) const {
     uint32_t most = 0;
     if (!kAll && tid >= TOT) return false;
+    const int row0 = tid / PR, c = (tid % PR) * V;
+    // in the order of accumulator pairs the halves of 8 values are 8 apart
+    const int c2 = PAIRS ? (c & ~31) + 2 * (c & (NX == 1 ? 8 : 12)) + ((c & 16) >> 2) : c;
+    uint16_t* first = X + row0 * LD + c2;
 #pragma unroll
     for (int i = 0; i < CNT; ++i) {
-      const int e = tid + THR * i, row = e / PR, c = (e % PR) * V;
-      uint16_t* to = X + row * LD + c;
+      uint16_t* to = first + i * (THR / PR) * LD;
       if constexpr (NX == 1) {
         if (CHECK) {
           note(most, r[i].x);
@@ -202,14 +222,12 @@ struct Tile {
           note(most, r[i].w);
         }
         if constexpr (PAIRS) {
-          uint16_t* half = X + row * LD + (c & ~31) + 2 * (c & 8) + ((c & 16) >> 2);
-          *reinterpret_cast<uint2*>(half) = make_uint2(r[i].x, r[i].y);
-          *reinterpret_cast<uint2*>(half + 8) = make_uint2(r[i].z, r[i].w);
+          *reinterpret_cast<uint2*>(to) = make_uint2(r[i].x, r[i].y);
+          *reinterpret_cast<uint2*>(to + 8) = make_uint2(r[i].z, r[i].w);
         } else {
           *reinterpret_cast<uint4*>(to) = r[i];
         }
       } else {
-        if (PAIRS) to = X + row * LD + (c & ~31) + 2 * (c & 12) + ((c & 16) >> 2);
         const float v[4] = {__uint_as_float(r[i].x), __uint_as_float(r[i].y), __uint_as_float(r[i].z),
                             __uint_as_float(r[i].w)};
         uint2 p[NX];

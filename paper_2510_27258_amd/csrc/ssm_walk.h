@@ -112,30 +112,41 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
                                  : nullptr;
   const Step* tab = a.tab + (size_t)bh * a.tok;
   // outputs: row r of a 16-token block, columns pw + 4g .. + 3 of a column block
-  T* yp = MODE == kOutputs ? static_cast<T*>(a.y) + (size_t)b * a.n * a.H * a.P : nullptr;
-  const int ystep = 16 * a.H * a.P * (int)sizeof(T);
+  const int ybytes = a.H * a.P * (int)sizeof(T), ystep = 16 * ybytes;
+  char* yp = MODE == kOutputs ? static_cast<char*>(a.y) + ((size_t)b * a.n + (size_t)i0 * Q) * ybytes : nullptr;
   const uint32_t yoff = (uint32_t)((r * a.H * a.P + head * a.P + pw + 4 * g) * (int)sizeof(T));
 
   Tile<T, NN, THR> tk, tq;
   Tile<T, PP, THR> tx;
   Step st{};
-  const long long kts = a.k.ts, xts = a.x.ts, qts = a.q.ts;
-  const uint32_t k1 = Tile<T, NN, THR>::first(kts, a.N, tid), kby = Tile<T, NN, THR>::step(kts);
-  const uint32_t x1 = Tile<T, PP, THR>::first(xts, a.P, tid), xby = Tile<T, PP, THR>::step(xts);
-  const uint32_t q1 = Tile<T, NN, THR>::first(qts, a.N, tid), qby = Tile<T, NN, THR>::step(qts);
+  // bytes of a token's row, and the tile that fetch() will load next
+  const int kbytes = (int)a.k.ts * (int)sizeof(T), xbytes = (int)a.x.ts * (int)sizeof(T);
+  const int qbytes = MODE == kOutputs ? (int)a.q.ts * (int)sizeof(T) : 0;
+  const uint32_t k1 = Tile<T, NN, THR>::first(a.k.ts, a.N, tid), kby = Tile<T, NN, THR>::step(a.k.ts);
+  const uint32_t x1 = Tile<T, PP, THR>::first(a.x.ts, a.P, tid), xby = Tile<T, PP, THR>::step(a.x.ts);
+  const uint32_t q1 = Tile<T, NN, THR>::first(a.q.ts, a.N, tid), qby = Tile<T, NN, THR>::step(a.q.ts);
+  const int first_tile = REV ? M - 1 - i0 : i0, ahead = REV ? -1 : 1;
+  const char* knext = reinterpret_cast<const char*>(kp + (long long)first_tile * Q * a.k.ts);
+  const char* xnext = reinterpret_cast<const char*>(xp + (long long)first_tile * Q * a.x.ts);
+  const char* qnext = reinterpret_cast<const char*>(qp) + (long long)first_tile * Q * qbytes;
+  const Step* tnext = tab + (long long)first_tile * Q;
   // no branches here: a wait after one would be for every load in flight
   auto fetch = [&](int i) {
-    const int t0 = (REV ? M - 1 - i : i) * Q, rows = min(Q, a.n - t0);
-    st = tab[t0 + (tid & (Q - 1))];
-    tk.load(kp + t0 * kts, rows, kts, a.N, k1, kby);
-    tx.load(xp + t0 * xts, rows, xts, a.P, x1, xby);
-    if (MODE == kOutputs) tq.load(qp + t0 * qts, rows, qts, a.N, q1, qby);
+    const int rows = min(Q, a.n - (REV ? M - 1 - i : i) * Q);
+    st = tnext[tid & (Q - 1)];
+    tk.load(knext, rows, kbytes, a.N, k1, kby);
+    tx.load(xnext, rows, xbytes, a.P, x1, xby);
+    if (MODE == kOutputs) tq.load(qnext, rows, qbytes, a.N, q1, qby);
+    knext += ahead * (long long)(Q * kbytes);
+    xnext += ahead * (long long)(Q * xbytes);
+    qnext += Q * qbytes;
+    tnext += ahead * Q;
   };
   fetch(i0);
   if (MODE == kOutputs) {
     // as many stores (dropped: an empty resource) as a tile has, so that the
     // loop's waits for its loads count the stores behind them on every path and need not drain them
-    const rsrc_t none = rows_rsrc(yp, 0);
+    const rsrc_t none = tile_rsrc(yp, 0);
 #pragma unroll
     for (int e = 0; e < TB * CB; ++e) {
       if constexpr (NX == 1) {
@@ -306,6 +317,13 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
         weigh(ta, sa, x0);
         weigh(ta, sa + 1, x1);
         weigh(tb, sb, x2);
+      } else if constexpr (TB == 4 && NW == 8) {
+        // eight waves: the blocks of w's parity of the 16 tokens w / 2
+        const int tb = w / 2, sb = w & 1;
+        bf16x8 cf[KN][NX];
+        rows_of(tb, cf);
+        weigh(tb, sb, product(sb, cf));
+        if (tb >= 2) weigh(tb, sb + 2, product(sb + 2, cf));
       } else {
         constexpr int WPT = NW > TB ? NW / TB : 1;
         bf16x8 cf[KN][NX];
@@ -350,7 +368,8 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) load_frags_tr<NX>(S.x, PX, LDX, pw + 16 * cb, 32 * ks, l, xf[ks][cb]);
-      const rsrc_t yr = rows_rsrc(yp + (long long)t0 * a.H * a.P, (long long)min(Q, a.n - t0) * a.H * a.P * sizeof(T));
+      const rsrc_t yr = tile_rsrc(yp, min(Q, a.n - t0) * ybytes);
+      yp += Q * ybytes;
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb) {
 #pragma unroll
@@ -408,28 +427,26 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     // h <- 2^Ltile h + sum_s k_s (w_s x_s)^T
     const float Ltile = S.Lh[Q - 1] + S.Ll[Q - 1], dec = exp2_(Ltile);
     segL += Ltile;
-    bf16x8 u[KS][CB][NU];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 u[CB][NU];
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) scaled<NX, NU>(xf[ks][cb], S.w + 32 * ks + 8 * g, u[ks][cb]);
+      for (int cb = 0; cb < CB; ++cb) scaled<NX, NU>(xf[ks][cb], S.w + 32 * ks + 8 * g, u[cb]);
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) h[nb][cb] *= dec;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
+      for (int nb = 0; nb < NB; ++nb) {
         bf16x8 bt[NX];
         load_frags_tr<NX>(S.k, PK, LDK, 16 * nb, 32 * ks, l, bt);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
+          if (ks == 0) h[nb][cb] *= dec;
           if constexpr (transposed(MODE))
-            mma_pieces<NU, NX>(u[ks][cb], bt, h[nb][cb]);
+            mma_pieces<NU, NX>(u[cb], bt, h[nb][cb]);
           else
-            mma_pieces<NX, NU>(bt, u[ks][cb], h[nb][cb]);
+            mma_pieces<NX, NU>(bt, u[cb], h[nb][cb]);
         }
       }
     }
+    if constexpr (NX == 1) interleave<KS * NB * CB * NU, 3>();
     if (flagged) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
