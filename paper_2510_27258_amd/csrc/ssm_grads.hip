@@ -135,7 +135,10 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   const uint32_t x1 = TP::first(a.x.ts, a.P, tid), xby = TP::step(a.x.ts);
   const uint32_t y1 = TP::first(a.dy.ts, a.P, tid), yby = TP::step(a.dy.ts);
   Step st{};
+  float An = 0.f, Dn = 0.f;
   auto fetch = [&](int head) {
+    An = a.A[head];
+    Dn = (a.D ? a.D : a.A)[head];
     tx.load(reinterpret_cast<const bf16*>(xp + (long long)head * a.P), rows, (int)a.x.ts * 2, a.P, x1, xby);
     ty.load(reinterpret_cast<const bf16*>(yp + (long long)head * a.P), rows, (int)a.dy.ts * 2, a.P, y1, yby);
     st = a.tab[((size_t)b * a.H + head) * a.tok + t0 + (tid & (kGQ - 1))];
@@ -160,6 +163,8 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
       for (int i = 0; i < 2; ++i) v[k][i] = __builtin_bit_cast(f32x4, load16(rs, off + 16 * i));
     }
   };
+  // the tile's rows of dx: the tokens past the sequence lie past the end
+  const rsrc_t dxr = tile_rsrc(static_cast<uint16_t*>(a.dx) + ((size_t)b * a.n + t0) * a.H * a.P, rows * a.H * a.P * 2);
   fetch(head0);
   if (kAhead) {
     rows_of(a.h0, head0, hv);
@@ -189,6 +194,7 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
 #pragma unroll 1
   for (int hh = 0; hh < heads; ++hh) {
     const int head = head0 + hh, bh = b * a.H + head;
+    const float Ah = An, Dh = a.D ? Dn : 0.f;
     const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
     tx.template store<false>(S.x, tid);
     ty.template store<false>(S.dy, tid);
@@ -345,7 +351,6 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
     // dx^T for the wave's columns p and token blocks
     {
       const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
-      const float Dh = a.D ? a.D[head] : 0.f;
       f32x4 acc[PT];
 #pragma unroll
       for (int j = 0; j < PT; ++j) acc[j] = zero4();
@@ -373,11 +378,9 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         const float dts = S.dt[s];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = dts * acc[j][e] + Dh * v[e];
-        if (s < rows && c < a.P) {
-          uint2 o[1];
-          pieces4<1>(v, o);
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dx) + (((size_t)b * a.n + t0 + s) * a.H + head) * a.P + c) = o[0];
-        }
+        uint2 o[1];
+        pieces4<1>(v, o);
+        store8(dxr, c < a.P ? (uint32_t)((s * a.H + head) * a.P + c) * 2 : 0x80000000u, o[0]);
       }
     }
     // the gradients of dt and the per-head parameters: one wave, a token a lane
@@ -399,7 +402,7 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
       const double back = (double)R - (double)dt * K + Et, ahead = (double)dt * Fs;
       const double upto = sums_to(back), suf = last_lane(upto) - upto + back, pre = sums_to(ahead) - ahead;
       const double da = suf + pre + (double)exp2_(Lend) * hg;
-      double d = (double)a.A[head] * da + ((double)K + S.own[l] + Fs);
+      double d = (double)Ah * da + ((double)K + S.own[l] + Fs);
       if (a.softplus) d *= -expm1f(-dt);
       if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, (float)d);
       const float dA = (float)last_lane(sums_to(l < rows ? dt * da : 0.0)), db = (float)last_lane(sums_to(l < rows ? d : 0.0));

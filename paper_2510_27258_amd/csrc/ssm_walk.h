@@ -143,21 +143,6 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     tnext += ahead * Q;
   };
   fetch(i0);
-  if (MODE == kOutputs) {
-    // as many stores (dropped: an empty resource) as a tile has, so that the
-    // loop's waits for its loads count the stores behind them on every path and need not drain them
-    const rsrc_t none = tile_rsrc(yp, 0);
-#pragma unroll
-    for (int e = 0; e < TB * CB; ++e) {
-      if constexpr (NX == 1) {
-        store8(none, 0, make_uint2(0, 0));
-      } else {
-        const float z[4] = {0.f, 0.f, 0.f, 0.f};
-        store16(none, 0, z);
-      }
-    }
-  }
-
   f32x4 h[NB][CB];
   // the [N][P] record of a head
   auto load_state = [&](const float* p) {
@@ -233,6 +218,10 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
 
   const float Dh = MODE == kOutputs && a.D ? a.D[head] : 0.f;
   float segL = 0.f;
+  // Everything loaded so far is here: were the state's loads still open where
+  // the loop begins, the wait before their first use in it would, on every
+  // turn, be one for the tile on its way.
+  __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
   for (int i = i0; i < i1; ++i) {
     const int tile = REV ? M - 1 - i : i, t0 = tile * Q, par = i & 1;
     const int tid = opaque(threadIdx.x), l = tid & 63, r = l & 15, g = l >> 4;
@@ -264,13 +253,14 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
     if (i + 1 < i1) fetch(i + 1);
 
     if (MODE == kStates) {
-      float* to = a.carry + ((size_t)bh * M + tile) * a.N * a.P;
+      const rsrc_t to = tile_rsrc(a.carry + ((size_t)bh * M + tile) * a.N * a.P, a.N * a.P * 4);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          const int n = 16 * nb + r, c = pw + 16 * cb + 4 * g;
-          if (n < a.N && c < a.P) *reinterpret_cast<f32x4*>(to + n * a.P + c) = h[nb][cb];
+          const int c = pw + 16 * cb + 4 * g;                    // rows past N lie past the end
+          const float v[4] = {h[nb][cb][0], h[nb][cb][1], h[nb][cb][2], h[nb][cb][3]};
+          store16(to, c < a.P ? (uint32_t)((16 * nb + r) * a.P + c) * 4 : 0x80000000u, v);
         }
     }
 
