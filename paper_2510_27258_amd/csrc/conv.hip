@@ -13,7 +13,6 @@
 // computed.  Sums are fp32, rounded once on the store.
 #include "common.h"
 #include "mixer.h"
-#include "profile.h"
 #include "vec.h"
 
 namespace hla {

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "profile.h"
+
 namespace hla {
 
 // Row-strided view of a [B, n, ...] tensor: elements between batches and tokens.
@@ -66,4 +68,10 @@ hipError_t launch_ssm_step(const Ssm& a, hipStream_t s);
 size_t ssm_backward_ws(int B, int n, int H, int P, int G, int N);
 hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s);
 
+// One kernel as a bracket of its own; its launch status.
+#define HLA_TIMED(name, kernel, grid, block, lds, stream, ...)       \
+  HLA_PROF(name, stream, [&]() {                                     \
+    HLA_LAUNCH(kernel, grid, block, lds, stream, __VA_ARGS__);       \
+    return hipGetLastError();                                        \
+  }())
 }  // namespace hla

@@ -24,10 +24,4 @@ hipError_t prof_launch(const void* fn, dim3 grid, dim3 block, void** args, size_
     else                                                                                           \
       hipLaunchKernelGGL(kernel, grid, block, lds, stream, __VA_ARGS__);                           \
   } while (0)
-// One kernel as a bracket of its own; its launch status.
-#define HLA_TIMED(name, kernel, grid, block, lds, stream, ...)       \
-  HLA_PROF(name, stream, [&]() {                                     \
-    HLA_LAUNCH(kernel, grid, block, lds, stream, __VA_ARGS__);       \
-    return hipGetLastError();                                        \
-  }())
 }  // namespace hla

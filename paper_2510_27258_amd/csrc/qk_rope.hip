@@ -17,7 +17,6 @@
 // a head) are contiguous; queries and keys share the launch.
 #include "common.h"
 #include "mixer.h"
-#include "profile.h"
 #include "vec.h"
 
 namespace hla {

@@ -8,7 +8,6 @@
 // the rows' sums meet in LDS in a fixed order.
 #include "common.h"
 #include "mixer.h"
-#include "profile.h"
 #include "vec.h"
 
 namespace hla {

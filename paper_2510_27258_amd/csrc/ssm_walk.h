@@ -1,7 +1,6 @@
 // The tile walk of the selective state space scan (ssm_scan.hip has the
 // mathematics and the plan), shared by the outputs and the gradients' states.
 #pragma once
-#include "profile.h"
 #include "ssm_tiles.h"
 
 namespace hla {
