@@ -49,48 +49,6 @@ struct GradLds {
   float R[kGW][kGQ], own[kGQ], K[kGW][kGQ], E[kGW][kGQ], F[kGW][kGQ], one[kGW][2];
 };
 
-// Sums across lanes without the LDS unit.  A swap of halves (rows 0 1 with 2 3,
-// or 0 with 1 and 2 with 3) of a value with itself leaves both halves' sum in
-// the two results' sum, in every lane.
-__device__ __forceinline__ float sum_groups(float v) {        // over the four rows of 16 lanes
-  auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
-  h = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(h[0]) + __uint_as_float(h[1]);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float dpp(float v) {               // 0 where the lane has no source
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xf, false));
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double dpp(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// over the 16 lanes of a row, in every one of them (rotations by 8, 4, 2, 1)
-__device__ __forceinline__ float sum_row(float v) {
-  v += dpp<0x128, 0xf>(v);
-  v += dpp<0x124, 0xf>(v);
-  v += dpp<0x122, 0xf>(v);
-  return v + dpp<0x121, 0xf>(v);
-}
-__device__ __forceinline__ float sum_wave(float v) { return sum_groups(sum_row(v)); }
-// sums over the lanes up to and with this one: shifts by 1, 2, 4, 8 in a row, then a row's last lane to the rows behind
-__device__ __forceinline__ double sums_to(double v) {
-  v += dpp<0x111, 0xf>(v);
-  v += dpp<0x112, 0xf>(v);
-  v += dpp<0x114, 0xf>(v);
-  v += dpp<0x118, 0xf>(v);
-  v += dpp<0x142, 0xa>(v);
-  return v + dpp<0x143, 0xc>(v);
-}
-__device__ __forceinline__ double last_lane(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
 __device__ __forceinline__ void unpack4(const uint2& u, float (&v)[4]) {
   v[0] = __uint_as_float(u.x << 16);
   v[1] = __uint_as_float(u.x & 0xffff0000u);

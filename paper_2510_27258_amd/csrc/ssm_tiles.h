@@ -88,6 +88,52 @@ __device__ __forceinline__ void mma_pieces(const bf16x8 (&a)[NA], const bf16x8 (
       if (s - i >= 0 && s - i < NB) c = mma(a[i], b[s - i], c);
 }
 
+// Sums across lanes without the LDS unit.  A swap of halves (rows 0 1 with 2 3,
+// or 0 with 1 and 2 with 3) of a value with itself leaves both halves' sum in
+// the two results' sum, in every lane.
+__device__ __forceinline__ float sum_groups(float v) {        // over the four rows of 16 lanes
+  auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  h = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(h[0]) + __uint_as_float(h[1]);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float v) {               // 0 where the lane has no source
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// over the 16 lanes of a row, in every one of them (rotations by 8, 4, 2, 1)
+__device__ __forceinline__ float sum_row(float v) {
+  v += dpp<0x128, 0xf>(v);
+  v += dpp<0x124, 0xf>(v);
+  v += dpp<0x122, 0xf>(v);
+  return v + dpp<0x121, 0xf>(v);
+}
+__device__ __forceinline__ float sum_wave(float v) { return sum_groups(sum_row(v)); }
+// sums over the lanes up to and with this one: shifts by 1, 2, 4, 8 in a row, then a row's last lane to the rows behind
+template <int LANES = 64>                                     // or within each 32
+__device__ __forceinline__ double sums_to(double v) {
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);
+  if (LANES == 64) v += dpp<0x143, 0xc>(v);
+  return v;
+}
+template <int LANE = 63>
+__device__ __forceinline__ double last_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, LANE);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), LANE);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 // Eight values in NP pieces, round to nearest.
 template <int NP>
 __device__ __forceinline__ void pieces8(const float (&v)[8], bf16x8 (&p)[NP]) {

@@ -506,13 +506,9 @@ __global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab
     if (a.softplus) dt = dt > 20.f ? dt : log1pf(expf(dt));
     la = (double)dt * (double)a.A[head] * 1.4426950408889634;
   }
-  double L = la;
-#pragma unroll
-  for (int m = 1; m < Q; m *= 2) {
-    const double o = __shfl_up(L, m, Q);
-    if ((lane & (Q - 1)) >= m) L += o;
-  }
-  const double end = __shfl(L, Q - 1, Q);
+  const double L = sums_to<Q>(la);
+  double end = last_lane(L);
+  if (Q == 32 && lane < 32) end = last_lane<31>(L);
   Step s;
   s.Lh = (float)L;
   s.Ll = (float)(L - (double)s.Lh);

@@ -506,6 +506,24 @@ def test_another_stream_and_a_captured_graph():
             assert all(torch.equal(a, b) for a, b in zip(held, want)), name
 
 
+def test_a_captured_graph_of_the_widest_scan():
+    """P = N = 128 takes more than 64 KB of LDS a workgroup, which a launch has to ask for."""
+    s, state, dy = _ssm_case(1, 300, 2, 128, 128, 1, BF16, 26)
+    for f in (lambda: [hla.ssm_forward(*s)], lambda: hla.ssm_backward(*s, dy), lambda: [hla.ssm_prefill(state.clone(), *s)]):
+        want = [x.clone() for x in f()]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = f()
+        for _ in range(3):
+            for x in held:
+                x.fill_(7)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
 def test_autograd_ops_give_the_kernels_gradients():
     c, _ = _conv_case(2, 50, 24, 3, BF16, True, 23)
     leaves = [t.clone().requires_grad_() for t in c[:3]]
