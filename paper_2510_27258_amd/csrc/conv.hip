@@ -11,6 +11,12 @@
 // rather than 16 bytes: half the registers a thread, so that twice the waves
 // hide the loads.  A chunk of rows loads while the one before it is
 // computed.  Sums are fp32, rounded once on the store.
+// Measured on 8000 x 4352 in bf16 with bias and SiLU (139 MB): 28.7 us, 4.8
+// TB/s; one token for 64 sequences 4.3 us, the same with one channel a thread
+// (latency).  Forward 18.5 us and gradients 36 us (126 MB, 3.5 TB/s; 86 as
+// 16-byte threads without loads ahead) over 4 x 4096 x 1280, the sums over the
+// blocks 4 us.  Calls with one channel a thread instead of four: the first 36
+// us instead of 29.5, the last with its gradients 78 instead of 59.
 #include "common.h"
 #include "mixer.h"
 #include "vec.h"

@@ -21,6 +21,11 @@
 // heads.  h and g are kept and enter their products to 24 bits (three pieces):
 // dA and d dt_bias are sums of either sign over every token, and with two
 // pieces (2^-17) they were 2.6e-6 off 64 bits instead of 1.8e-6, for 1 % of the time.
+//
+// Measured on 4 x 4096 tokens of 16 heads of 64 x 128 (us): the walks both ways
+// to the segments' ends 33, their states 89 (268 MB written, 3.0 TB/s), this
+// kernel 113 (268 MB of states read; with four waves a workgroup of two row
+// blocks each, before its loads were moved ahead, 253), the last sums 5.
 #include "ssm_walk.h"
 
 namespace hla {
@@ -490,10 +495,14 @@ hipError_t grads_n(const GradArgs& a, hipStream_t s) {
   return grads<PP, 128>(a, s);
 }
 
-// Head subsets a group: workgroups for two a CU, each of at least one head.
+// Head subsets a group: as many as keep all workgroups in one round, one a CU
+// (its registers).  This kernel with subsets and without (us): 35 and 102 for
+// 3864 tokens of 16 heads of 64 x 128, 17 and 54 for 2 x 517 of 8; the sums over
+// the subsets add 0.3 and 1.5.  Calls: with two workgroups a CU as the aim 336,
+// with one 317 (4 x 4096 of 16); 158 workgroups in two subsets 262, in one 248.
 int head_subsets(int B, int tiles, int G, int share) {
   const long long wgs = (long long)B * tiles * G;
-  long long hs = wgs >= 512 ? 1 : (512 + wgs - 1) / wgs;
+  long long hs = wgs >= 256 ? 1 : 256 / wgs;
   if (hs > share) hs = share;
   const int per = (int)((share + hs - 1) / hs);
   return (share + per - 1) / per;
@@ -501,7 +510,7 @@ int head_subsets(int B, int tiles, int G, int share) {
 
 struct GradWs {
   Step* tab;
-  float *tot, *par, *ends[2], *segdec[2], *carry[2], *bc[2];
+  float *par, *ends[2], *segdec[2], *carry[2], *bc[2];
   size_t bytes;
 };
 GradWs carve(void* ws, int B, int n, int H, int P, int G, int N) {
@@ -517,7 +526,6 @@ GradWs carve(void* ws, int B, int n, int H, int P, int G, int N) {
     return q;
   };
   r.tab = reinterpret_cast<Step*>(take(4 * tok * BH));
-  r.tot = take((size_t)p.tiles * BH);
   r.par = take((size_t)p.tiles * BH * 3);
   const int hs = head_subsets(B, p.tiles, G, H / G);
   for (int i = 0; i < 2; ++i) {
@@ -536,7 +544,7 @@ size_t ssm_backward_ws(int B, int n, int H, int P, int G, int N) { return carve(
 
 hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {
   const GradWs c = carve(ws, a.B, a.n, a.H, a.P, a.G, a.N);
-  hipError_t e = launch_steps(a, c.tab, c.tot, kGQ, s);
+  hipError_t e = launch_steps(a, c.tab, kGQ, s);
   if (e != hipSuccess) return e;
   WalkPair pair{};
   for (int i = 0; i < 2; ++i) {

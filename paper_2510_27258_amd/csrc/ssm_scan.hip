@@ -11,6 +11,20 @@
 // state, the decayed sum of the earlier ends (Fig. 1C's two levels with a
 // scalar decay).  The state stays in MFMA accumulators for the whole walk;
 // k_ssm_steps makes each token's dt, L and weights once for all walks.
+//
+// Measured in bf16 (us): 2 x 16384 tokens of 32 heads of 128 x 128 335: ends 94
+// (seven of eight segments), outputs 246, steps 11, sums of the ends 10.  A
+// prompt of 8000 tokens of 32 heads 123: ends 36, outputs 75, sums 13, steps 6.
+// Floors by bytes: 108 and 27.
+// What bounds it: no one unit.  The outputs' walk of the first keeps vector
+// instructions busy 52 % of the time, LDS 61 % (42 % of that conflicts) and the
+// matrix cores 26 %; waves wait for memory or barriers 48 % of theirs.  In
+// copies of a somewhat slower version (276 us) without loads and stores it took
+// 212, without the products 197, without both 107 (staging, weights, barriers):
+// two workgroups a CU overlap these only in part.
+// Tried and not kept, on the first: half as many waves with twice the columns
+// 361 (against 347-353), two tiles of loads ahead for the shorter walks 340
+// (340), the update at a higher wave priority 326-340 (332-350).
 #include "ssm_walk.h"
 #include "profile.h"
 
@@ -25,7 +39,7 @@ bool ssm_sizes_ok(int P, int N) { return P >= 16 && P <= 128 && P % 16 == 0 && N
 
 struct SsmWs {
   Step* tab;
-  float *tot, *ends, *segdec;
+  float *ends, *segdec;
   size_t bytes;
 };
 static SsmWs carve(void* ws, int BH, int n, int P, int N, int Q) {
@@ -36,8 +50,6 @@ static SsmWs carve(void* ws, int BH, int n, int P, int N, int Q) {
   size_t o = 0;
   r.tab = reinterpret_cast<Step*>(c + o);
   o += align256(sizeof(Step) * tok * BH);
-  r.tot = reinterpret_cast<float*>(c + o);
-  o += align256(sizeof(float) * (size_t)p.tiles * BH);
   r.segdec = reinterpret_cast<float*>(c + o);
   o += align256(sizeof(float) * (size_t)p.segs * BH);
   r.ends = reinterpret_cast<float*>(c + o);
@@ -54,7 +66,7 @@ template <typename T, int NU>
 static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
   constexpr int Q = Kind<T>::Q;
   const SsmWs c = carve(ws, a.B * a.H, a.n, a.P, a.N, Q);
-  hipError_t e = launch_steps(a, c.tab, c.tot, Q, s);
+  hipError_t e = launch_steps(a, c.tab, Q, s);
   if (e != hipSuccess) return e;
   WalkPair pair{};
   WalkArgs& w = pair.a[0];
@@ -67,7 +79,8 @@ static hipError_t forward(const Ssm& a, void* ws, hipStream_t s) {
 }
 
 // The scaled inputs go into the state in three pieces where the state is an
-// output (24 bits: fp32's), in two where only bf16 outputs read it.
+// output (24 bits: fp32's), in two where only bf16 outputs read it: 323 us for
+// 2 x 16384 tokens of 32 heads of 128 x 128, with three pieces 359.
 hipError_t launch_ssm_forward(const Ssm& a, void* ws, hipStream_t s) {
   if (a.dtype != 1) return forward<float, 3>(a, ws, s);
   return a.state ? forward<bf16, 3>(a, ws, s) : forward<bf16, 2>(a, ws, s);

@@ -5,7 +5,10 @@
 // Bound by the state's bytes: each fp32 element is read once and written once.
 // A workgroup takes a head; a thread holds 16-byte pieces of every RG-th row
 // of [N][P], all of them loading before the token's vectors are needed, and
-// the rows' sums meet in LDS in a fixed order.
+// the rows' sums meet in LDS in a fixed order.  The stores are non-temporal
+// (the state is not read again within the step).
+// Measured: 64 sequences of 32 heads of 128 x 128 (269 MB) 45 us, 6.0 TB/s,
+// more than a copy of 1 GiB reaches (5.1): the last-level cache may hold part.
 #include "common.h"
 #include "mixer.h"
 #include "vec.h"

@@ -53,8 +53,12 @@ struct WalkLds {
 };
 
 // ends[s] += decay ends[s - 1], s = 1 .. segs - 2: the state after each segment.
-// Beyond kOwnSums earlier segments (the sum is then longer than a launch), so
-// that no walk reads more than one.  V: float4s a slot.
+// Beyond kOwnSums earlier segments, so that no walk reads more than one; V:
+// float4s a slot.  Each walk summing for itself costs the reads of all earlier
+// ends.  A call with this launch against one without (us): 111 and 141 with 16
+// segments of 32 heads of 128 x 128, 323 and 326 with 8 of 64; at 8 of 64 heads
+// of 64 x 128 337 and 331, 36 and 35 with 16 of 8 fp32 heads of 64 x 64: the
+// gain where the ends are large is worth the loss where they are small.
 constexpr int kOwnSums = 3;
 __global__ __launch_bounds__(256) void k_ssm_carry(WalkPair pair, int V) {
   const WalkArgs& a = pair.a[blockIdx.z];
@@ -491,9 +495,10 @@ hipError_t walk_pn(const WalkPair& a, int count, int B, hipStream_t s) {
 
 // A wave: 64 tokens of one (sequence, head).  Sums in fp64: L reaches the
 // hundreds, where fp32 sums would put 1e-5 into the weights of neighbours.
+// Measured: 11 us for 2 x 16384 tokens of 32 heads (16.8 MB written), 5.6 for
+// 8000 tokens of 32: bound by latency, a wave does one block of 64.
 template <int Q>
-__global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab, float* __restrict__ tot, int tok,
-                                                   int tiles) {
+__global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab, int tok) {
   const int wv = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
   const int head = wv % a.H, blk = (wv / a.H) % (tok / 64), b = wv / a.H / (tok / 64);
   if (b >= a.B) return;
@@ -515,12 +520,13 @@ __global__ __launch_bounds__(256) void k_ssm_steps(Ssm a, Step* __restrict__ tab
   s.dt = dt;
   s.w = dt * exp2_((float)(end - L));
   tab[(size_t)bh * tok + t] = s;
-  if ((lane & (Q - 1)) == Q - 1 && t / Q < tiles) tot[(size_t)bh * tiles + t / Q] = (float)end;
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Segments a head: walks for two workgroups a CU, each of at least four tiles.
+// 256, 512, 768 and 1024 workgroups (us): 415, 342, 377 and 363 on 2 x 16384
+// tokens of 32 heads of 128 x 128; 127, 114, 134 and 141 on 8000 tokens.
 inline SsmPlan ssm_plan(int BH, int n, int Q) {
   SsmPlan p;
   p.tiles = (n + Q - 1) / Q;
@@ -532,12 +538,12 @@ inline SsmPlan ssm_plan(int BH, int n, int Q) {
   return p;
 }
 
-inline hipError_t launch_steps(const Ssm& a, Step* tab, float* tot, int Q, hipStream_t s) {
-  const int tok = (a.n + 63) / 64 * 64, tiles = (a.n + Q - 1) / Q;
+inline hipError_t launch_steps(const Ssm& a, Step* tab, int Q, hipStream_t s) {
+  const int tok = (a.n + 63) / 64 * 64;
   const long long waves = (long long)a.B * a.H * (tok / 64);
   const dim3 grid((unsigned)((waves + 3) / 4));
-  if (Q == 64) return HLA_TIMED("ssm_steps", k_ssm_steps<64>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
-  return HLA_TIMED("ssm_steps", k_ssm_steps<32>, grid, dim3(256), 0, s, a, tab, tot, tok, tiles);
+  if (Q == 64) return HLA_TIMED("ssm_steps", k_ssm_steps<64>, grid, dim3(256), 0, s, a, tab, tok);
+  return HLA_TIMED("ssm_steps", k_ssm_steps<32>, grid, dim3(256), 0, s, a, tab, tok);
 }
 
 constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }

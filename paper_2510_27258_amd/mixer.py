@@ -60,7 +60,8 @@ def _on_gpu(t):
         raise ValueError("tensors must be on the GPU")
 
 
-# the device and stream of the calling thread, without torch.cuda's wrappers: they cost a decode call more than its kernel
+# the device and stream of the calling thread, without torch.cuda's wrappers, which cost a
+# decode call more than its kernel
 _device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
