@@ -290,8 +290,8 @@ __global__ __launch_bounds__(Waves<PP>::THR, sizeof(T) == 2 ? (PP == 128 ? 4 : 2
       auto weigh = [&](int tb, int sb, const f32x4& acc) {
         const int t = 16 * tb + r, s0 = 16 * sb + 4 * g;
         const f32x4 lh = *reinterpret_cast<const f32x4*>(S.Lh + s0), dd = *reinterpret_cast<const f32x4*>(S.dt + s0);
-        f32x4 d = S.Lh[t] - lh;
-        if (NX == 3) d += S.Ll[t] - *reinterpret_cast<const f32x4*>(S.Ll + s0);
+        // both parts for every type: behind one very large step the high parts alone are 2^-24 of L apart
+        const f32x4 d = (S.Lh[t] - lh) + (S.Ll[t] - *reinterpret_cast<const f32x4*>(S.Ll + s0));
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = s0 + e <= t ? acc[e] * (exp2_(d[e]) * dd[e]) : 0.f;
