@@ -27,7 +27,16 @@ namespace {
 constexpr int kConvThreads = 256;
 constexpr int kConvBackRun = 16;   // tokens a thread of the gradients walks
 
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+// sigmoid(z) for values of type T.  fp32: within 2 * 2^-23 of itself.  bf16: by
+// the hardware's exponential and reciprocal, whose error, 2^-24 |z| and a
+// little more, is nothing beside the output's 2^-8.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float z) {
+  if constexpr (sizeof(T) == 2)
+    return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+  else
+    return 1.f / (1.f + expf(-z));
+}
 
 template <int V, int K>
 __device__ __forceinline__ void taps(const Conv& a, int c, float (&w)[K][V], float (&b)[V]) {
@@ -104,7 +113,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv(Conv a, int CV, int runs,
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) z[i] += w[j][i] * win[j][i];
         z[i] += w[K - 1][i] * x_t;
-        if (a.silu) z[i] *= sigmoid(z[i]);
+        if (a.silu) z[i] *= sigmoid<T>(z[i]);
 #pragma unroll
         for (int j = 0; j + 1 < K - 1; ++j) win[j][i] = win[j + 1][i];
         win[K - 2][i] = x_t;
@@ -187,7 +196,7 @@ __global__ __launch_bounds__(kConvThreads) void k_conv_back(Conv a, float* part)
             float z = bias[i];
 #pragma unroll
             for (int j = 0; j < K; ++j) z += w[j][i] * win[j][i];
-            const float s = sigmoid(z);
+            const float s = sigmoid<T>(z);
             d *= s * (1.f + z * (1.f - s));
           }
           dz[K - 1][i] = there ? d : 0.f;

@@ -27,3 +27,21 @@ def test_tokens_behind_a_very_large_step(dtype, big):
     first = state.clone()
     y = hla.ssm_prefill(state, *args, softplus=False)
     _check_scan(args, first, y, state, False)
+
+
+@pytest.mark.parametrize("K", [2, 4])
+def test_fp32_silu_is_fp32_accurate(K):
+    """A single tap of one, so that z is the input itself.  In units of 2^-23 of
+    a value exp is off by one, a sum, a quotient and a product by a half each:
+    s = 1 / (1 + exp(-z)) by 2 and y = z s by less than 4.  The slope s (1 + z
+    (1 - s)) has 4 of its terms for s and the last three roundings, and s's own
+    2, with half a rounding of 1 - s, times |z|."""
+    z = torch.linspace(-80, 80, 64 * 1024, device="cuda").view(1, 1024, 64).contiguous()
+    w = torch.zeros(64, K, device="cuda")
+    w[:, K - 1] = 1
+    zn = _n(z)
+    s = 1 / (1 + np.exp(-zn))
+    y = hla.conv_forward(z, w)
+    _within(y, zn * s, np.abs(zn * s), 4 * 2 ** -23, "y")
+    dx = hla.conv_backward(z, w, None, torch.ones_like(z))[0]
+    _within(dx, s * (1 + zn * (1 - s)), s * (4 * (1 + np.abs(zn) * (1 - s)) + 3 * np.abs(zn) * s), 2 ** -23, "dx")
