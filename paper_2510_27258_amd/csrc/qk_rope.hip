@@ -249,13 +249,14 @@ __global__ __launch_bounds__(kQkThreads) void k_qk_rope_back(QkRope a, int qbloc
         dot += u[i] * w[i] * in[k].at(i);
       }
       const float r = 1.f / sqrtf(row_sum<LP>(ss) / a.d + a.eps);
-      const float mean = row_sum<LP>(dot) / a.d * (r * r * r);
+      const float mean = row_sum<LP>(dot) / a.d * r;      // r^3 would overflow for rows below 1e-12
       if (there && k <= last) {
         float o[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          o[i] = r * (u[i] * w[i]) - in[k].at(i) * mean;
-          dw[i] += u[i] * (in[k].at(i) * r);
+          const float xhat = in[k].at(i) * r;
+          o[i] = r * (u[i] * w[i] - xhat * mean);
+          dw[i] += u[i] * xhat;
         }
         store_vec<T, V>(dx + (size_t)k * a.d, o);
       }

@@ -45,3 +45,21 @@ def test_fp32_silu_is_fp32_accurate(K):
     _within(y, zn * s, np.abs(zn * s), 4 * 2 ** -23, "y")
     dx = hla.conv_backward(z, w, None, torch.ones_like(z))[0]
     _within(dx, s * (1 + zn * (1 - s)), s * (4 * (1 + np.abs(zn) * (1 - s)) + 3 * np.abs(zn) * s), 2 ** -23, "dx")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_qk_gradients_of_tiny_rows_without_eps(dtype):
+    """Rows of 1e-14 with eps = 0: r is 1e14 and r^3 no fp32 number, dx is 1e14."""
+    q, k, qw, kw, cos, sin, pos, gq, gk = _qk_case(2, 9, 3, 2, 64, 64, dtype, 31)
+    q = (q.float() * 1e-14).to(dtype)
+    grads = hla.qk_norm_rope_backward(q, k, qw, kw, cos, sin, pos, gq, gk, 0.0)
+    c, s = (_n(t)[pos.cpu().numpy()] for t in (cos, sin))
+    xn, wn, gn = _n(q), _n(qw), _n(gq)
+    dx, dw = O.norm_rope_vjp(xn, wn, c, s, 0.0, False, gn)
+    inv = 1 / np.sqrt((xn * xn).mean(-1, keepdims=True))
+    size = 2 * inv * (np.abs(gn).max(-1) * np.abs(wn).max()).transpose(0, 2, 1)[..., None]
+    size = size * (1 + np.abs(xn * inv).max(-1, keepdims=True))
+    if dtype == BF16:
+        _within(grads[0], dx, np.abs(dx) + 1e-3 * size, 2 ** -8, "dx")
+    else:
+        _within(grads[0], dx, size, 1e-5, "dx")
