@@ -103,6 +103,13 @@ def _space(nbytes, device, workspace=None):
     return workspace, workspace.numel() * workspace.element_size()
 
 
+def _upstream(g):
+    """An upstream gradient as the kernels read it: contiguous and on a 16-byte
+    boundary, which autograd's views (slices of the gradient of a torch.cat)
+    need not be."""
+    return g.contiguous() if g.data_ptr() % 16 == 0 else g.clone(memory_format=torch.contiguous_format)
+
+
 # ----------------------------------------------------------------------------
 # Short causal convolution
 def _conv_args(x, weight, bias, rank):
@@ -276,7 +283,7 @@ class QKNormRope(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq_out, dk_out):
-        grads = qk_norm_rope_backward(*ctx.saved_tensors, dq_out.contiguous(), dk_out.contiguous(), *ctx.how)
+        grads = qk_norm_rope_backward(*ctx.saved_tensors, _upstream(dq_out), _upstream(dk_out), *ctx.how)
         return (*grads, None, None, None, None, None)
 
 
@@ -374,7 +381,7 @@ class SSMScan(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        return (*ssm_backward(*ctx.saved_tensors, dy.contiguous(), ctx.softplus), None)
+        return (*ssm_backward(*ctx.saved_tensors, _upstream(dy), ctx.softplus), None)
 
 
 def ssm_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus=True):

@@ -63,3 +63,24 @@ def test_qk_gradients_of_tiny_rows_without_eps(dtype):
         _within(grads[0], dx, np.abs(dx) + 1e-3 * size, 2 ** -8, "dx")
     else:
         _within(grads[0], dx, size, 1e-5, "dx")
+
+
+def test_upstream_gradients_at_any_address():
+    """The gradient of a slice of torch.cat is a contiguous view that starts
+    where the slice does, here two bytes behind a boundary."""
+    q = _qk_case(1, 20, 2, 2, 32, 32, BF16, 33)
+    args, _, dy = _ssm_case(1, 80, 2, 32, 32, 1, BF16, 34)
+    one = torch.ones(1, dtype=BF16, device="cuda")
+
+    def grads(leaves, outs, ups, shift):
+        flat = torch.cat([*([one] if shift else []), *(o.flatten() for o in outs)])
+        up = torch.cat([*([one] if shift else []), *(u.flatten() for u in ups)])
+        return torch.autograd.grad(flat, leaves, up)
+
+    leaves = [t.clone().requires_grad_() for t in q[:4]]
+    outs = hla.qk_norm_rope(*leaves, *q[4:7])
+    for a, b in zip(grads(leaves, hla.qk_norm_rope(*leaves, *q[4:7]), q[7:9], True), grads(leaves, outs, q[7:9], False)):
+        assert torch.equal(a, b)
+    leaves = [t.clone().requires_grad_() for t in args]
+    for a, b in zip(grads(leaves, [hla.ssm_scan(*leaves)], [dy], True), grads(leaves, [hla.ssm_scan(*leaves)], [dy], False)):
+        assert torch.equal(a, b)
