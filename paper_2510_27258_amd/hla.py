@@ -258,6 +258,8 @@ class HLA2(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g):
         q, k, v = ctx.saved_tensors
+        if g.data_ptr() % 16:                 # a contiguous view of autograd's may start anywhere
+            g = g.clone(memory_format=torch.contiguous_format)
         return (*_backward(q, k, v, g, ctx.chunk, None, q.dtype), None)
 
 

@@ -84,3 +84,16 @@ def test_upstream_gradients_at_any_address():
     leaves = [t.clone().requires_grad_() for t in args]
     for a, b in zip(grads(leaves, [hla.ssm_scan(*leaves)], [dy], True), grads(leaves, [hla.ssm_scan(*leaves)], [dy], False)):
         assert torch.equal(a, b)
+
+
+def test_attentions_upstream_gradient_at_any_address():
+    """The same for the second-order attention, whose output is fp32."""
+    g = torch.Generator("cuda").manual_seed(2)
+    q, k, v = (torch.randn(1, 2, 100, 64, generator=g, device="cuda").mul(0.1).to(BF16).requires_grad_() for _ in range(3))
+    up = torch.randn(1, 2, 100, 64, generator=g, device="cuda")
+    out = hla.hla2_attention(q, k, v)
+    want = torch.autograd.grad(out, (q, k, v), up)
+    flat = torch.cat([torch.zeros(1, device="cuda"), hla.hla2_attention(q, k, v).flatten()])
+    got = torch.autograd.grad(flat, (q, k, v), torch.cat([torch.zeros(1, device="cuda"), up.flatten()]))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
