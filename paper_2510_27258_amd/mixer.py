@@ -8,6 +8,7 @@ batches and tokens, such as slices of a projection's output; outputs are new
 contiguous tensors.
 """
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 from . import capi
 
@@ -83,6 +84,11 @@ def _launch(entry, t, *args):
 
 
 def _learns(*tensors):
+    """Whether a call has to go through its autograd function: an input has a
+    graph, or may have a tangent (inside a forward-mode level), which that
+    function refuses."""
+    if getattr(_forward_ad, "_current_level", 0) >= 0:
+        return True
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 

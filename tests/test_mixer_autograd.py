@@ -1,0 +1,70 @@
+"""What automatic differentiation may and may not do with the differentiable
+operators, without a GPU: the launches are stubbed, so the values mean nothing;
+whether derivatives are taken or refused does."""
+import pytest
+import torch
+import torch.autograd.forward_ad as fwd
+
+from paper_2510_27258_amd import mixer
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def stubbed(monkeypatch):
+    launched = []
+
+    def launch(entry, t, *args):
+        launched.append(entry.__name__)
+    monkeypatch.setattr(mixer, "_launch", launch)
+    monkeypatch.setattr(mixer, "_on_gpu", lambda t: None)
+    return launched
+
+
+def _calls(dtype=BF16):
+    """name: (operator of its learned tensors, those tensors)."""
+    z = lambda *s, t=dtype: torch.zeros(*s, dtype=t)  # noqa: E731
+    f = torch.float32
+    return {
+        "conv": (lambda x, w, b: mixer.short_conv(x, w, b), [z(2, 8, 16), z(16, 4), z(16)]),
+        "qk": (lambda *a: torch.cat([o.flatten() for o in mixer.qk_norm_rope(*a)]),
+               [z(2, 8, 4, 64), z(2, 8, 2, 64), z(64), z(64)]),
+        "scan": (lambda *a: mixer.ssm_scan(*a),
+                 [z(2, 8, 4, 16), z(2, 8, 4), z(4, t=f), z(2, 8, 2, 16), z(2, 8, 2, 16), z(4, t=f), z(4, t=f)]),
+    }
+
+
+NAMES = sorted(_calls())
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_forward_mode_is_refused(name):
+    """No operator has a forward-mode formula: a dual input raises, whichever
+    it is, and never loses its tangent silently."""
+    op, args = _calls()[name]
+    for i in range(len(args)):
+        with fwd.dual_level():
+            dual = [fwd.make_dual(a, torch.ones_like(a)) if j == i else a for j, a in enumerate(args)]
+            with pytest.raises(NotImplementedError):
+                op(*dual)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_function_transforms_are_refused(name):
+    op, args = _calls()[name]
+    with pytest.raises((RuntimeError, NotImplementedError)):
+        torch.func.jvp(op, tuple(args), tuple(torch.ones_like(a) for a in args))
+    with pytest.raises((RuntimeError, NotImplementedError)):
+        torch.func.grad(lambda *a: op(*a).sum())(*args)
+    with pytest.raises((RuntimeError, NotImplementedError)):
+        torch.vmap(op)(*(a[None] for a in args))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_no_graph_without_a_learned_input(name, stubbed):
+    op, args = _calls()[name]
+    assert not op(*args).requires_grad and len(stubbed) == 1
+    args[0].requires_grad_()
+    assert op(*args).requires_grad
+    with torch.no_grad():
+        assert not op(*args).requires_grad
