@@ -11,6 +11,7 @@ import torch
 import torch.autograd.forward_ad as _forward_ad
 
 from . import capi
+from .autograd import once
 
 _CODES = {torch.float32: capi.HLA_FP32, torch.bfloat16: capi.HLA_BF16}
 
@@ -188,6 +189,7 @@ class ShortConv(torch.autograd.Function):
         return conv_forward(x, weight, bias, silu)
 
     @staticmethod
+    @once
     def backward(ctx, dy):
         x, weight, bias = ctx.saved_tensors
         if dy.stride(-1) != 1:
@@ -288,6 +290,7 @@ class QKNormRope(torch.autograd.Function):
         return qk_norm_rope_forward(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
 
     @staticmethod
+    @once
     def backward(ctx, dq_out, dk_out):
         grads = qk_norm_rope_backward(*ctx.saved_tensors, _upstream(dq_out), _upstream(dk_out), *ctx.how)
         return (*grads, None, None, None, None, None)
@@ -386,6 +389,7 @@ class SSMScan(torch.autograd.Function):
         return ssm_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus)
 
     @staticmethod
+    @once
     def backward(ctx, dy):
         return (*ssm_backward(*ctx.saved_tensors, _upstream(dy), ctx.softplus), None)
 

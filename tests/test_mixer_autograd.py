@@ -68,3 +68,17 @@ def test_no_graph_without_a_learned_input(name, stubbed):
     assert op(*args).requires_grad
     with torch.no_grad():
         assert not op(*args).requires_grad
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_second_derivatives_are_refused(name):
+    """A gradient taken with a graph cannot be differentiated again: a penalty
+    on it raises, also beside a term that can."""
+    op, args = _calls()[name]
+    for i in range(len(args)):
+        leaves = [a.clone().requires_grad_(j == i) for j, a in enumerate(args)]
+        out = op(*leaves)
+        grad, = torch.autograd.grad(out.float().sum(), leaves[i], create_graph=True)
+        assert grad.shape == args[i].shape
+        with pytest.raises(RuntimeError, match="differentiable once"):
+            (grad.float().square().sum() + leaves[i].float().square().sum()).backward()
