@@ -7,6 +7,7 @@ q/k/v are float32 or bfloat16, outputs and states are float32.
 import torch
 
 from . import capi
+from .autograd import once
 
 
 def _code(t):
@@ -256,6 +257,7 @@ class HLA2(torch.autograd.Function):
         return forward(q, k, v, chunk)
 
     @staticmethod
+    @once
     def backward(ctx, g):
         q, k, v = ctx.saved_tensors
         if g.data_ptr() % 16:                 # a contiguous view of autograd's may start anywhere

@@ -82,3 +82,15 @@ def test_second_derivatives_are_refused(name):
         assert grad.shape == args[i].shape
         with pytest.raises(RuntimeError, match="differentiable once"):
             (grad.float().square().sum() + leaves[i].float().square().sum()).backward()
+
+
+def test_second_derivatives_of_the_attention_are_refused(monkeypatch):
+    from paper_2510_27258_amd import hla
+    monkeypatch.setattr(hla, "forward", lambda q, k, v, chunk: torch.zeros(v.shape))
+    monkeypatch.setattr(hla, "_backward", lambda q, k, v, g, chunk, ws, dtype: tuple(torch.zeros_like(t) for t in (q, k, v)))
+    args = [torch.zeros(1, 2, 8, 64, dtype=BF16) for _ in range(3)]
+    for i in range(3):
+        leaves = [a.clone().requires_grad_(j == i) for j, a in enumerate(args)]
+        grad, = torch.autograd.grad(hla.hla2_attention(*leaves).sum(), leaves[i], create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiable once"):
+            (grad.float().square().sum() + leaves[i].float().square().sum()).backward()
