@@ -84,13 +84,15 @@ def _launch(entry, t, *args):
         torch.cuda.set_device(now)
 
 
+def _has_graph(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _learns(*tensors):
     """Whether a call has to go through its autograd function: an input has a
     graph, or may have a tangent (inside a forward-mode level), which that
     function refuses."""
-    if getattr(_forward_ad, "_current_level", 0) >= 0:
-        return True
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    return getattr(_forward_ad, "_current_level", 0) >= 0 or _has_graph(*tensors)
 
 
 def _out(out, shape, like, name="out"):
@@ -395,7 +397,11 @@ class SSMScan(torch.autograd.Function):
 
 
 def ssm_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus=True):
-    """Differentiable ssm_forward."""
+    """Differentiable ssm_forward.  The gradients cover bf16 inputs: fp32 ones
+    that need them are refused here."""
+    if x.dtype != torch.bfloat16 and _has_graph(x, dt, A, Bm, Cm, D, dt_bias):
+        raise capi.HLAError(capi.HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs: x, Bm and Cm must be "
+                            f"bf16 to be differentiated, got {x.dtype}; without gradients take ssm_forward or no_grad")
     if not _learns(x, dt, A, Bm, Cm, D, dt_bias):
         return ssm_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus)
     return SSMScan.apply(x, dt, A, Bm, Cm, D, dt_bias, softplus)

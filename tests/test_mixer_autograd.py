@@ -5,7 +5,7 @@ import pytest
 import torch
 import torch.autograd.forward_ad as fwd
 
-from paper_2510_27258_amd import mixer
+from paper_2510_27258_amd import capi, mixer
 
 BF16 = torch.bfloat16
 
@@ -94,3 +94,17 @@ def test_second_derivatives_of_the_attention_are_refused(monkeypatch):
         grad, = torch.autograd.grad(hla.hla2_attention(*leaves).sum(), leaves[i], create_graph=True)
         with pytest.raises(RuntimeError, match="differentiable once"):
             (grad.float().square().sum() + leaves[i].float().square().sum()).backward()
+
+
+def test_fp32_scan_to_be_trained_is_refused_before_its_forward(stubbed):
+    """The scan's gradients cover bf16: fp32 inputs that need them raise in
+    the forward, not after it."""
+    op, args = _calls(torch.float32)["scan"]
+    for i in range(len(args)):
+        leaves = [a.clone().requires_grad_(j == i) for j, a in enumerate(args)]
+        with pytest.raises(capi.HLAError, match="bf16") as e:
+            op(*leaves)
+        assert e.value.code == capi.HLA_ERR_UNSUPPORTED and not stubbed
+    with torch.no_grad():
+        op(*leaves)
+    assert len(stubbed) == 1
