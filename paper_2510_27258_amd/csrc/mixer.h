@@ -46,6 +46,7 @@ struct QkRope {
   void *dqw, *dkw;              // [d] of the weights' type, or null
 };
 hipError_t launch_qk_rope(const QkRope& a, hipStream_t s);
+double qk_rope_threads(const QkRope& a);   // of the forward's launch
 size_t qk_rope_backward_ws(int d);
 hipError_t launch_qk_rope_backward(const QkRope& a, void* ws, hipStream_t s);
 

@@ -109,11 +109,8 @@ int qk_check(const hla::QkRope& a) {
       (rc = check_type(a.w_dtype, "w_dtype")) || (rc = check_flag(a.pos64, "pos64")))
     return rc;
   if (!std::isfinite(a.eps) || a.eps < 0.f) return fail(HLA_ERR_INVALID, "eps must be finite and >= 0");
-  // 256 threads a block, at most 2^32 threads a launch
-  const int v = 16 / esize(a.dtype);
-  long long lanes = 4;
-  while (lanes * v < a.d) lanes *= 2;
-  if ((double)a.B * a.n * ((double)a.H + a.Hk) * (double)lanes / 4 >= 4294967296.0 - 256)
+  // a launch has less than 2^32 threads (the gradients' own has few: they cover what the forward does)
+  if (hla::qk_rope_threads(a) >= 4294967296.0)
     return fail(HLA_ERR_UNSUPPORTED, "B=%d n=%d H=%d Hk=%d: too many rows for a launch", a.B, a.n, a.H, a.Hk);
   const unsigned ws = esize(a.w_dtype);
   if ((rc = check_rows(a.q, a.dtype, "q")) || (rc = check_rows(a.k, a.dtype, "k")) ||

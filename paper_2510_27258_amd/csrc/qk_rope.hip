@@ -18,6 +18,8 @@
 // Measured: 2 x 16384 tokens of 32 + 32 heads of 128 in bf16 (1.07 GB) 278 us,
 // 3.9 TB/s; 4 x 4096 of 16 + 16 heads of 64 40 us, their gradients (201 MB) 53
 // us, 3.8 TB/s, and 4 us for the weights' sums.
+#include <cmath>
+
 #include "common.h"
 #include "mixer.h"
 #include "vec.h"
@@ -321,12 +323,16 @@ hipError_t launch_back(const QkRope& a, float* part, hipStream_t s) {
 // Forward eight (a load each), gradients four (two loads each).  Measured, several
 // heads against one: 276 and 639 us (2 x 16384 tokens of 64 heads of 128), 97 and 130
 // (4 x 4096 of 32 of 64 with gradients); the other way 7.1 and 4.5 us (64 tokens).
+constexpr int kQkHeads = 8, kQkBackHeads = 4;
+bool several_heads(const QkRope& a, int LP, int HP) {      // in doubles: any sizes may be asked for
+  return (double)a.B * a.n * ((double)a.H + a.Hk) * LP / HP >= 256. * 8 * 64;
+}
 template <typename T, int V, int LP>
 hipError_t by_heads(const QkRope& a, float* part, hipStream_t s) {
-  const long long rows = (long long)a.B * a.n * (a.H + a.Hk);
   if (part)
-    return rows * LP / 4 >= 256LL * 8 * 64 ? launch_back<T, V, LP, 4>(a, part, s) : launch_back<T, V, LP, 1>(a, part, s);
-  return rows * LP / 8 >= 256LL * 8 * 64 ? launch<T, V, LP, 8>(a, s) : launch<T, V, LP, 1>(a, s);
+    return several_heads(a, LP, kQkBackHeads) ? launch_back<T, V, LP, kQkBackHeads>(a, part, s)
+                                              : launch_back<T, V, LP, 1>(a, part, s);
+  return several_heads(a, LP, kQkHeads) ? launch<T, V, LP, kQkHeads>(a, s) : launch<T, V, LP, 1>(a, s);
 }
 
 template <typename T, int V>
@@ -348,6 +354,13 @@ hipError_t by_type(const QkRope& a, float* part, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_qk_rope(const QkRope& a, hipStream_t s) { return by_type(a, nullptr, s); }
+double qk_rope_threads(const QkRope& a) {
+  const int pieces = a.d / (a.dtype == 1 ? 8 : 4);
+  int LP = 4;
+  while (LP < pieces) LP *= 2;
+  const double HP = several_heads(a, LP, kQkHeads) ? kQkHeads : 1, RB = kQkThreads / LP;
+  return std::ceil((double)a.B * a.n / RB) * (std::ceil(a.H / HP) + std::ceil(a.Hk / HP)) * kQkThreads;
+}
 size_t qk_rope_backward_ws(int d) { return sizeof(float) * (kQkBackBlocks + 2) * (size_t)d; }
 hipError_t launch_qk_rope_backward(const QkRope& a, void* ws, hipStream_t s) {
   return by_type(a, static_cast<float*>(ws), s);
