@@ -66,6 +66,7 @@ bool ssm_sizes_ok(int P, int N);
 size_t ssm_forward_ws(int B, int n, int H, int P, int N, int dtype);
 hipError_t launch_ssm_forward(const Ssm& a, void* ws, hipStream_t s);
 hipError_t launch_ssm_step(const Ssm& a, hipStream_t s);
+double ssm_backward_threads(int B, int n, int H, int G);   // of its largest launch
 size_t ssm_backward_ws(int B, int n, int H, int P, int G, int N);
 hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s);
 

@@ -135,6 +135,14 @@ int ssm_sizes(int B, int n, int H, int P, int G, int N) {
   return HLA_OK;
 }
 
+// What the gradients ask for beyond the scan itself: a launch has less than 2^32 threads.
+int ssm_back_sizes(int B, int n, int H, int G, int dtype) {
+  if (dtype != HLA_BF16) return fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
+  if (hla::ssm_backward_threads(B, n, H, G) >= 4294967296.0)
+    return fail(HLA_ERR_UNSUPPORTED, "n=%d is too long for the gradients of B=%d G=%d", n, B, G);
+  return HLA_OK;
+}
+
 // Rows of w elements, n of them a sequence.  The kernels' tiles end where the
 // next row would begin, so rows must not overlap; the stride of a single row
 // is not used and set to one that does not.
@@ -297,11 +305,9 @@ int hla_ssm_step(float* state, const void* x, long long x_bs, const void* dt, lo
 }
 
 size_t hla_ssm_backward_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype) {
-  if (ssm_sizes(B, n, H, P, G, N) != HLA_OK || check_type(dtype, "dtype") != HLA_OK) return 0;
-  if (dtype != HLA_BF16) {
-    fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
+  if (ssm_sizes(B, n, H, P, G, N) != HLA_OK || check_type(dtype, "dtype") != HLA_OK ||
+      ssm_back_sizes(B, n, H, G, dtype) != HLA_OK)
     return 0;
-  }
   return hla::ssm_backward_ws(B, n, H, P, G, N);
 }
 
@@ -321,8 +327,7 @@ int hla_ssm_backward(const void* x, long long x_bs, long long x_ts, const void* 
   a.dx = dx; a.ddt = ddt; a.dA = dA; a.dBm = dBm; a.dCm = dCm; a.dD = dD; a.ddt_bias = ddt_bias;
   a.B = B; a.n = n; a.H = H; a.P = P; a.G = G; a.N = N; a.softplus = softplus; a.dtype = dtype; a.dt_dtype = dt_dtype;
   int rc;
-  if ((rc = ssm_check(a)) != HLA_OK) return rc;
-  if (dtype != HLA_BF16) return fail(HLA_ERR_UNSUPPORTED, "the scan's gradients cover bf16 inputs");
+  if ((rc = ssm_check(a)) || (rc = ssm_back_sizes(B, n, H, G, dtype))) return rc;
   if ((rc = ssm_rows(a.dy, n, H * P, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
       (rc = check_own(ddt, esize(dt_dtype), "ddt")) || (rc = check_own(dA, 4, "dA")) || (rc = check_16(dBm, "dBm")) ||
       (rc = check_16(dCm, "dCm")) || (rc = check_own(dD, 4, "dD", false)) ||

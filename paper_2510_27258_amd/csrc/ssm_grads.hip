@@ -545,6 +545,10 @@ GradWs carve(void* ws, int B, int n, int H, int P, int G, int N) {
 
 }  // namespace
 
+double ssm_backward_threads(int B, int n, int H, int G) {
+  const int tiles = ssm_plan(B * H, n, kGQ).tiles;
+  return (double)B * tiles * G * head_subsets(B, tiles, G, H / G) * kGThreads;
+}
 size_t ssm_backward_ws(int B, int n, int H, int P, int G, int N) { return carve(nullptr, B, n, H, P, G, N).bytes; }
 
 hipError_t launch_ssm_backward(const Ssm& a, void* ws, hipStream_t s) {

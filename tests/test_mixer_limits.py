@@ -17,3 +17,18 @@ from tests.test_mixer_refusals import BF16, FP32, INVALID, P, UNSUP, _conv, _qk,
 def test_qk_launches(B, n, H, Hk, dtype, fits):
     rc = _qk(B=B, n=n, H=H, Hk=Hk, qt=H * 128, kt=Hk * 128, dt=dtype)
     _refused(rc, *((INVALID, "k_out is NULL") if fits else (UNSUP, "too many rows")))
+
+
+# The gradients' first launch has 512 threads for every 64 tokens, group and
+# subset of a group's heads.
+@pytest.mark.parametrize("B,n,H,G,fits", [
+    (4, (1 << 23) - 64, 16, 16, True), (4, 1 << 23, 16, 16, False), (1, (1 << 25) + 1, 16, 16, False),
+    (4, 1 << 24, 16, 8, False), (4, (1 << 24) - 64, 16, 8, True), (4, 1 << 24, 16, 1, True)])
+def test_scan_gradient_launches(B, n, H, G, fits):
+    need = capi.hla_ssm_backward_workspace_bytes(B, n, H, 16, G, 16, BF16)
+    assert (need > 0) == fits
+    if not fits:
+        assert "too long" in capi.hla_last_error()
+    rc = capi.lib().hla_ssm_backward(P, 0, H * 16, P, 0, H, P, P, 0, G * 16, P, 0, G * 16, None, None, P, 0, H * 16, P, P,
+                                     P, P, P, None, None, B, n, H, 16, G, 16, 1, BF16, BF16, None, 0, None)
+    _refused(rc, *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else (UNSUP, "too long")))
