@@ -130,8 +130,8 @@ int ssm_sizes(int B, int n, int H, int P, int G, int N) {
   if ((long long)B * H > 65535) return fail(HLA_ERR_UNSUPPORTED, "B*H=%lld exceeds 65535", (long long)B * H);
   if (!hla::ssm_sizes_ok(P, N))
     return fail(HLA_ERR_UNSUPPORTED, "P and N must be multiples of 16 from 16 to 128 (got P=%d N=%d)", P, N);
-  if ((long long)B * H * n >= (1LL << 31))
-    return fail(HLA_ERR_UNSUPPORTED, "n=%d is too long: B*H*n must stay below 2^31", n);
+  if ((long long)B * H * n >= (1LL << 31) || n > (1LL << 31) - 64)   // tokens are counted in whole blocks of 64
+    return fail(HLA_ERR_UNSUPPORTED, "n=%d is too long: B*H*n must stay below 2^31, n at most 2^31 - 64", n);
   return HLA_OK;
 }
 

@@ -32,3 +32,14 @@ def test_scan_gradient_launches(B, n, H, G, fits):
     rc = capi.lib().hla_ssm_backward(P, 0, H * 16, P, 0, H, P, P, 0, G * 16, P, 0, G * 16, None, None, P, 0, H * 16, P, P,
                                      P, P, P, None, None, B, n, H, 16, G, 16, 1, BF16, BF16, None, 0, None)
     _refused(rc, *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else (UNSUP, "too long")))
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_longest_scans(dtype):
+    """Tokens come in blocks of 64, which are counted below 2^31."""
+    for n, fits in (((1 << 31) - 1, False), ((1 << 31) - 63, False), ((1 << 31) - 64, True)):
+        need = capi.hla_ssm_workspace_bytes(1, n, 1, 16, 1, 16, dtype)
+        # 16 bytes a token, and the ends
+        assert (16 * n <= need < 17 * n) if fits else need == 0
+        _refused(_ssm(n=n, H=1, dtt=1, ty=dtype, y=P, ws=None), *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else
+                                                                  (UNSUP, "too long")))
