@@ -82,6 +82,13 @@ int conv_sizes(int B, int n, int D, int K) {
   return HLA_OK;
 }
 
+// The gradients' sums over the tokens: 16 threads a weight or bias, in whole blocks of 64 of these, less than 2^32.
+int conv_back_sizes(int D, int K) {
+  if ((long long)D * (K + 1) > (1LL << 28) - 64)
+    return fail(HLA_ERR_UNSUPPORTED, "D=%d of K=%d is too wide for the gradients: D (K + 1) must stay below 2^28 - 63", D, K);
+  return HLA_OK;
+}
+
 int conv_check(const hla::Conv& c) {
   int rc;
   if ((rc = conv_sizes(c.B, c.n, c.D, c.K)) || (rc = check_flag(c.silu, "silu")) ||
@@ -189,7 +196,7 @@ int hla_conv_forward(const void* x, long long x_bs, long long x_ts, const void* 
 }
 
 size_t hla_conv_backward_workspace_bytes(int B, int n, int D, int K) {
-  if (conv_sizes(B, n, D, K) != HLA_OK) return 0;
+  if (conv_sizes(B, n, D, K) != HLA_OK || conv_back_sizes(D, K) != HLA_OK) return 0;
   return hla::conv_backward_ws(B, n, D, K);
 }
 
@@ -203,7 +210,7 @@ int hla_conv_backward(const void* x, long long x_bs, long long x_ts, const void*
   c.w = weight; c.bias = bias; c.dx = dx; c.dw = dweight; c.dbias = dbias;
   c.B = B; c.n = n; c.D = D; c.K = K; c.silu = silu; c.dtype = dtype; c.w_dtype = w_dtype;
   int rc;
-  if ((rc = conv_check(c)) != HLA_OK) return rc;
+  if ((rc = conv_check(c)) || (rc = conv_back_sizes(D, K))) return rc;
   const unsigned es = esize(dtype), wes = esize(w_dtype);
   if ((rc = check_own(dy, es, "dy")) || (rc = check_stride(dy_bs, dy_ts, "dy")) || (rc = check_own(dx, es, "dx")) ||
       (rc = check_own(dweight, wes, "dweight")) || (rc = check_own(dbias, wes, "dbias", false)) ||

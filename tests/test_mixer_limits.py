@@ -43,3 +43,13 @@ def test_longest_scans(dtype):
         assert (16 * n <= need < 17 * n) if fits else need == 0
         _refused(_ssm(n=n, H=1, dtt=1, ty=dtype, y=P, ws=None), *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else
                                                                   (UNSUP, "too long")))
+
+
+@pytest.mark.parametrize("D,K,fits", [((1 << 26) - 16, 3, True), ((1 << 26) - 15, 3, False), (1 << 27, 2, False), (500000000, 4, False),
+                                      (50000000, 4, True)])
+def test_conv_gradient_widths(D, K, fits):
+    """The sums over the tokens take 16 threads a weight or bias, of less than 2^32."""
+    assert (capi.hla_conv_backward_workspace_bytes(1, 1, D, K) > 0) == fits
+    rc = capi.lib().hla_conv_backward(P, 0, D, P, None, P, 0, D, P, P, None, 1, 1, D, K, 1, BF16, BF16, None, 0, None)
+    _refused(rc, *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else (UNSUP, "too wide")))
+    assert _conv(n=1, xt=D, D=D, K=K) == INVALID and "y is NULL" in capi.hla_last_error()
