@@ -51,6 +51,12 @@ int check_own(const void* p, unsigned a, const char* name, bool need = true) {
 }
 int check_16(const void* p, const char* name, bool need = true) { return check_own(p, 16, name, need); }
 
+// The strides of dimensions of size one are not used, whatever they are.
+void drop_unused(hla::Rows& r, int B, int n) {
+  if (B == 1) r.bs = 0;
+  if (n == 1) r.ts = 0;
+}
+
 int check_stride(long long bs, long long ts, const char* name) {
   if (bs < 0 || ts < 0) return fail(HLA_ERR_INVALID, "%s: strides must be >= 0 (got %lld, %lld)", name, bs, ts);
   return HLA_OK;
@@ -89,8 +95,10 @@ int conv_back_sizes(int D, int K) {
   return HLA_OK;
 }
 
-int conv_check(const hla::Conv& c) {
+int conv_check(hla::Conv& c) {
   int rc;
+  drop_unused(c.x, c.B, c.n);
+  drop_unused(c.dy, c.B, c.n);
   if ((rc = conv_sizes(c.B, c.n, c.D, c.K)) || (rc = check_flag(c.silu, "silu")) ||
       (rc = check_type(c.dtype, "dtype")) || (rc = check_type(c.w_dtype, "w_dtype")))
     return rc;
@@ -102,8 +110,10 @@ int conv_check(const hla::Conv& c) {
 }
 
 // ---------------------------------------------------------------------------
-int qk_check(const hla::QkRope& a) {
+int qk_check(hla::QkRope& a) {
   int rc;
+  drop_unused(a.q, a.B, a.n);
+  drop_unused(a.k, a.B, a.n);
   if (a.B < 1 || a.n < 1 || a.H < 1 || a.Hk < 1)
     return fail(HLA_ERR_INVALID, "B, n, H and Hk must be >= 1 (got B=%d n=%d H=%d Hk=%d)", a.B, a.n, a.H, a.Hk);
   if (a.d < 16 || a.d > 256 || a.d % 8)
@@ -152,8 +162,9 @@ int ssm_back_sizes(int B, int n, int H, int G, int dtype) {
 
 // Rows of w elements, n of them a sequence.  The kernels' tiles end where the
 // next row would begin, so rows must not overlap; the stride of a single row
-// is not used and set to one that does not.
-int ssm_rows(hla::Rows& r, int n, int w, int dtype, const char* name) {
+// is set to one that does not.
+int ssm_rows(hla::Rows& r, int B, int n, int w, int dtype, const char* name) {
+  drop_unused(r, B, n);
   if (n == 1) r.ts = w;
   const int rc = check_rows(r, dtype, name);
   if (rc) return rc;
@@ -170,8 +181,10 @@ int ssm_check(hla::Ssm& a) {
   if ((rc = ssm_sizes(a.B, a.n, a.H, a.P, a.G, a.N)) || (rc = check_flag(a.softplus, "softplus")) ||
       (rc = check_type(a.dtype, "dtype")) || (rc = check_type(a.dt_dtype, "dt_dtype")))
     return rc;
-  if ((rc = ssm_rows(a.x, a.n, a.H * a.P, a.dtype, "x")) || (rc = ssm_rows(a.Bm, a.n, a.G * a.N, a.dtype, "Bm")) ||
-      (rc = ssm_rows(a.Cm, a.n, a.G * a.N, a.dtype, "Cm")) || (rc = check_own(a.dt.p, esize(a.dt_dtype), "dt")) ||
+  drop_unused(a.dt, a.B, a.n);
+  if ((rc = ssm_rows(a.x, a.B, a.n, a.H * a.P, a.dtype, "x")) ||
+      (rc = ssm_rows(a.Bm, a.B, a.n, a.G * a.N, a.dtype, "Bm")) ||
+      (rc = ssm_rows(a.Cm, a.B, a.n, a.G * a.N, a.dtype, "Cm")) || (rc = check_own(a.dt.p, esize(a.dt_dtype), "dt")) ||
       (rc = check_stride(a.dt.bs, a.dt.ts, "dt")) || (rc = check_own(a.A, 4, "A")) ||
       (rc = check_own(a.D, 4, "D", false)) || (rc = check_own(a.dt_bias, 4, "dt_bias", false)))
     return rc;
@@ -212,7 +225,7 @@ int hla_conv_backward(const void* x, long long x_bs, long long x_ts, const void*
   int rc;
   if ((rc = conv_check(c)) || (rc = conv_back_sizes(D, K))) return rc;
   const unsigned es = esize(dtype), wes = esize(w_dtype);
-  if ((rc = check_own(dy, es, "dy")) || (rc = check_stride(dy_bs, dy_ts, "dy")) || (rc = check_own(dx, es, "dx")) ||
+  if ((rc = check_own(dy, es, "dy")) || (rc = check_stride(c.dy.bs, c.dy.ts, "dy")) || (rc = check_own(dx, es, "dx")) ||
       (rc = check_own(dweight, wes, "dweight")) || (rc = check_own(dbias, wes, "dbias", false)) ||
       (rc = check_ws(workspace, workspace_bytes, hla::conv_backward_ws(B, n, D, K))))
     return rc;
@@ -335,7 +348,7 @@ int hla_ssm_backward(const void* x, long long x_bs, long long x_ts, const void* 
   a.B = B; a.n = n; a.H = H; a.P = P; a.G = G; a.N = N; a.softplus = softplus; a.dtype = dtype; a.dt_dtype = dt_dtype;
   int rc;
   if ((rc = ssm_check(a)) || (rc = ssm_back_sizes(B, n, H, G, dtype))) return rc;
-  if ((rc = ssm_rows(a.dy, n, H * P, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
+  if ((rc = ssm_rows(a.dy, B, n, H * P, dtype, "dy")) || (rc = check_16(dx, "dx")) ||
       (rc = check_own(ddt, esize(dt_dtype), "ddt")) || (rc = check_own(dA, 4, "dA")) || (rc = check_16(dBm, "dBm")) ||
       (rc = check_16(dCm, "dCm")) || (rc = check_own(dD, 4, "dD", false)) ||
       (rc = check_own(ddt_bias, 4, "ddt_bias", false)) ||

@@ -53,3 +53,30 @@ def test_conv_gradient_widths(D, K, fits):
     rc = capi.lib().hla_conv_backward(P, 0, D, P, None, P, 0, D, P, P, None, 1, 1, D, K, 1, BF16, BF16, None, 0, None)
     _refused(rc, *((capi.HLA_ERR_WORKSPACE, "workspace of") if fits else (UNSUP, "too wide")))
     assert _conv(n=1, xt=D, D=D, K=K) == INVALID and "y is NULL" in capi.hla_last_error()
+
+
+def test_strides_of_size_one_dimensions_are_not_used():
+    """One sequence has no distance to the next, one token none to the next:
+    whatever stands there is not looked at, odd and negative values included."""
+    for kw in (dict(xb=-1), dict(xt=-1, n=1), dict(xb=-3, xt=-5, n=1)):
+        _refused(_conv(**kw), INVALID, "y is NULL")
+    for kw in (dict(qb=-1), dict(qb=3), dict(qt=-1, kt=3, n=1)):
+        _refused(_qk(**kw), INVALID, "k_out is NULL")
+    for kw in (dict(xb=3), dict(xb=-1), dict(xt=3, bt=-1, dtt=-1, n=1), dict(dtb=-1)):
+        _refused(_scan(**kw), INVALID, "y is NULL")
+    _refused(capi.lib().hla_ssm_step(P, P, -1, P, -1, P, P, 3, P, 5, None, None, None, 1, 2, 64, 1, 64, 1, BF16, BF16, None),
+             INVALID, "y is NULL")
+    _refused(capi.lib().hla_conv_backward(P, -1, -1, P, None, P, -1, -1, None, P, None, 1, 1, 64, 4, 1, BF16, BF16, P, 1 << 30,
+                                          None), INVALID, "dx is NULL")
+    _refused(capi.lib().hla_ssm_backward(P, -1, 3, P, -1, -1, P, P, 3, 3, P, 3, 3, None, None, P, -1, 3, None, P, P, P, P, None,
+                                         None, 1, 1, 2, 64, 1, 64, 1, BF16, BF16, P, 1 << 40, None), INVALID, "dx is NULL")
+    # two of them are looked at
+    _refused(_conv(B=2, xb=-1), INVALID, "strides")
+    _refused(_qk(B=2, qb=3), INVALID, "whole 16-byte")
+    _refused(_scan(B=2, xb=3), INVALID, "whole 16-byte")
+    _refused(_scan(B=2, xb=1024, dtb=-1), INVALID, "strides")
+
+
+def _scan(B=1, n=8, xb=0, xt=128, dtb=0, dtt=2, bt=64):
+    return capi.lib().hla_ssm_forward(P, xb, xt, P, dtb, dtt, P, P, 0, bt, P, 0, 64, None, None, None, None, B, n, 2, 64, 1, 64,
+                                      1, BF16, BF16, P, 1 << 40, None)
