@@ -453,7 +453,7 @@ int hla_ssm_forward(const void *x, long long x_bs, long long x_ts, const void *d
 
 /* hla_ssm_step — one token of it for every head, the state updated in place:
  * x [B, H, P], dt [B, H], Bm, Cm [B, G, N], y [B, H, P]; strides between
- * batches only.  No workspace. */
+ * batches only.  No workspace.  B*H < 2^24. */
 int hla_ssm_step(float *state, const void *x, long long x_bs, const void *dt, long long dt_bs, const float *A,
                  const void *Bm, long long b_bs, const void *Cm, long long c_bs, const float *D,
                  const float *dt_bias, void *y, int B, int H, int P, int G, int N, int softplus, int dtype,

@@ -140,11 +140,15 @@ int qk_check(hla::QkRope& a) {
 }
 
 // ---------------------------------------------------------------------------
-int ssm_sizes(int B, int n, int H, int P, int G, int N) {
+// A launch of the scan has the heads in its second dimension, the step a workgroup of 256 threads for each.
+constexpr long long kScanHeads = 65535, kStepHeads = (1LL << 24) - 1;
+
+int ssm_sizes(int B, int n, int H, int P, int G, int N, long long most = kScanHeads) {
   if (B < 1 || n < 1 || H < 1 || G < 1)
     return fail(HLA_ERR_INVALID, "B, n, H and G must be >= 1 (got B=%d n=%d H=%d G=%d)", B, n, H, G);
   if (H % G) return fail(HLA_ERR_INVALID, "H=%d must be a multiple of G=%d", H, G);
-  if ((long long)B * H > 65535) return fail(HLA_ERR_UNSUPPORTED, "B*H=%lld exceeds 65535", (long long)B * H);
+  if ((long long)B * H > most)
+    return fail(HLA_ERR_UNSUPPORTED, "B*H=%lld exceeds %lld", (long long)B * H, most);
   if (!hla::ssm_sizes_ok(P, N))
     return fail(HLA_ERR_UNSUPPORTED, "P and N must be multiples of 16 from 16 to 128 (got P=%d N=%d)", P, N);
   if ((long long)B * H * n >= (1LL << 31) || n > (1LL << 31) - 64)   // tokens are counted in whole blocks of 64
@@ -176,9 +180,9 @@ int ssm_rows(hla::Rows& r, int B, int n, int w, int dtype, const char* name) {
   return HLA_OK;
 }
 
-int ssm_check(hla::Ssm& a) {
+int ssm_check(hla::Ssm& a, long long most = kScanHeads) {
   int rc;
-  if ((rc = ssm_sizes(a.B, a.n, a.H, a.P, a.G, a.N)) || (rc = check_flag(a.softplus, "softplus")) ||
+  if ((rc = ssm_sizes(a.B, a.n, a.H, a.P, a.G, a.N, most)) || (rc = check_flag(a.softplus, "softplus")) ||
       (rc = check_type(a.dtype, "dtype")) || (rc = check_type(a.dt_dtype, "dt_dtype")))
     return rc;
   drop_unused(a.dt, a.B, a.n);
@@ -319,7 +323,7 @@ int hla_ssm_step(float* state, const void* x, long long x_bs, const void* dt, lo
   a.A = A; a.D = D; a.dt_bias = dt_bias; a.state = state; a.y = y;
   a.B = B; a.n = 1; a.H = H; a.P = P; a.G = G; a.N = N; a.softplus = softplus; a.dtype = dtype; a.dt_dtype = dt_dtype;
   int rc;
-  if ((rc = ssm_check(a)) || (rc = check_16(y, "y")) || (rc = check_16(state, "state"))) return rc;
+  if ((rc = ssm_check(a, kStepHeads)) || (rc = check_16(y, "y")) || (rc = check_16(state, "state"))) return rc;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return done(hla::launch_ssm_step(a, s), "state space step");
 }

@@ -97,3 +97,12 @@ def test_attentions_upstream_gradient_at_any_address():
     got = torch.autograd.grad(flat, (q, k, v), torch.cat([torch.zeros(1, device="cuda"), up.flatten()]))
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_step_of_more_heads_than_a_grid_dimension():
+    """70400 heads: more than 65535."""
+    args, state, _ = _ssm_case(2200, 1, 32, 16, 16, 1, BF16, 35)
+    x, dt, A, Bm, Cm, D, bias = args
+    first = state.clone()
+    y = hla.ssm_step(state, x[:, 0], dt[:, 0], A, Bm[:, 0], Cm[:, 0], D, bias)
+    _check_scan(args, first, y[:, None], state)

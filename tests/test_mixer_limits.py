@@ -80,3 +80,11 @@ def test_strides_of_size_one_dimensions_are_not_used():
 def _scan(B=1, n=8, xb=0, xt=128, dtb=0, dtt=2, bt=64):
     return capi.lib().hla_ssm_forward(P, xb, xt, P, dtb, dtt, P, P, 0, bt, P, 0, 64, None, None, None, None, B, n, 2, 64, 1, 64,
                                       1, BF16, BF16, P, 1 << 40, None)
+
+
+@pytest.mark.parametrize("B,H,fits", [(2048, 32, True), ((1 << 24) - 1, 1, True), (1 << 12, 1 << 12, False), (1 << 20, 1 << 20, False)])
+def test_heads_of_a_step(B, H, fits):
+    """A workgroup a head, 2^32 threads; more than the scan's 65535 heads, which are a grid's second dimension."""
+    rc = capi.lib().hla_ssm_step(P, P, H * 16, P, H, P, P, 16, P, 16, None, None, None, B, H, 16, 1, 16, 1, BF16, BF16, None)
+    _refused(rc, *((INVALID, "y is NULL") if fits else (UNSUP, "B*H")))
+    assert capi.hla_ssm_workspace_bytes(2048, 1, 32, 16, 1, 16, BF16) == 0 and "65535" in capi.hla_last_error()
