@@ -437,12 +437,13 @@ int hla_qk_norm_rope_backward(const void *q, long long q_bs, long long q_ts, con
  * [B, H, N, P]: the state before the first token, replaced by the one after
  * the last; without it the scan starts from zero.
  * P and N: multiples of 16 from 16 to 128; G divides H; B*H <= 65535;
- * B*H*n < 2^31, n <= 2^31 - 64.  A <= 0 is meant (a growing state may overflow).  x, Bm, Cm:
- * 16-byte aligned, strides of whole 16-byte pieces, the rows of a sequence not
- * overlapping.  bf16 inputs: scores and
- * the state that the outputs read are rounded to bf16 (2^-8 of a term, as the
- * outputs are), the state itself is kept in fp32.  An infinite or NaN input
- * gives NaN in every output that depends on it, and in no other.
+ * B*H*n < 2^31, n <= 2^31 - 64.  A <= 0 is meant (a growing state may
+ * overflow).  x, Bm, Cm: 16-byte aligned, strides of whole 16-byte pieces, the
+ * rows of a sequence not overlapping.  bf16 inputs: scores and the state that
+ * the outputs read are rounded to bf16 (2^-8 of a term, as the outputs are),
+ * the state itself is kept in fp32.  An infinite or NaN input leaves every
+ * output and state element that depends on it infinite or NaN (which of the
+ * two depends on where the sequence is cut), and no other.
  * workspace: at least hla_ssm_workspace_bytes(...) bytes. */
 size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype);
 int hla_ssm_forward(const void *x, long long x_bs, long long x_ts, const void *dt, long long dt_bs,

@@ -106,3 +106,36 @@ def test_step_of_more_heads_than_a_grid_dimension():
     first = state.clone()
     y = hla.ssm_step(state, x[:, 0], dt[:, 0], A, Bm[:, 0], Cm[:, 0], D, bias)
     _check_scan(args, first, y[:, None], state)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("n", [700, 2100])
+def test_infinities_over_segments(dtype, n):
+    """Bad values in the first, a middle and the last segment, whose states the
+    later segments take from the walk to the segments' ends (2 and 8 segments
+    in bf16, 5 and 16 in fp32): what depends on them is infinite or NaN,
+    whatever the segments, and the rest keeps its bits."""
+    args, state, _ = _ssm_case(1, n, 2, 64, 64, 1, dtype, 36, views=False)
+    clean_state = state.clone()
+    clean = hla.ssm_prefill(clean_state, *args)
+    for what in (0, 1, 3):
+        for t in (3, n // 2, n - 2):
+            for bad in (float("nan"), float("inf"), -float("inf")):
+                if what == 1 and bad < 0:
+                    continue                  # a step of softplus(-inf) = 0 is a number
+                _say(f"n={n} {dtype} bad value {bad} in argument {what} at {t}")
+                a = [m.clone() for m in args]
+                st = state.clone()
+                hit, hit_state = torch.zeros_like(clean, dtype=torch.bool), torch.zeros_like(st, dtype=torch.bool)
+                if what == 0:
+                    a[0][0, t, 1, 5] = bad
+                    hit[0, t:, 1, 5] = hit_state[0, 1, :, 5] = True
+                elif what == 1:
+                    a[1][0, t, 1] = bad
+                    hit[0, t:, 1] = hit_state[0, 1] = True
+                else:
+                    a[3][0, t, 0, 7] = bad
+                    hit[0, t:] = hit_state[0, :, 7] = True
+                y = hla.ssm_prefill(st, *a)
+                assert torch.equal(~torch.isfinite(y), hit) and torch.equal(~torch.isfinite(st), hit_state)
+                assert torch.equal(y[~hit], clean[~hit]) and torch.equal(st[~hit_state], clean_state[~hit_state])
