@@ -58,7 +58,9 @@ __device__ __forceinline__ void angles(const QkRope& a, int b, int t, int c, flo
   const bool in = pos >= 0 && pos < a.positions;
   const int half = a.rot / 2;
   const size_t at = in ? (size_t)pos * half : 0;
-  if (!a.interleaved && half % V == 0) {
+  // 16 bytes of a table at once, where its rows and its own address allow (it needs an fp32's alignment only)
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.cs) | reinterpret_cast<uintptr_t>(a.sn)) & 15) == 0;
+  if (!a.interleaved && half % V == 0 && wide) {
     if (c < a.rot) {
       const int p = c < half ? c : c - half;
       load_many<float, 4, V>(a.cs, at + p, cs);

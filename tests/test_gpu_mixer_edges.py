@@ -139,3 +139,18 @@ def test_infinities_over_segments(dtype, n):
                 y = hla.ssm_prefill(st, *a)
                 assert torch.equal(~torch.isfinite(y), hit) and torch.equal(~torch.isfinite(st), hit_state)
                 assert torch.equal(y[~hit], clean[~hit]) and torch.equal(st[~hit_state], clean_state[~hit_state])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_qk_tables_at_any_fp32_address(dtype):
+    """Tables that start one float behind a 16-byte boundary."""
+    q, k, qw, kw, cos, sin, pos, gq, gk = _qk_case(2, 30, 3, 2, 64, 64, dtype, 32)
+    off = []
+    for t in (cos, sin):
+        flat = torch.empty(t.numel() + 1, device="cuda")
+        flat[1:] = t.flatten()
+        off.append(flat[1:].view_as(t))
+        assert off[-1].data_ptr() % 16 == 4
+    for f, more in ((hla.qk_norm_rope_forward, ()), (hla.qk_norm_rope_backward, (gq, gk))):
+        for a, b in zip(f(q, k, qw, kw, cos, sin, pos, *more), f(q, k, qw, kw, *off, pos, *more)):
+            assert torch.equal(a, b)
