@@ -384,14 +384,20 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
     lds_barrier();
   }
 
-  // the tile's own part of dB and dC: the heads' sum z[t][s] with C and B
+  // the tile's own part of dB and dC: the heads' sum z[t][s], in two pieces (16
+  // bits; with one dB and dC were 0.0023 off 64 bits instead of the 0.0017 of
+  // their own rounding), with C and B.  The second lies where x and dy were.
+  static_assert(sizeof(S.x) + sizeof(S.dy) >= sizeof(S.p), "room for the second piece");
+  uint16_t* const p2 = reinterpret_cast<uint16_t*>(smem + offsetof(L_, x));
   const int l = opaque(threadIdx.x) & 63, r = l & 15, g = l >> 4;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float v[4] = {z[i][0], z[i][1], z[i][2], z[i][3]};
-    uint2 o[1];
-    pieces4<1>(v, o);
-    *reinterpret_cast<uint2*>(S.p + (16 * ts + r) * LDP + 16 * (s1 + 2 * i) + 4 * g) = o[0];
+    uint2 o[2];
+    pieces4<2>(v, o);
+    const int at = (16 * ts + r) * LDP + 16 * (s1 + 2 * i) + 4 * g;
+    *reinterpret_cast<uint2*>(S.p + at) = o[0];
+    *reinterpret_cast<uint2*>(p2 + at) = o[1];
   }
   lds_barrier();
 #pragma unroll
@@ -400,8 +406,14 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int tb = nt0 + j;
-      if (tb >= 2 * ks) dq[j] = mma(kt, frag(S.p, LDP, 16 * tb, 32 * ks, l), dq[j]);
-      if (tb < 2 * ks + 2) dk[j] = mma(qt, frag_tr(S.p, LDP, 16 * tb, 32 * ks, l), dk[j]);
+      if (tb >= 2 * ks) {
+        dq[j] = mma(kt, frag(p2, LDP, 16 * tb, 32 * ks, l), dq[j]);
+        dq[j] = mma(kt, frag(S.p, LDP, 16 * tb, 32 * ks, l), dq[j]);
+      }
+      if (tb < 2 * ks + 2) {
+        dk[j] = mma(qt, frag_tr(p2, LDP, 16 * tb, 32 * ks, l), dk[j]);
+        dk[j] = mma(qt, frag_tr(S.p, LDP, 16 * tb, 32 * ks, l), dk[j]);
+      }
     }
   }
 #pragma unroll

@@ -150,3 +150,16 @@ def test_scan_gradients_of_several_heads_a_workgroup(case, per):
             _within(g, e, np.abs(e) + (1e-5 * 2 ** 8) * s, 2 ** -8, name)
         else:
             _within(g, e, s, 1e-5, name)
+
+
+# No part of dB and dC is rounded before the output but the heads' weighted
+# scores, which are held in two pieces (2^-16 of a term); with 1e-5 of the
+# terms for the fp32 sums and 2^-8 of the value for the output:
+@pytest.mark.parametrize("case", [(2, 130, 4, 64, 64, 1), (1, 300, 2, 128, 128, 1), (1, 200, 6, 16, 48, 2), (22, 330, 2, 32, 32, 1)])
+def test_scan_gradients_of_shared_inputs_are_rounded_once(case):
+    _say(f"scan gradients {case}")
+    args, _, dy = _ssm_case(*case, BF16, 45)
+    got = hla.ssm_backward(*args, dy)
+    ref, scale = _vjp64(args, True, dy), _vjp64(args, True, dy, absolute=True)
+    for i, name in ((3, "dB"), (4, "dC")):
+        _within(got[i], ref[i], 2 ** -8 * np.abs(ref[i]) + 3e-5 * scale[i], 1, name)
