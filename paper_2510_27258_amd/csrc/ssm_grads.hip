@@ -11,7 +11,9 @@
 //   da_r = sum_{t>=r} (R_t - dt_t K_t + E_t) + sum_{s<r} dt_s F_s + 2^(Lend) <g, h>
 // with R and K the row and column sums of q_ts = M_ts (C_t . B_s)(dy_t . x_s),
 // s < t (R with dt_s), E_t = 2^(L_t) C_t . (h dy_t) and F_s = 2^(Lend - L_s) B_s .
-// (g x_s).  All cancellation stays within a tile, in fp32 sums.
+// (g x_s).  All cancellation stays within a tile, between R and K, whose fp32
+// terms (the same ones) are summed in fp64: the rounding of an fp32 sum counts
+// for every token before it, and d dt_bias was 1.2e-6 off 64 bits instead of 4e-7.
 //
 // The states before and the gradients after every tile come from two walks
 // (ssm_walk.h), one each way, into the workspace: 2 x 4 N P bytes a tile and
@@ -51,7 +53,8 @@ struct GradLds {
   uint16_t k[kGQ * LDK], q[kGQ * LDK], g[NN * LDX];
   uint16_t x[kGQ * LDX], dy[kGQ * LDX], p[kGQ * LDP];
   float Lh[kGQ], Ll[kGQ], dt[kGQ], el[kGQ], wq[kGQ];
-  float R[kGW][kGQ], own[kGQ], K[kGW][kGQ], E[kGW][kGQ], F[kGW][kGQ], one[kGW][2];
+  double R[2][kGQ], K[4][kGQ];
+  float own[kGQ], E[kGW][kGQ], F[kGW][kGQ], one[kGW][2];
 };
 
 __device__ __forceinline__ void unpack4(const uint2& u, float (&v)[4]) {
@@ -186,7 +189,8 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
       bf16x8 yf[KP];
 #pragma unroll
       for (int k = 0; k < KP; ++k) yf[k] = frag(S.dy, LDX, 16 * ts, 32 * k, l);
-      float rsum = 0.f, diag = 0.f;
+      double rsum = 0.0;
+      float diag = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int s0 = 16 * (s1 + 2 * i) + 4 * g;
@@ -204,7 +208,7 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
           // q's diagonal has no part in da: left out of the sums that would cancel it
           q[e] = s0 + e < t ? p[e] * v[e] : 0.f;
           z[i][e] += in ? m * v[e] * dd[e] : 0.f;
-          rsum += q[e] * dd[e];
+          rsum += (double)q[e] * (double)dd[e];
           if (s0 + e == t) {
             diag = v[e];
             S.own[t] = p[e] * v[e];
@@ -215,8 +219,8 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         *reinterpret_cast<uint2*>(S.p + t * LDP + s0) = o[0];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          q[e] = sum_row(q[e]);
-          if (r == 0) S.K[ts][s0 + e] = q[e];
+          const double k = sum_row((double)q[e]);
+          if (r == 0) S.K[ts][s0 + e] = k;
         }
       }
       rsum = sum_groups(rsum);
@@ -353,8 +357,10 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
     }
     // the gradients of dt and the per-head parameters: one wave, a token a lane
     if (w == (hh & (kGW - 1))) {
-      const float dt = S.dt[l], R = S.R[0][l] + S.R[1][l], Lend = S.Lh[kGQ - 1] + S.Ll[kGQ - 1];
-      float K = 0.f, Et = 0.f, Fs = 0.f, hg = 0.f, dD = 0.f;
+      const float dt = S.dt[l], Lend = S.Lh[kGQ - 1] + S.Ll[kGQ - 1];
+      const double R = S.R[0][l] + S.R[1][l];
+      double K = 0.0;
+      float Et = 0.f, Fs = 0.f, hg = 0.f, dD = 0.f;
 #pragma unroll
       for (int i = 0; i < TB; ++i) K += S.K[i][l];
 #pragma unroll
@@ -367,10 +373,10 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
         dD += S.one[i][0];
         hg += S.one[i][1];
       }
-      const double back = (double)R - (double)dt * K + Et, ahead = (double)dt * Fs;
+      const double back = R - (double)dt * K + Et, ahead = (double)dt * Fs;
       const double upto = sums_to(back), suf = last_lane(upto) - upto + back, pre = sums_to(ahead) - ahead;
       const double da = suf + pre + (double)exp2_(Lend) * hg;
-      double d = (double)Ah * da + ((double)K + S.own[l] + Fs);
+      double d = (double)Ah * da + (K + S.own[l] + Fs);
       if (a.softplus) d *= -expm1f(-dt);
       if (l < rows) store_any(a.ddt, a.dt_dtype, ((size_t)b * a.n + t0 + l) * a.H + head, (float)d);
       const float dA = (float)last_lane(sums_to(l < rows ? dt * da : 0.0)), db = (float)last_lane(sums_to(l < rows ? d : 0.0));

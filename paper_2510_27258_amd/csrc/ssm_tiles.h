@@ -97,6 +97,16 @@ __device__ __forceinline__ float sum_groups(float v) {        // over the four r
   h = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
+__device__ __forceinline__ double sum_groups(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  lo = __builtin_amdgcn_permlane16_swap((uint32_t)w, (uint32_t)w, false, false);
+  hi = __builtin_amdgcn_permlane16_swap((uint32_t)(w >> 32), (uint32_t)(w >> 32), false, false);
+  return __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+}
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp(float v) {               // 0 where the lane has no source
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xf, false));
@@ -109,7 +119,8 @@ __device__ __forceinline__ double dpp(double v) {
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 // over the 16 lanes of a row, in every one of them (rotations by 8, 4, 2, 1)
-__device__ __forceinline__ float sum_row(float v) {
+template <typename F>
+__device__ __forceinline__ F sum_row(F v) {
   v += dpp<0x128, 0xf>(v);
   v += dpp<0x124, 0xf>(v);
   v += dpp<0x122, 0xf>(v);

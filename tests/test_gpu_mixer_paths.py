@@ -163,3 +163,17 @@ def test_scan_gradients_of_shared_inputs_are_rounded_once(case):
     ref, scale = _vjp64(args, True, dy), _vjp64(args, True, dy, absolute=True)
     for i, name in ((3, "dB"), (4, "dC")):
         _within(got[i], ref[i], 2 ** -8 * np.abs(ref[i]) + 3e-5 * scale[i], 1, name)
+
+
+@pytest.mark.parametrize("P,N", [(32, 32), (64, 128), (128, 128)])
+def test_steps_before_all_pairs_have_no_gradient(P, N):
+    """x at the tokens 61 and 62 of a tile and dy at 62 and 63: the decay of a
+    token up to 61 lies between no pair, and its step has no gradient.  What a
+    kernel adds and takes away again there has to cancel to fp64's 2^-53 of at
+    most 64 x 64 terms, 5e-13 of the largest gradient."""
+    x, dt, A, Bm, Cm, D, bias = _ssm_case(1, 64, 3, P, N, 1, BF16, 46, dt_dtype=FP32, views=False)[0]
+    x[:, :61], x[:, 63:] = 0, 0
+    dy = torch.zeros_like(x)
+    dy[:, 62:] = torch.randn(dy[:, 62:].shape, device="cuda").to(BF16)
+    ddt = hla.ssm_backward(x, dt, A, Bm, Cm, D, bias, dy)[1]
+    assert (ddt[:, :61].abs().amax((0, 1)) <= 1e-12 * ddt.abs().amax((0, 1))).all(), ddt[0, :, 0]
