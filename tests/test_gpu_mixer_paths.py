@@ -177,3 +177,17 @@ def test_steps_before_all_pairs_have_no_gradient(P, N):
     dy[:, 62:] = torch.randn(dy[:, 62:].shape, device="cuda").to(BF16)
     ddt = hla.ssm_backward(x, dt, A, Bm, Cm, D, bias, dy)[1]
     assert (ddt[:, :61].abs().amax((0, 1)) <= 1e-12 * ddt.abs().amax((0, 1))).all(), ddt[0, :, 0]
+
+
+def test_keys_past_32_bits():
+    """Keys of more than 2^32 bytes and 2^31 elements, of 61 heads (no multiple
+    of what a thread takes): the last rows against the same rows by themselves."""
+    n, Hk = 280000, 61
+    k = torch.empty(1, n, Hk, 128, dtype=BF16, device="cuda")
+    k.normal_(generator=torch.Generator("cuda").manual_seed(1))
+    ang = torch.arange(1000, device="cuda")[:, None] * 100.0 ** (-torch.arange(64, device="cuda") / 64)
+    pos = torch.arange(n, device="cuda")[None] % 1000
+    args = None, None, ang.cos(), ang.sin()
+    qo, ko = hla.qk_norm_rope_forward(k[:, :, :1], k, *args, pos)
+    qt, kt = hla.qk_norm_rope_forward(k[:, -100:, :1], k[:, -100:], *args, pos[:, -100:])
+    assert torch.equal(ko[:, :, -100:], kt) and torch.equal(qo[:, :, -100:], qt)
