@@ -369,7 +369,8 @@ int ahla_forward(const void *q, const void *k, const void *v, float *out,
  *   - Outputs and gradients have the type of what they belong to (`dtype`,
  *     `w_dtype`, `dt_dtype`: HLA_FP32 or HLA_BF16), states of the scan and its
  *     per-head parameters are fp32.  All arithmetic is fp32 or better, rounded
- *     once on the way out unless said otherwise.
+ *     once on the way out unless said otherwise; the SiLU of bf16 inputs takes
+ *     the hardware's approximate exponential and reciprocal (2^-17 of a value).
  *   - A pointer said to be optional may be NULL.
  * ------------------------------------------------------------------------- */
 
@@ -389,6 +390,7 @@ int hla_conv_forward(const void *x, long long x_bs, long long x_ts, const void *
 
 /* hla_conv_backward — gradients of hla_conv_forward without a state: dx
  * [B, n, D], dweight [D, K] and dbias [D] (optional) for dy [B, n, D].
+ * D (K + 1) < 2^28 - 63.
  * workspace: at least hla_conv_backward_workspace_bytes(...) bytes. */
 size_t hla_conv_backward_workspace_bytes(int B, int n, int D, int K);
 int hla_conv_backward(const void *x, long long x_bs, long long x_ts, const void *weight, const void *bias,
@@ -464,8 +466,13 @@ int hla_ssm_step(float *state, const void *x, long long x_bs, const void *dt, lo
  * [B, n, H, P] (strides as x's): dx [B, n, H, P], dBm, dCm [B, n, G, N] (summed
  * over the heads of a group), ddt [B, n, H] of dt_dtype, and fp32 [H] dA, dD
  * (optional), ddt_bias (optional).  bf16 inputs (dtype = HLA_BF16); fp32 ones
- * return HLA_ERR_UNSUPPORTED.  Inputs and dy are meant to be finite: NaN in
- * one token may reach the gradients of the 64-token tile around it.
+ * return HLA_ERR_UNSUPPORTED.  Rounded to bf16 on the way: the weighted scores
+ * and the gradient of the state that dx reads (2^-8 of a term), the weighted
+ * products of dy and x that dB and dC read (2^-16).  The gradients of dt and of
+ * the per-head parameters are fp32 and fp64 sums.  Inputs and dy are meant to be
+ * finite: NaN in one token may reach the gradients of the 64-token tile around
+ * it.  B, n, G and the heads a group has must fit a launch (2^32 threads, 512
+ * for every 64 tokens, group and subset of a group's heads).
  * workspace: at least hla_ssm_backward_workspace_bytes(...) bytes (two states
  * for every 64 tokens of a head). */
 size_t hla_ssm_backward_workspace_bytes(int B, int n, int H, int P, int G, int N, int dtype);

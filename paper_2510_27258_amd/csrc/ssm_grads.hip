@@ -21,13 +21,20 @@
 // heads that share its B and C: C B^T is formed once, the heads' M dt V are
 // summed before they meet B and C, and dB and dC stay in accumulators over the
 // heads.  h and g are kept and enter their products to 24 bits (three pieces):
-// dA and d dt_bias are sums of either sign over every token, and with two
-// pieces (2^-17) they were 2.6e-6 off 64 bits instead of 1.8e-6, for 1 % of the time.
+// dA is a sum of either sign over every token, and with two pieces (2^-17) it
+// was 2.6e-6 off 64 bits instead of 1.8e-6, for 1 % of the time.  What is left
+// (1.7e-6 on 4 x 4096 tokens, 1.8e-7 with fp32 products on vector units) is an
+// offset of one sign, 1e-7 of a tile's terms, that adds up over tokens where
+// the terms themselves cancel.  It is there only where h and g take part; fp64
+// sums of E, F and <g, h>, exact exponentials or another order of the pieces'
+// products hardly change it.
+// dx takes g and the weighted scores in one piece, 2^-8 of a term (0.0017 off).
 //
 // Measured on 4 x 4096 tokens of 16 heads of 64 x 128 (us): the walks both ways
 // to the segments' ends 33, their states 89 (268 MB written, 3.0 TB/s), this
-// kernel 113 (268 MB of states read; with four waves a workgroup of two row
-// blocks each, before its loads were moved ahead, 253), the last sums 5.
+// kernel 117 (268 MB of states read; 113 with R and K in fp32; with four waves a
+// workgroup of two row blocks each, before its loads were moved ahead, 253), the
+// last sums 5.
 #include "ssm_walk.h"
 
 namespace hla {
@@ -119,7 +126,8 @@ __global__ __launch_bounds__(kGThreads, 2) void k_ssm_grads(GradArgs a) {
   constexpr bool kAhead = PP <= 64;
   // The next head's tiles wait until the states' products are done where those
   // fill the registers (P = N = 128: 20 registers spilled instead of 37, 271 us
-  // instead of 310 on 4 x 4096 tokens of 16 heads); elsewhere nothing spills.
+  // instead of 310 on 4 x 4096 tokens of 16 heads, 279 since R and K are fp64);
+  // elsewhere nothing spills.
   constexpr bool kLate = PP > 64 && NN > 64;
   f32x4 hv[KP][2], gv[KP][2];
   auto rows_of = [&](const float* states, int head, f32x4 (&v)[KP][2]) {

@@ -12,17 +12,19 @@
 // scalar decay).  The state stays in MFMA accumulators for the whole walk;
 // k_ssm_steps makes each token's dt, L and weights once for all walks.
 //
-// Measured in bf16 (us): 2 x 16384 tokens of 32 heads of 128 x 128 335: ends 94
-// (seven of eight segments), outputs 246, steps 11, sums of the ends 10.  A
-// prompt of 8000 tokens of 32 heads 123: ends 36, outputs 75, sums 13, steps 6.
-// Floors by bytes: 108 and 27.
+// Measured in bf16 (us): a call over 2 x 16384 tokens of 32 heads of 128 x 128
+// 335 to 350, over a prompt of 8000 tokens of 32 heads 113 to 123.  Floors by
+// bytes: 108 and 27.  Kernel by kernel under the profiler, where each is slower
+// than in the call (their sums exceed it): of the first the ends 95 (seven of
+// eight segments), outputs 253, steps 11, sums of the ends 10; of the second 35,
+// 75, 5 and 13.
 // What bounds it: no one unit.  The outputs' walk of the first keeps vector
-// instructions busy 52 % of the time, LDS 61 % (42 % of that conflicts) and the
-// matrix cores 26 %; waves wait for memory or barriers 48 % of theirs.  In
+// instructions busy 53 % of the time, LDS 61 % (41 % of that conflicts) and the
+// matrix cores 25 %; waves wait for memory or barriers 48 % of theirs.  In
 // copies of a somewhat slower version (276 us) without loads and stores it took
 // 212, without the products 197, without both 107 (staging, weights, barriers):
 // two workgroups a CU overlap these only in part.
-// Tried and not kept, on the first: half as many waves with twice the columns
+// Tried and not kept, on calls of the first: half as many waves with twice the columns
 // 361 (against 347-353), two tiles of loads ahead for the shorter walks 340
 // (340), the update at a higher wave priority 326-340 (332-350).
 #include "ssm_walk.h"

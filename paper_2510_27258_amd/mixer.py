@@ -5,7 +5,9 @@ selective state space scan.
 torch supplies device memory and the current HIP stream; the computation runs
 in libhla.so.  Activations are [B, n, ...] views with any strides between
 batches and tokens, such as slices of a projection's output; outputs are new
-contiguous tensors.
+contiguous tensors.  short_conv, qk_norm_rope and ssm_scan are differentiable
+once, in reverse mode: forward mode, function transforms and second derivatives
+are refused.
 """
 import torch
 import torch.autograd.forward_ad as _forward_ad
