@@ -13,7 +13,7 @@
 // k_ssm_steps makes each token's dt, L and weights once for all walks.
 //
 // Measured in bf16 (us): a call over 2 x 16384 tokens of 32 heads of 128 x 128
-// 335 to 350, over a prompt of 8000 tokens of 32 heads 113 to 123.  Floors by
+// 333 to 350, over a prompt of 8000 tokens of 32 heads 113 to 123.  Floors by
 // bytes: 108 and 27.  Kernel by kernel under the profiler, where each is slower
 // than in the call (their sums exceed it): of the first the ends 95 (seven of
 // eight segments), outputs 253, steps 11, sums of the ends 10; of the second 35,
