@@ -105,9 +105,9 @@ def _out(out, shape, like, name="out"):
 
 
 def _space(nbytes, device, workspace=None):
-    if nbytes == 0:
-        raise capi.HLAError(capi.HLA_ERR_INVALID, capi.hla_last_error())
-    if workspace is None:
+    """A workspace of nbytes; none for sizes that the query refuses (0), which
+    the entry refuses with its own code before it looks at the workspace."""
+    if workspace is None or nbytes == 0:
         return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")

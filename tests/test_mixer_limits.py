@@ -88,3 +88,28 @@ def test_heads_of_a_step(B, H, fits):
     rc = capi.lib().hla_ssm_step(P, P, H * 16, P, H, P, P, 16, P, 16, None, None, None, B, H, 16, 1, 16, 1, BF16, BF16, None)
     _refused(rc, *((INVALID, "y is NULL") if fits else (UNSUP, "B*H")))
     assert capi.hla_ssm_workspace_bytes(2048, 1, 32, 16, 1, 16, BF16) == 0 and "65535" in capi.hla_last_error()
+
+
+def test_the_binding_keeps_the_librarys_error_codes(monkeypatch):
+    """Sizes whose workspace query refuses them: the error has the entry's code, not one of its own."""
+    import torch
+
+    from paper_2510_27258_amd import mixer
+    monkeypatch.setattr(mixer, "_on_gpu", lambda t: None)
+    monkeypatch.setattr(mixer, "_launch", lambda entry, t, *args: entry(*args, None))
+
+    def z(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype)
+
+    def scan(P, dtype=torch.bfloat16):
+        return z(1, 4, 2, P, dtype=dtype), z(1, 4, 2), z(2, dtype=torch.float32), z(1, 4, 1, 16, dtype=dtype), z(1, 4, 1, 16,
+                                                                                                            dtype=dtype)
+    wide, fp32 = scan(24), scan(16, torch.float32)
+    for code, text, call in ((UNSUP, "P and N", lambda: mixer.ssm_forward(*wide)),
+                             (UNSUP, "P and N", lambda: mixer.ssm_backward(*wide, None, None, wide[0])),
+                             (UNSUP, "bf16", lambda: mixer.ssm_backward(*fp32, None, None, fp32[0])),
+                             (UNSUP, "K must be", lambda: mixer.conv_backward(z(1, 4, 8), z(8, 5), None, z(1, 4, 8))),
+                             (INVALID, "B, n and D", lambda: mixer.conv_backward(z(1, 0, 8), z(8, 4), None, z(1, 0, 8)))):
+        with pytest.raises(capi.HLAError) as e:
+            call()
+        assert e.value.code == code and text in str(e.value), (code, str(e.value))
