@@ -81,6 +81,9 @@ typedef enum {
 
 typedef enum { HLA_FP32 = 0, HLA_BF16 = 1 } hla_dtype;
 
+/* Activation of a gated projection. */
+typedef enum { HLA_ACT_SILU = 0, HLA_ACT_GELU = 1 } hla_act;
+
 /* Forward algorithms selectable through hla2_forward_ex. */
 typedef enum {
   HLA_ALGO_AUTO = 0,     /* library choice (fused when supported)             */
@@ -483,6 +486,112 @@ int hla_ssm_backward(const void *x, long long x_bs, long long x_ts, const void *
                      void *dBm, void *dCm, float *dD, float *ddt_bias, int B, int n, int H, int P, int G,
                      int N, int softplus, int dtype, int dt_dtype, void *workspace, size_t workspace_bytes,
                      void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The operators of a block around its mixer.  Activations, outputs, gradients
+ * and optional pointers as for the operators around the attention; pointers
+ * need the alignment of their type unless said otherwise, and 16-byte rows are
+ * faster.  B*n < 2^31.
+ * ------------------------------------------------------------------------- */
+
+/* hla_gated_norm — the norm of a mixer's output with its gate, over the d
+ * elements of a group (a head, or with G = 1 the whole token):
+ *   norm_first = 0:  v = y z sigmoid(z),  out = w v / sqrt(mean v^2 + eps)
+ *   norm_first = 1:  out = w y / sqrt(mean y^2 + eps) z sigmoid(z)
+ * y [B, n, G, d] of y_dtype and z (optional: no gate) of dtype, any strides
+ * >= 0 between batches, tokens and groups (_bs, _ts, _gs); weight (optional:
+ * ones) of w_dtype, [d] or with per_group = 1 [G, d]; out [B, n, G, d] of dtype.
+ * y_dtype is dtype or HLA_FP32.  d <= 16384, G <= 65535, eps finite and >= 0. */
+int hla_gated_norm(const void *y, long long y_bs, long long y_ts, long long y_gs, const void *z, long long z_bs,
+                   long long z_ts, long long z_gs, const void *weight, void *out, int B, int n, int G, int d,
+                   int per_group, int norm_first, float eps, int y_dtype, int dtype, int w_dtype, void *stream);
+
+/* hla_gated_norm_backward — its gradients for dout [B, n, G, d]: dy of y_dtype
+ * with strides of its own (rows that do not overlap), dz [B, n, G, d] (unused
+ * without a z), dweight (optional) like weight, an fp32 sum over tokens (and
+ * groups) in a fixed order.  workspace: at least
+ * hla_gated_norm_backward_workspace_bytes(...) bytes. */
+size_t hla_gated_norm_backward_workspace_bytes(int B, int n, int G, int d, int per_group);
+int hla_gated_norm_backward(const void *y, long long y_bs, long long y_ts, long long y_gs, const void *z,
+                            long long z_bs, long long z_ts, long long z_gs, const void *weight, const void *dout,
+                            void *dy, long long dy_bs, long long dy_ts, long long dy_gs, void *dz, void *dweight,
+                            int B, int n, int G, int d, int per_group, int norm_first, float eps, int y_dtype,
+                            int dtype, int w_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* hla_residual_norm — the residual addition with the norms on both sides:
+ *   u = y, or with post_weight (optional) post_weight y / sqrt(mean y^2 + eps)
+ *   r = x + alpha scale u,  out = weight r / sqrt(mean r^2 + eps)
+ * x [B, n, D] (the residual stream) and r of x_dtype, y (a block's output) and
+ * out of dtype; weight, post_weight, scale [D] of w_dtype, each optional
+ * (weight and scale: ones).  out is made from r before its rounding.  x_dtype
+ * is dtype or HLA_FP32.  D <= 16384, alpha finite, eps finite and >= 0. */
+int hla_residual_norm(const void *x, long long x_bs, long long x_ts, const void *y, long long y_bs, long long y_ts,
+                      const void *weight, const void *post_weight, const void *scale, void *out, void *r, int B,
+                      int n, int D, float alpha, float eps, int x_dtype, int dtype, int w_dtype, void *stream);
+
+/* hla_residual_norm_backward — its gradients for dout [B, n, D] of dtype and dr
+ * [B, n, D] of x_dtype (each optional, not both: no gradient): dx of x_dtype, dy
+ * of dtype, and (optional) dweight, dpost_weight, dscale [D] of w_dtype, fp32
+ * sums over the tokens in a fixed order.  workspace: at least
+ * hla_residual_norm_backward_workspace_bytes(...) bytes. */
+size_t hla_residual_norm_backward_workspace_bytes(int B, int n, int D);
+int hla_residual_norm_backward(const void *x, long long x_bs, long long x_ts, const void *y, long long y_bs,
+                               long long y_ts, const void *weight, const void *post_weight, const void *scale,
+                               const void *dout, const void *dr, void *dx, void *dy, void *dweight,
+                               void *dpost_weight, void *dscale, int B, int n, int D, float alpha, float eps,
+                               int x_dtype, int dtype, int w_dtype, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* hla_glr_forward — gated linear recurrence of every channel:
+ *   r = sigmoid(f + f_bias), i = sigmoid(g + g_bias), a = exp(-c softplus(decay) r)
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,  y_t = h_t
+ * x, f, g [B, n, D] of dtype; decay, f_bias, g_bias (the biases optional) fp32
+ * [D]; y [B, n, D] of dtype.  state (optional) fp32 [B, D]: the state before
+ * the first token, replaced by that after the last; without it zeros.  kept
+ * (optional): hla_glr_kept_bytes(...) bytes for what the gradients need of the
+ * forward.  c finite and >= 0, D <= 2^24.  An infinite or NaN input leaves the
+ * outputs of its channel from its token on infinite or NaN, and no other.
+ * workspace: at least hla_glr_workspace_bytes(...) bytes. */
+size_t hla_glr_workspace_bytes(int B, int n, int D);
+size_t hla_glr_kept_bytes(int B, int n, int D);
+int hla_glr_forward(const void *x, long long x_bs, long long x_ts, const void *f, long long f_bs, long long f_ts,
+                    const void *g, long long g_bs, long long g_ts, const float *decay, const float *f_bias,
+                    const float *g_bias, float *state, void *y, float *kept, int B, int n, int D, float c, int dtype,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* hla_glr_step — one token of it for every sequence, the state updated in
+ * place: x, f, g, y [B, D]; strides between batches only.  No workspace. */
+int hla_glr_step(float *state, const void *x, long long x_bs, const void *f, long long f_bs, const void *g,
+                 long long g_bs, const float *decay, const float *f_bias, const float *g_bias, void *y, int B, int D,
+                 float c, int dtype, void *stream);
+
+/* hla_glr_backward — gradients of hla_glr_forward without a state, for dy
+ * [B, n, D] and what the forward kept: dx, df, dg [B, n, D] of dtype, fp32 [D]
+ * ddecay, df_bias, dg_bias (the biases' optional).  workspace: at least
+ * hla_glr_backward_workspace_bytes(...) bytes. */
+size_t hla_glr_backward_workspace_bytes(int B, int n, int D);
+int hla_glr_backward(const void *x, long long x_bs, long long x_ts, const void *f, long long f_bs, long long f_ts,
+                     const void *g, long long g_bs, long long g_ts, const float *decay, const float *f_bias,
+                     const float *g_bias, const float *kept, const void *dy, long long dy_bs, long long dy_ts,
+                     void *dx, void *df, void *dg, float *ddecay, float *df_bias, float *dg_bias, int B, int n, int D,
+                     float c, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* hla_glu_forward — gated feed-forward projections
+ *   h = act(x w_gate^T) * (x w_up^T),  act SiLU or GELU (by the error function)
+ * x [B, n, D], w_gate, w_up [F, D], h [B, n, F], all bf16 (dtype = HLA_BF16;
+ * fp32 returns HLA_ERR_UNSUPPORTED), sums in fp32, rounded once.  D and F are
+ * multiples of 8, at most 2^20; addresses and strides whole 16-byte pieces. */
+int hla_glu_forward(const void *x, long long x_bs, long long x_ts, const void *w_gate, const void *w_up, void *h,
+                    int B, int n, int D, int F, int act, int dtype, void *stream);
+
+/* hla_glu_backward — its gradients for dh [B, n, F] (strides as x's): dx
+ * [B, n, D], dw_gate, dw_up [F, D].  The gradients of the two projections are
+ * rounded to bf16 before they meet weights and inputs (2^-9 of a term).
+ * workspace: at least hla_glu_backward_workspace_bytes(...) bytes. */
+size_t hla_glu_backward_workspace_bytes(int B, int n, int D, int F);
+int hla_glu_backward(const void *x, long long x_bs, long long x_ts, const void *w_gate, const void *w_up,
+                     const void *dh, long long dh_bs, long long dh_ts, void *dx, void *dw_gate, void *dw_up, int B,
+                     int n, int D, int F, int act, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
  * Benchmark timing.  hla_profile_begin(max_records) creates 2*max_records HIP

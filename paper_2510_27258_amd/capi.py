@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libhla.so")
 
 HLA_OK, HLA_ERR_INVALID, HLA_ERR_UNSUPPORTED, HLA_ERR_WORKSPACE, HLA_ERR_HIP = range(5)
 HLA_FP32, HLA_BF16 = 0, 1
+HLA_ACT_SILU, HLA_ACT_GELU = 0, 1
 HLA_ALGO_AUTO, HLA_ALGO_CHUNKED, HLA_ALGO_FUSED = 0, 1, 2
 
 _lib = None
@@ -34,6 +35,7 @@ class HLA2State(ctypes.Structure):
 _SP = ctypes.POINTER(HLA2State)
 _ZP = ctypes.POINTER(_Z)
 _ROWS = [_P, _L, _L]      # a row-strided tensor: address, elements between batches, between tokens
+_ROWS3 = [_P, _L, _L, _L]  # address, elements between batches, tokens, groups
 _IP = ctypes.POINTER(_I)
 
 _SIGS = {
@@ -80,6 +82,22 @@ _SIGS = {
     "hla_ssm_backward_workspace_bytes": (_Z, [_I] * 7),
     "hla_ssm_backward": (_I, _ROWS * 2 + [_P] + _ROWS * 2 + [_P] * 2 + _ROWS + [_P] * 7 + [_I] * 9 + [_P, _Z, _P]),
     "hla_ssm_step": (_I, [_P] + [_P, _L] * 2 + [_P] + [_P, _L] * 2 + [_P] * 3 + [_I] * 8 + [_P]),
+    "hla_gated_norm": (_I, _ROWS3 * 2 + [_P] * 2 + [_I] * 6 + [_F] + [_I] * 3 + [_P]),
+    "hla_gated_norm_backward_workspace_bytes": (_Z, [_I] * 5),
+    "hla_gated_norm_backward": (_I, _ROWS3 * 2 + [_P] * 2 + _ROWS3 + [_P] * 2 + [_I] * 6 + [_F] + [_I] * 3 +
+                                [_P, _Z, _P]),
+    "hla_residual_norm": (_I, _ROWS * 2 + [_P] * 5 + [_I] * 3 + [_F] * 2 + [_I] * 3 + [_P]),
+    "hla_residual_norm_backward_workspace_bytes": (_Z, [_I] * 3),
+    "hla_residual_norm_backward": (_I, _ROWS * 2 + [_P] * 10 + [_I] * 3 + [_F] * 2 + [_I] * 3 + [_P, _Z, _P]),
+    "hla_glr_workspace_bytes": (_Z, [_I] * 3),
+    "hla_glr_kept_bytes": (_Z, [_I] * 3),
+    "hla_glr_forward": (_I, _ROWS * 3 + [_P] * 6 + [_I] * 3 + [_F, _I, _P, _Z, _P]),
+    "hla_glr_step": (_I, [_P] + [_P, _L] * 3 + [_P] * 4 + [_I] * 2 + [_F, _I, _P]),
+    "hla_glr_backward_workspace_bytes": (_Z, [_I] * 3),
+    "hla_glr_backward": (_I, _ROWS * 3 + [_P] * 4 + _ROWS + [_P] * 6 + [_I] * 3 + [_F, _I, _P, _Z, _P]),
+    "hla_glu_forward": (_I, _ROWS + [_P] * 3 + [_I] * 6 + [_P]),
+    "hla_glu_backward_workspace_bytes": (_Z, [_I] * 4),
+    "hla_glu_backward": (_I, _ROWS + [_P] * 2 + _ROWS + [_P] * 3 + [_I] * 6 + [_P, _Z, _P]),
 }
 
 
@@ -292,6 +310,67 @@ def hla_ssm_backward(*args):
 
 def hla_ssm_step(*args):
     return _call("hla_ssm_step", *args)
+
+
+# The operators of a block, likewise.
+def hla_gated_norm(*args):
+    return _call("hla_gated_norm", *args)
+
+
+def hla_gated_norm_backward_workspace_bytes(B, n, G, d, per_group):
+    return lib().hla_gated_norm_backward_workspace_bytes(B, n, G, d, per_group)
+
+
+def hla_gated_norm_backward(*args):
+    return _call("hla_gated_norm_backward", *args)
+
+
+def hla_residual_norm(*args):
+    return _call("hla_residual_norm", *args)
+
+
+def hla_residual_norm_backward_workspace_bytes(B, n, D):
+    return lib().hla_residual_norm_backward_workspace_bytes(B, n, D)
+
+
+def hla_residual_norm_backward(*args):
+    return _call("hla_residual_norm_backward", *args)
+
+
+def hla_glr_workspace_bytes(B, n, D):
+    return lib().hla_glr_workspace_bytes(B, n, D)
+
+
+def hla_glr_kept_bytes(B, n, D):
+    return lib().hla_glr_kept_bytes(B, n, D)
+
+
+def hla_glr_forward(*args):
+    return _call("hla_glr_forward", *args)
+
+
+def hla_glr_step(*args):
+    return _call("hla_glr_step", *args)
+
+
+def hla_glr_backward_workspace_bytes(B, n, D):
+    return lib().hla_glr_backward_workspace_bytes(B, n, D)
+
+
+def hla_glr_backward(*args):
+    return _call("hla_glr_backward", *args)
+
+
+def hla_glu_forward(*args):
+    return _call("hla_glu_forward", *args)
+
+
+def hla_glu_backward_workspace_bytes(B, n, D, F):
+    return lib().hla_glu_backward_workspace_bytes(B, n, D, F)
+
+
+def hla_glu_backward(*args):
+    return _call("hla_glu_backward", *args)
 
 
 def hla_profile_begin(max_records):

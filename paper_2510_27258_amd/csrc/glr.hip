@@ -1,0 +1,606 @@
+// Gated linear recurrence, channel by channel:
+//   r = sigmoid(f + fb), i = sigmoid(g + gb), L = -c softplus(decay) r, a = e^L
+//   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,  y_t = h_t
+// and its gradients, with l_t = dy_t + a_{t+1} l_{t+1} that of h_t:
+//   dL = l (a h_{t-1} - i x a^2 / sqrt(1 - a^2)),  dx = l sqrt(1 - a^2) i,
+//   dg = l sqrt(1 - a^2) x i (1 - i),  df = dL L (1 - r),
+//   ddecay = sum dL (-c) r sigmoid(decay).
+//
+// A span of tokens acts on the state as h -> A h + H, and spans join: a thread
+// takes S neighbouring tokens of V channels, a wave 64 / LPR such runs below
+// one another (LPR lanes a token's CB = V LPR channels), W waves a tile.  Runs
+// join by lane moves within a wave and through LDS between waves, then every
+// thread goes over its tokens again from its true state, all from registers:
+// inputs are read once.  The next tile's loads are in flight meanwhile.  Where
+// the channel blocks of all sequences leave CUs empty, sequences are cut into
+// segments: a first launch brings each segment's A and H (or, backwards, its
+// effect on l), and every segment of the second joins what lies before it.
+// 1 - a^2 is taken as -expm1(2 L): a state that keeps 0.999 of itself a token
+// would lose ten bits of it to the difference.
+#include <cmath>
+
+#include "block.h"
+#include "lanes.h"
+#include "vec.h"
+
+namespace hla {
+namespace {
+
+// V values of one token as they lie in memory.
+template <typename T, int V>
+struct Few {
+  static constexpr int N = V * sizeof(T) / 4 ? V * sizeof(T) / 4 : 1;
+  uint32_t w[N];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (N == 2) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      w[0] = u.x;
+      w[1] = u.y;
+    } else if constexpr (sizeof(T) * V == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = (uint32_t) reinterpret_cast<const uint16_t*>(p)[0] << 16;
+    }
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4 || V == 1)
+      return __uint_as_float(w[i]);
+    else
+      return __uint_as_float(i ? w[0] & 0xffff0000u : w[0] << 16);
+  }
+};
+template <typename T, int V>
+__device__ __forceinline__ void store_few(T* p, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (V == 2)
+      *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    else
+      *p = v[0];
+  } else if constexpr (V == 2) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<uint32_t*>(p) = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[0], v[1]}, b2));
+  } else {
+    p->bits = to_bf16(v[0]);
+  }
+}
+
+constexpr float kLog2e = 1.44269504f;
+
+__device__ __forceinline__ float sigm(float v) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
+}
+
+// A channel's constants.
+struct Channel {
+  float k;        // -c softplus(decay)
+  float fb, gb;
+};
+__device__ __forceinline__ float softplus(float d) { return fmaxf(d, 0.f) + log1pf(expf(-fabsf(d))); }
+__device__ __forceinline__ Channel channel(const Glr& p, int c) {
+  return {-p.c * softplus(p.decay[c]), p.fb ? p.fb[c] : 0.f, p.gb ? p.gb[c] : 0.f};
+}
+
+// 1 - e^(2 L) for L <= 0, a = e^L: its series to 2^-26 below 2 |L| = 1/2, the difference above.
+__device__ __forceinline__ float one_minus_square(float L, float a) {
+  const float u = -2.f * L;
+  float s = fmaf(u, -1.f / 40320, 1.f / 5040);
+  s = fmaf(u, s, -1.f / 720);
+  s = fmaf(u, s, 1.f / 120);
+  s = fmaf(u, s, -1.f / 24);
+  s = fmaf(u, s, 1.f / 6);
+  s = fmaf(u, s, -0.5f);
+  s = fmaf(u * u, s, u);
+  return u < 0.5f ? s : fmaf(-a, a, 1.f);
+}
+
+struct Gates {
+  float r, i, L, a, om;
+};
+__device__ __forceinline__ Gates gates(const Channel& ch, float f, float g) {
+  Gates o;
+  o.r = sigm(f + ch.fb);
+  o.i = sigm(g + ch.gb);
+  o.L = ch.k * o.r;
+  o.a = __builtin_amdgcn_exp2f(kLog2e * o.L);
+  o.om = one_minus_square(o.L, o.a);
+  return o;
+}
+
+// How a launch is cut: channel blocks, sequences, segments of `tiles` tiles.
+struct Cut {
+  int blocks, segs, tiles;
+};
+
+// A workgroup's place.  Workgroups go to the 8 XCDs in turn; neighbouring
+// channel blocks, which share cache lines, are given to one XCD.
+struct Spot {
+  int c0, b, seg;
+};
+__device__ __forceinline__ Spot spot(const Cut& cut, int B, int CB) {
+  const unsigned total = gridDim.x, x = blockIdx.x & 7, k = blockIdx.x >> 3;
+  const unsigned per = total >> 3, more = total & 7;
+  const unsigned id = x * per + min(x, more) + k;
+  const unsigned rest = id / cut.blocks;
+  return {(int)(id - rest * cut.blocks) * CB, (int)(rest % B), (int)(rest / B)};
+}
+
+// The maps v -> A v + M of a wave's runs joined: ex* = what the runs before
+// (UP) or behind (!UP) this lane's do, all* = the whole wave's, in the lanes of
+// its last run in that direction.
+template <int LPR, int V, bool UP>
+__device__ __forceinline__ void join_wave(const float (&A)[V], const float (&M)[V], float (&exA)[V], float (&exM)[V],
+                                          float (&allA)[V], float (&allM)[V]) {
+  constexpr int RW = 64 / LPR;
+  const int row = (threadIdx.x & 63) / LPR, at = UP ? row : RW - 1 - row;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float a = A[v], m = M[v];
+#pragma unroll
+    for (int k = 1; k < RW; k *= 2) {
+      const float pa = UP ? __shfl_up(a, k * LPR) : __shfl_down(a, k * LPR);
+      const float pm = UP ? __shfl_up(m, k * LPR) : __shfl_down(m, k * LPR);
+      if (at >= k) {
+        m = fmaf(a, pm, m);
+        a *= pa;
+      }
+    }
+    allA[v] = a;
+    allM[v] = m;
+    const float pa = UP ? __shfl_up(a, LPR) : __shfl_down(a, LPR);
+    const float pm = UP ? __shfl_up(m, LPR) : __shfl_down(m, LPR);
+    exA[v] = at ? pa : 1.f;
+    exM[v] = at ? pm : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Forward.  ENDS: only a segment's A and H, to sums [seg][B][D] (A, H); the
+// first segment's launch also keeps the state at `first` [B][D], which the
+// last segment of the second launch replaces.
+template <typename T, int V, int LPR, int S, int W, bool ENDS>
+__global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restrict__ sums, float* __restrict__ first) {
+  constexpr int CB = V * LPR, RW = 64 / LPR, TILE = S * RW * W;
+  __shared__ float2 join[2][W][CB];
+  const Spot at = spot(cut, p.B, CB);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR;
+  const bool mine = at.c0 + lane % LPR * V < p.D;
+  const int c = mine ? at.c0 + lane % LPR * V : 0;
+  const T* x = static_cast<const T*>(p.x.p) + (size_t)at.b * p.x.bs + c;
+  const T* f = static_cast<const T*>(p.f.p) + (size_t)at.b * p.f.bs + c;
+  const T* g = static_cast<const T*>(p.g.p) + (size_t)at.b * p.g.bs + c;
+  Channel ch[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) ch[v] = channel(p, c + v);
+
+  // the state before this segment
+  float carry[V], through[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const size_t s0 = (size_t)at.b * p.D + c + v;
+    through[v] = 1.f;
+    carry[v] = 0.f;
+    if constexpr (ENDS) {
+      if (at.seg == 0 && wave == 0 && row == 0 && mine) first[s0] = p.state ? p.state[s0] : 0.f;
+    } else {
+      carry[v] = cut.segs > 1 ? first[s0] : p.state ? p.state[s0] : 0.f;
+      for (int s = 0; s < at.seg; ++s) {
+        const float2 m = sums[(size_t)s * p.B * p.D + s0];
+        carry[v] = fmaf(m.x, carry[v], m.y);
+      }
+    }
+  }
+
+  const long long t_first = (long long)at.seg * cut.tiles * TILE;
+  const int tiles = (int)min((long long)cut.tiles, (p.n - t_first + TILE - 1) / TILE);
+  Few<T, V> rx[S], rf[S], rg[S];
+  auto load = [&](long long t0) {
+    const long long t = t0 + (wave * RW + row) * S;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const long long u = min(t + s, (long long)p.n - 1);
+      rx[s].load(x + u * p.x.ts);
+      rf[s].load(f + u * p.f.ts);
+      rg[s].load(g + u * p.g.ts);
+    }
+  };
+  load(t_first);
+  for (int k = 0; k < tiles; ++k) {
+    const long long t0 = t_first + (long long)k * TILE, t = t0 + (wave * RW + row) * S;
+    float a[S][V], b[S][V], A[V], H[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      A[v] = 1.f;
+      H[v] = 0.f;
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const Gates o = gates(ch[v], rf[s].at(v), rg[s].at(v));
+        a[s][v] = o.a;
+        b[s][v] = __builtin_amdgcn_sqrtf(o.om) * o.i * rx[s].at(v);
+      }
+    if (t0 + TILE > p.n) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (t + s >= p.n) {
+            a[s][v] = 1.f;
+            b[s][v] = 0.f;
+          }
+    }
+    if (k + 1 < tiles) load(t0 + TILE);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] *= a[s][v];
+        H[v] = fmaf(a[s][v], H[v], b[s][v]);
+      }
+    float exA[V], exH[V], allA[V], allH[V];
+    join_wave<LPR, V, true>(A, H, exA, exH, allA, allH);
+    if (row == RW - 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) join[k & 1][wave][lane % LPR * V + v] = make_float2(allA[v], allH[v]);
+    }
+    lds_barrier();
+    float h[V];
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float2 m = join[k & 1][w][lane % LPR * V + v];
+        if (w == wave) h[v] = fmaf(exA[v], carry[v], exH[v]);
+        carry[v] = fmaf(m.x, carry[v], m.y);
+        if constexpr (ENDS) through[v] *= m.x;
+      }
+    if constexpr (!ENDS) {
+      if (p.kept && mine && t < p.n && t % kGlrTile == 0) {
+        float* to = p.kept + ((size_t)at.b * ((p.n + kGlrTile - 1) / kGlrTile) + t / kGlrTile) * p.D + c;
+#pragma unroll
+        for (int v = 0; v < V; ++v) to[v] = h[v];
+      }
+      T* y = static_cast<T*>(p.y) + ((size_t)at.b * p.n + t) * p.D + c;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = fmaf(a[s][v], h[v], b[s][v]);
+        if (mine && t + s < p.n) store_few<T, V>(y + (size_t)s * p.D, h);
+      }
+    }
+  }
+  if (wave != 0 || row != 0 || !mine) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const size_t s0 = (size_t)at.b * p.D + c + v;
+    if constexpr (ENDS)
+      sums[(size_t)at.seg * p.B * p.D + s0] = make_float2(through[v], carry[v]);
+    else if (p.state && at.seg == cut.segs - 1)
+      p.state[s0] = carry[v];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gradients.  The walk goes from the last tile to the first; the states before
+// its tiles were kept by the forward.  m_t = a_t l_t is what token t hands to
+// the one before it: a span acts on it as m -> A m + M.  ENDS: only a
+// segment's A and M.  part: the sums of the parameters' gradients over this
+// segment, [3][B segs][D], formed in fp64 across a thread's runs.
+template <typename T, int V, int LPR, int S, int W, bool ENDS>
+__global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __restrict__ sums, float* __restrict__ part) {
+  constexpr int CB = V * LPR, RW = 64 / LPR, TILE = S * RW * W;
+  static_assert(TILE % kGlrTile == 0, "a tile begins where a state is kept");
+  __shared__ float2 join[2][2][W][CB];
+  __shared__ double total[ENDS ? 1 : 3][W][CB];
+  const Spot at = spot(cut, p.B, CB);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR, q = lane % LPR * V;
+  const bool mine = at.c0 + q < p.D;
+  const int c = mine ? at.c0 + q : 0;
+  const T* x = static_cast<const T*>(p.x.p) + (size_t)at.b * p.x.bs + c;
+  const T* f = static_cast<const T*>(p.f.p) + (size_t)at.b * p.f.bs + c;
+  const T* g = static_cast<const T*>(p.g.p) + (size_t)at.b * p.g.bs + c;
+  const T* dy = static_cast<const T*>(p.dy.p) + (size_t)at.b * p.dy.bs + c;
+  Channel ch[V];
+  float carry[V], through[V];
+  double sum[3][V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    ch[v] = channel(p, c + v);
+    through[v] = 1.f;
+    carry[v] = 0.f;
+    sum[0][v] = sum[1][v] = sum[2][v] = 0.;
+    if constexpr (!ENDS) {
+      for (int s = cut.segs - 1; s > at.seg; --s) {
+        const float2 m = sums[((size_t)s * p.B + at.b) * p.D + c + v];
+        carry[v] = fmaf(m.x, carry[v], m.y);
+      }
+    }
+  }
+  const int kept = (p.n + kGlrTile - 1) / kGlrTile;
+  const long long t_first = (long long)at.seg * cut.tiles * TILE;
+  const int tiles = (int)min((long long)cut.tiles, (p.n - t_first + TILE - 1) / TILE);
+  Few<T, V> rx[S], rf[S], rg[S], ry[S];
+  float start[V];
+  auto load = [&](long long t0) {
+    const long long t = t0 + (wave * RW + row) * S;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const long long u = min(t + s, (long long)p.n - 1);
+      rf[s].load(f + u * p.f.ts);
+      ry[s].load(dy + u * p.dy.ts);
+      if constexpr (!ENDS) {
+        rx[s].load(x + u * p.x.ts);
+        rg[s].load(g + u * p.g.ts);
+      }
+    }
+    if constexpr (!ENDS) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) start[v] = p.kept[((size_t)at.b * kept + t0 / kGlrTile) * p.D + c + v];
+    }
+  };
+  load(t_first + (long long)(tiles - 1) * TILE);
+  for (int k = tiles - 1; k >= 0; --k) {
+    const long long t0 = t_first + (long long)k * TILE, t = t0 + (wave * RW + row) * S;
+    const bool whole = t0 + TILE <= p.n;
+    float a[S][V], r[S][V], in[S][V], om[S][V], xs[S][V], dys[S][V], A[V], H[V], M[V], st[V];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const bool there = whole || t + s < p.n;
+        const Gates o = gates(ch[v], rf[s].at(v), ENDS ? 0.f : rg[s].at(v));
+        a[s][v] = there ? o.a : 1.f;
+        dys[s][v] = there ? ry[s].at(v) : 0.f;
+        if constexpr (!ENDS) {
+          r[s][v] = o.r;
+          in[s][v] = o.i;
+          om[s][v] = there ? o.om : 0.f;
+          xs[s][v] = there ? rx[s].at(v) : 0.f;
+        }
+      }
+#pragma unroll
+    for (int v = 0; v < V; ++v) st[v] = start[v];
+    if (k > 0) load(t0 - TILE);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      A[v] = 1.f;
+      H[v] = M[v] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        A[v] *= a[s][v];
+        if constexpr (!ENDS) H[v] = fmaf(a[s][v], H[v], __builtin_amdgcn_sqrtf(om[s][v]) * in[s][v] * xs[s][v]);
+      }
+#pragma unroll
+      for (int s = S - 1; s >= 0; --s) M[v] = a[s][v] * (dys[s][v] + M[v]);
+    }
+    float exA[V], exH[V], bkA[V], bkM[V], all[V], allH[V], allM[V];
+    join_wave<LPR, V, false>(A, M, bkA, bkM, all, allM);
+    if (row == 0) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) join[k & 1][1][wave][q + v] = make_float2(all[v], allM[v]);
+    }
+    if constexpr (!ENDS) {
+      join_wave<LPR, V, true>(A, H, exA, exH, all, allH);
+      if (row == RW - 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) join[k & 1][0][wave][q + v] = make_float2(all[v], allH[v]);
+      }
+    }
+    lds_barrier();
+    float h[V], m[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+      for (int w = W - 1; w >= 0; --w) {
+        const float2 o = join[k & 1][1][w][q + v];
+        if (w == wave) m[v] = fmaf(bkA[v], carry[v], bkM[v]);
+        carry[v] = fmaf(o.x, carry[v], o.y);
+        if constexpr (ENDS) through[v] *= o.x;
+      }
+      if constexpr (!ENDS) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const float2 o = join[k & 1][0][w][q + v];
+          if (w == wave) h[v] = fmaf(exA[v], st[v], exH[v]);
+          st[v] = fmaf(o.x, st[v], o.y);
+        }
+      }
+    }
+    if constexpr (!ENDS) {
+      float before[S][V], run[3][V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        run[0][v] = run[1][v] = run[2][v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          before[s][v] = h[v];
+          h[v] = fmaf(a[s][v], h[v], __builtin_amdgcn_sqrtf(om[s][v]) * in[s][v] * xs[s][v]);
+        }
+      }
+      const size_t to = ((size_t)at.b * p.n + t) * p.D + c;
+#pragma unroll
+      for (int s = S - 1; s >= 0; --s) {
+        float dx[V], df[V], dg[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float l = dys[s][v] + m[v], root = __builtin_amdgcn_sqrtf(om[s][v]);
+          // where r = 0 the root is too, and L / root has the limit 0
+          const float inv = __builtin_amdgcn_rsqf(fmaxf(om[s][v], 1e-36f)), ix = in[s][v] * xs[s][v];
+          const float dL = l * (a[s][v] * before[s][v] - ix * (a[s][v] * (a[s][v] * inv)));
+          dx[v] = l * root * in[s][v];
+          dg[v] = l * root * ix * (1.f - in[s][v]);
+          df[v] = dL * (ch[v].k * r[s][v]) * (1.f - r[s][v]);
+          const bool there = whole || t + s < p.n;
+          run[0][v] += there ? dL * r[s][v] : 0.f;
+          run[1][v] += there ? df[v] : 0.f;
+          run[2][v] += there ? dg[v] : 0.f;
+          m[v] = a[s][v] * l;
+        }
+        if (mine && t + s < p.n) {
+          store_few<T, V>(static_cast<T*>(p.dx) + to + (size_t)s * p.D, dx);
+          store_few<T, V>(static_cast<T*>(p.df) + to + (size_t)s * p.D, df);
+          store_few<T, V>(static_cast<T*>(p.dg) + to + (size_t)s * p.D, dg);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) sum[j][v] += (double)run[j][v];
+    }
+  }
+  if constexpr (ENDS) {
+    if (wave == 0 && row == 0 && mine) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        sums[((size_t)at.seg * p.B + at.b) * p.D + c + v] = make_float2(through[v], carry[v]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int k = LPR; k < 64; k *= 2) sum[j][v] += __shfl_xor(sum[j][v], k);
+        if (row == 0) total[j][wave][q + v] = sum[j][v];
+      }
+    __syncthreads();
+    if (wave != 0 || row != 0 || !mine) return;
+    const size_t rows = (size_t)p.B * cut.segs, mr = (size_t)at.b * cut.segs + at.seg;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        double s = 0.;
+        for (int w = 0; w < W; ++w) s += total[j][w][q + v];
+        if (j == 0) s *= -p.c / (1. + exp(-(double)p.decay[c + v]));
+        part[((size_t)j * rows + mr) * p.D + c + v] = (float)s;
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// One token a sequence: a thread takes V channels.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_glr_step(Glr p) {
+  const unsigned per = (p.D + V - 1) / V;
+  for (unsigned long long id = blockIdx.x * 256ull + threadIdx.x; id < (unsigned long long)p.B * per;
+       id += gridDim.x * 256ull) {
+    const unsigned b = (unsigned)(id / per), c = (unsigned)(id - (unsigned long long)b * per) * V;
+    Few<T, V> x, f, g;
+    x.load(static_cast<const T*>(p.x.p) + (size_t)b * p.x.bs + c);
+    f.load(static_cast<const T*>(p.f.p) + (size_t)b * p.f.bs + c);
+    g.load(static_cast<const T*>(p.g.p) + (size_t)b * p.g.bs + c);
+    float* state = p.state + (size_t)b * p.D + c;
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Gates o = gates(channel(p, c + v), f.at(v), g.at(v));
+      h[v] = fmaf(o.a, state[v], __builtin_amdgcn_sqrtf(o.om) * o.i * x.at(v));
+      state[v] = h[v];
+    }
+    store_few<T, V>(static_cast<T*>(p.y) + (size_t)b * p.D + c, h);
+  }
+}
+
+// Pairs of channels where every row allows them.
+bool pairs(const Glr& p) {
+  const unsigned es = p.dtype == 1 ? 2 : 4, mask = 2 * es - 1;
+  auto fits = [&](const Rows& r) {
+    return !r.p || ((reinterpret_cast<uintptr_t>(r.p) & mask) == 0 && r.bs % 2 == 0 && r.ts % 2 == 0);
+  };
+  bool ok = p.D % 2 == 0 && fits(p.x) && fits(p.f) && fits(p.g) && fits(p.dy);
+  for (const void* q : {(const void*)p.y, (const void*)p.dx, (const void*)p.df, (const void*)p.dg})
+    ok = ok && (reinterpret_cast<uintptr_t>(q) & mask) == 0;
+  return ok;
+}
+
+constexpr int kFwdS = 16, kFwdW = 8, kBackS = 8, kBackW = 4;
+constexpr int kWant = 256;       // workgroups that fill the CUs
+constexpr int kMostSegs = 32;
+
+template <int V, int LPR, int S, int W>
+Cut cut_of(int B, int n, int D) {
+  constexpr int CB = V * LPR, TILE = S * (64 / LPR) * W;
+  const int blocks = (D + CB - 1) / CB;
+  const long long tiles = ((long long)n + TILE - 1) / TILE, have = (long long)blocks * B;
+  long long segs = have >= kWant ? 1 : (2 * kWant + have - 1) / have;
+  if (segs > kMostSegs) segs = kMostSegs;
+  if (segs > tiles / 2) segs = tiles / 2 > 1 ? tiles / 2 : 1;
+  const long long per = (tiles + segs - 1) / segs;
+  return {blocks, (int)((tiles + per - 1) / per), (int)per};
+}
+
+template <typename T, int V, int LPR>
+hipError_t forward(const Glr& p, void* ws, hipStream_t s) {
+  const Cut cut = cut_of<V, LPR, kFwdS, kFwdW>(p.B, p.n, p.D);
+  float* first = static_cast<float*>(ws);
+  float2* sums = reinterpret_cast<float2*>(first + (((size_t)p.B * p.D + 3) & ~(size_t)3));
+  const unsigned one = (unsigned)cut.blocks * p.B;
+  if (cut.segs > 1) {
+    const hipError_t e = HLA_TIMED("glr_ends", (k_glr<T, V, LPR, kFwdS, kFwdW, true>), dim3(one * (cut.segs - 1)),
+                                   dim3(64 * kFwdW), 0, s, p, cut, sums, first);
+    if (e != hipSuccess) return e;
+  }
+  return HLA_TIMED("glr", (k_glr<T, V, LPR, kFwdS, kFwdW, false>), dim3(one * cut.segs), dim3(64 * kFwdW), 0, s, p, cut,
+                   sums, first);
+}
+
+template <typename T, int V, int LPR>
+hipError_t backward(const Glr& p, void* ws, hipStream_t s) {
+  const Cut cut = cut_of<V, LPR, kBackS, kBackW>(p.B, p.n, p.D);
+  const size_t rows = (size_t)p.B * cut.segs;
+  float* part = static_cast<float*>(ws);
+  float2* sums = reinterpret_cast<float2*>(part + ((3 * rows * p.D + 3) & ~(size_t)3));
+  const unsigned one = (unsigned)cut.blocks * p.B;
+  if (cut.segs > 1) {
+    const hipError_t e = HLA_TIMED("glr_back_ends", (k_glr_back<T, V, LPR, kBackS, kBackW, true>), dim3(one * cut.segs),
+                                   dim3(64 * kBackW), 0, s, p, cut, sums, part);
+    if (e != hipSuccess) return e;
+  }
+  const hipError_t e = HLA_TIMED("glr_back", (k_glr_back<T, V, LPR, kBackS, kBackW, false>), dim3(one * cut.segs),
+                                 dim3(64 * kBackW), 0, s, p, cut, sums, part);
+  if (e != hipSuccess) return e;
+  return launch_column_sums({part, {p.ddecay, p.dfb, p.dgb}, (int)rows, p.D, 0}, s);
+}
+
+constexpr int kLpr = 8;
+
+}  // namespace
+
+size_t glr_forward_ws(int B, int n, int D) {
+  const int a = cut_of<1, kLpr, kFwdS, kFwdW>(B, n, D).segs, b = cut_of<2, kLpr, kFwdS, kFwdW>(B, n, D).segs;
+  return sizeof(float) * (size_t)B * D * (2 * (a > b ? a : b) + 1) + 64;
+}
+size_t glr_backward_ws(int B, int n, int D) {
+  const int a = cut_of<1, kLpr, kBackS, kBackW>(B, n, D).segs, b = cut_of<2, kLpr, kBackS, kBackW>(B, n, D).segs;
+  return sizeof(float) * (size_t)B * D * 5 * (a > b ? a : b) + 64;
+}
+
+double glr_threads(int B, int n, int D) {   // of the largest launch: one channel a lane, as many segments as there may be
+  const double blocks = std::ceil(D / (double)kLpr) * B;
+  const Cut f = cut_of<1, kLpr, kFwdS, kFwdW>(B, n, D), b = cut_of<1, kLpr, kBackS, kBackW>(B, n, D);
+  return blocks * std::fmax(f.segs * 64. * kFwdW, b.segs * 64. * kBackW);
+}
+
+hipError_t launch_glr_forward(const Glr& p, void* ws, hipStream_t s) {
+  if (p.dtype == 1) return pairs(p) ? forward<bf16, 2, kLpr>(p, ws, s) : forward<bf16, 1, kLpr>(p, ws, s);
+  return pairs(p) ? forward<float, 2, kLpr>(p, ws, s) : forward<float, 1, kLpr>(p, ws, s);
+}
+hipError_t launch_glr_backward(const Glr& p, void* ws, hipStream_t s) {
+  if (p.dtype == 1) return pairs(p) ? backward<bf16, 2, kLpr>(p, ws, s) : backward<bf16, 1, kLpr>(p, ws, s);
+  return pairs(p) ? backward<float, 2, kLpr>(p, ws, s) : backward<float, 1, kLpr>(p, ws, s);
+}
+hipError_t launch_glr_step(const Glr& p, hipStream_t s) {
+  const bool two = pairs(p);
+  const long long threads = (long long)p.B * ((p.D + two) / (1 + two)), blocks = (threads + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
+  if (p.dtype == 1)
+    return two ? HLA_TIMED("glr_step", (k_glr_step<bf16, 2>), grid, block, 0, s, p)
+               : HLA_TIMED("glr_step", (k_glr_step<bf16, 1>), grid, block, 0, s, p);
+  return two ? HLA_TIMED("glr_step", (k_glr_step<float, 2>), grid, block, 0, s, p)
+             : HLA_TIMED("glr_step", (k_glr_step<float, 1>), grid, block, 0, s, p);
+}
+
+}  // namespace hla

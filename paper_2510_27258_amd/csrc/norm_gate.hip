@@ -1,0 +1,287 @@
+// The norm of a mixer's output with its gate, over the d elements of a group
+// (a head, or the whole token):
+//   gate = z sigmoid(z),  v = y gate,  out = w v r         (the gate first)
+//                         v = y,       out = w v r gate    (norm_first)
+//   r = 1 / sqrt(mean v^2 + eps)
+// and its gradients, with hat = v r and g the incoming one (times the gate
+// where the norm comes first):
+//   dv = r (g w - hat mean(g w hat)),  dw = sum g hat,
+//   dz = (dv y or dout w hat) sigmoid(z) (1 + z (1 - sigmoid(z))).
+//
+// Bound by memory: every input is read once and every output written once.
+// A thread keeps its group and its elements of a row while its block goes over
+// the tokens, so the weight is loaded once and its gradient summed in registers.
+#include <initializer_list>
+
+#include "block.h"
+#include "rows.h"
+
+namespace hla {
+namespace {
+
+constexpr int kBlocks = 2048;       // of a forward, at most, a block of groups
+constexpr int kBackBlocks = 1024;   // of a backward, in all
+
+// A thread's place: slots of LANES threads take the block's groups, then its tokens.
+template <typename S>
+struct Place {
+  int lane, g, off, tokens;  // off: its token among the block's `tokens`
+  bool there;
+  __device__ __forceinline__ Place(int G) {
+    const int slot = threadIdx.x / S::LANES, per = min(G, S::ROWS);
+    lane = threadIdx.x % S::LANES;
+    tokens = S::ROWS / per;
+    off = slot / per;
+    g = blockIdx.y * per + slot % per;
+    there = off < tokens && g < G;
+  }
+};
+
+__device__ __forceinline__ size_t at(const Rows3& r, unsigned b, unsigned t, int g) {
+  return (size_t)b * r.bs + (size_t)t * r.ts + (size_t)g * r.gs;
+}
+
+template <typename TY, typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void k_gated_norm(GatedNorm a) {
+  __shared__ float red[2][1][S::WAVES];
+  constexpr bool kExact = sizeof(T) == 4;
+  const Place<S> p(a.G);
+  const unsigned toks = (unsigned)a.B * a.n;
+  float w[S::E];
+  load_weight<S>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
+  int turn = 0;
+  for (unsigned t0 = blockIdx.x; t0 * (unsigned long long)p.tokens < toks; t0 += gridDim.x, turn ^= 1) {
+    const unsigned long long tok = (unsigned long long)t0 * p.tokens + p.off;
+    const bool there = p.there && tok < toks;
+    const unsigned b = a.B > 1 ? (unsigned)tok / a.n : 0, t = (unsigned)tok - b * a.n;
+    const int d = there ? a.d : 0;
+    RowRaw<TY, S> y;
+    RowRaw<T, S> z;
+    y.load(static_cast<const TY*>(a.y.p) + (there ? at(a.y, b, t, p.g) : 0), d, p.lane);
+    if (a.z.p) z.load(static_cast<const T*>(a.z.p) + (there ? at(a.z, b, t, p.g) : 0), d, p.lane);
+    float v[S::E], gate[S::E], ss[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      v[e] = y.at(e);
+      if (a.z.p) {
+        gate[e] = z.at(e) * sigmoid<kExact>(z.at(e));
+        if (!a.norm_first) v[e] *= gate[e];
+      }
+      ss[0] += v[e] * v[e];
+    }
+    row_sums<S, 1>(ss, red[turn]);
+    const float r = 1.f / sqrtf(ss[0] / a.d + a.eps);
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      v[e] *= r * w[e];
+      if (a.z.p && a.norm_first) v[e] *= gate[e];
+    }
+    store_row<T, S>(static_cast<T*>(a.out) + (there ? ((size_t)tok * a.G + p.g) * a.d : 0), d, p.lane, v);
+  }
+}
+
+// Blocks keep their groups and take every gridDim.x-th share of the tokens; the
+// weight's partial sums: [grid.x][G][d] with a weight for each group, else
+// [grid.x grid.y][d], the block's rows summed in a fixed order.
+template <typename TY, typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, float* __restrict__ part) {
+  __shared__ float red[2][2][1][S::WAVES];
+  constexpr bool kExact = sizeof(TY) == 4;
+  const Place<S> p(a.G);
+  const unsigned toks = (unsigned)a.B * a.n;
+  float w[S::E], dw[S::E];
+  load_weight<S>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
+#pragma unroll
+  for (int e = 0; e < S::E; ++e) dw[e] = 0.f;
+  int turn = 0;
+  for (unsigned t0 = blockIdx.x; t0 * (unsigned long long)p.tokens < toks; t0 += gridDim.x, turn ^= 1) {
+    const unsigned long long tok = (unsigned long long)t0 * p.tokens + p.off;
+    const bool there = p.there && tok < toks;
+    const unsigned b = a.B > 1 ? (unsigned)tok / a.n : 0, t = (unsigned)tok - b * a.n;
+    const int d = there ? a.d : 0;
+    const size_t here = there ? ((size_t)tok * a.G + p.g) * a.d : 0;
+    RowRaw<TY, S> y;
+    RowRaw<T, S> z, go;
+    y.load(static_cast<const TY*>(a.y.p) + (there ? at(a.y, b, t, p.g) : 0), d, p.lane);
+    go.load(static_cast<const T*>(a.dout) + here, d, p.lane);
+    if (a.z.p) z.load(static_cast<const T*>(a.z.p) + (there ? at(a.z, b, t, p.g) : 0), d, p.lane);
+    float v[S::E], sig[S::E], ss[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      v[e] = y.at(e);
+      if (a.z.p) {
+        sig[e] = sigmoid<kExact>(z.at(e));
+        if (!a.norm_first) v[e] *= z.at(e) * sig[e];
+      }
+      ss[0] += v[e] * v[e];
+    }
+    row_sums<S, 1>(ss, red[turn][0]);
+    const float r = 1.f / sqrtf(ss[0] / a.d + a.eps);
+    float dot[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      v[e] *= r;                                   // hat from here on
+      const float g = a.z.p && a.norm_first ? go.at(e) * (z.at(e) * sig[e]) : go.at(e);
+      dot[0] += g * w[e] * v[e];
+      dw[e] += g * v[e];
+    }
+    row_sums<S, 1>(dot, red[turn][1]);
+    const float mean = dot[0] / a.d;
+    float dy[S::E], dz[S::E];
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float zz = a.z.p ? z.at(e) : 0.f, s = a.z.p ? sig[e] : 0.f, gate = a.z.p ? zz * s : 1.f;
+      const float g = a.norm_first ? go.at(e) * gate : go.at(e);
+      const float dv = r * (g * w[e] - v[e] * mean);
+      dy[e] = a.norm_first ? dv : dv * gate;
+      dz[e] = (a.norm_first ? go.at(e) * w[e] * v[e] : dv * y.at(e)) * (s * (1.f + zz * (1.f - s)));
+    }
+    store_row<TY, S>(static_cast<TY*>(const_cast<void*>(a.dy.p)) + (there ? at(a.dy, b, t, p.g) : 0), d, p.lane, dy);
+    if (a.z.p) store_row<T, S>(static_cast<T*>(a.dz) + here, d, p.lane, dz);
+  }
+  if (!a.dw) return;
+  if constexpr (S::ROWS == 1) {
+    float* to = part + (a.per_group ? (size_t)blockIdx.x * a.G + p.g : (size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.d;
+#pragma unroll
+    for (int ch = 0; ch < S::CH; ++ch)
+#pragma unroll
+      for (int i = 0; i < S::V; ++i) {
+        const int c = (ch * S::LANES + p.lane) * S::V + i;
+        if (c < a.d) to[c] = dw[ch * S::V + i];
+      }
+  } else {
+    __shared__ float sums[S::ROWS][S::LANES * S::E + 1];
+    const int per = min(a.G, S::ROWS), slot = threadIdx.x / S::LANES;
+#pragma unroll
+    for (int ch = 0; ch < S::CH; ++ch)
+#pragma unroll
+      for (int i = 0; i < S::V; ++i)
+        sums[slot][(ch * S::LANES + p.lane) * S::V + i] = p.there ? dw[ch * S::V + i] : 0.f;
+    __syncthreads();
+    if (a.per_group) {
+      for (int e = threadIdx.x; e < per * a.d; e += S::THREADS) {
+        const int k = e / a.d, c = e - k * a.d, g = blockIdx.y * per + k;
+        if (g >= a.G) continue;
+        float s = 0.f;
+        for (int o = 0; o < p.tokens; ++o) s += sums[o * per + k][c];
+        part[((size_t)blockIdx.x * a.G + g) * a.d + c] = s;
+      }
+    } else {
+      for (int c = threadIdx.x; c < a.d; c += S::THREADS) {
+        float s = 0.f;
+        for (int o = 0; o < S::ROWS; ++o) s += sums[o][c];
+        part[((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.d + c] = s;
+      }
+    }
+  }
+}
+
+constexpr int kSumRows = 64, kSumCols = 16;
+__global__ __launch_bounds__(kSumRows * kSumCols) void k_column_sums(ColumnSums c) {
+  __shared__ float red[kSumRows][kSumCols];
+  const int cl = threadIdx.x % kSumCols, rg = threadIdx.x / kSumCols, col = blockIdx.x * kSumCols + cl;
+  void* to = c.to[blockIdx.y];
+  if (!to) return;
+  const float* part = c.part + (size_t)blockIdx.y * c.rows * c.cols;
+  float s = 0.f;
+  if (col < c.cols)
+    for (int r = rg; r < c.rows; r += kSumRows) s += part[(size_t)r * c.cols + col];
+  red[rg][cl] = s;
+  __syncthreads();
+  if (rg != 0 || col >= c.cols) return;
+  for (int r = 1; r < kSumRows; ++r) s += red[r][cl];
+  store_any(to, c.dtype, col, s);
+}
+
+bool on_16(const void* p, int es, std::initializer_list<long long> strides) {
+  if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+  for (long long st : strides)
+    if (st * es % 16) return false;
+  return true;
+}
+bool on_16(const Rows3& r, int dtype) { return on_16(r.p, dtype == 1 ? 2 : 4, {r.bs, r.ts, r.gs}); }
+
+// Sequences laid one behind the other are one long one: no division by n.
+void flatten(GatedNorm& a) {
+  auto joined = [&](const Rows3& r) { return !r.p || a.n == 1 || r.bs == (long long)a.n * r.ts; };
+  if (a.B == 1) return;
+  if (a.n == 1) {   // a batch of single tokens is a sequence
+    auto turn = [](Rows3& r) { r.ts = r.bs; };
+    turn(a.y), turn(a.z), turn(a.dy);
+  } else if (!joined(a.y) || !joined(a.z) || !joined(a.dy)) {
+    return;
+  }
+  a.n *= a.B;
+  a.B = 1;
+}
+
+struct Grid {
+  int x, y;
+};
+template <typename S>
+Grid grid_of(int B, int n, int G, int most) {
+  const int per = G < S::ROWS ? G : S::ROWS, tokens = S::ROWS / per, gy = (G + per - 1) / per;
+  const long long shares = ((long long)B * n + tokens - 1) / tokens, x = most / gy > 1 ? most / gy : 1;
+  return {(int)(shares < x ? shares : x), gy};
+}
+
+template <typename TY, typename T, bool VEC>
+hipError_t forward(const GatedNorm& a, hipStream_t s) {
+  return by_row<VEC>(a.d, [&](auto shape) {
+    using S = decltype(shape);
+    const Grid g = grid_of<S>(a.B, a.n, a.G, kBlocks * ((a.G + S::ROWS - 1) / S::ROWS));
+    return HLA_TIMED("gated_norm", (k_gated_norm<TY, T, S>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a);
+  });
+}
+
+template <typename TY, typename T, bool VEC>
+hipError_t backward(const GatedNorm& a, float* part, hipStream_t s) {
+  Grid g{};
+  const hipError_t e = by_row<VEC>(a.d, [&](auto shape) {
+    using S = decltype(shape);
+    g = grid_of<S>(a.B, a.n, a.G, kBackBlocks);
+    return HLA_TIMED("gated_norm_back", (k_gated_norm_back<TY, T, S>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a, part);
+  });
+  if (e != hipSuccess || !a.dw) return e;
+  ColumnSums c{part, {a.dw, nullptr, nullptr}, a.per_group ? g.x : g.x * g.y, a.per_group ? a.G * a.d : a.d, a.w_dtype};
+  return launch_column_sums(c, s);
+}
+
+template <typename TY, typename T>
+hipError_t by_layout(GatedNorm a, bool back, float* part, hipStream_t s) {
+  flatten(a);
+  bool vec = a.d % 8 == 0 && on_16(a.y, a.y_dtype) && (!a.z.p || on_16(a.z, a.dtype));
+  if (back)
+    vec = vec && on_16(a.dy, a.y_dtype) && on_16(a.dout, 2, {}) && (!a.dz || on_16(a.dz, 2, {}));
+  else
+    vec = vec && on_16(a.out, 2, {});
+  if (back) return vec ? backward<TY, T, true>(a, part, s) : backward<TY, T, false>(a, part, s);
+  return vec ? forward<TY, T, true>(a, s) : forward<TY, T, false>(a, s);
+}
+
+hipError_t by_type(const GatedNorm& a, bool back, float* part, hipStream_t s) {
+  if (a.dtype == 0) return by_layout<float, float>(a, back, part, s);
+  return a.y_dtype == 0 ? by_layout<float, bf16>(a, back, part, s) : by_layout<bf16, bf16>(a, back, part, s);
+}
+
+}  // namespace
+
+hipError_t launch_column_sums(const ColumnSums& c, hipStream_t s) {
+  return HLA_TIMED("column_sums", k_column_sums, dim3((c.cols + kSumCols - 1) / kSumCols, 3), dim3(kSumRows * kSumCols), 0,
+                   s, c);
+}
+
+hipError_t launch_gated_norm(const GatedNorm& a, hipStream_t s) { return by_type(a, false, nullptr, s); }
+size_t gated_norm_backward_ws(int B, int n, int G, int d, int per_group) {
+  auto rows = [&](auto shape) {
+    const Grid g = grid_of<decltype(shape)>(B, n, G, kBackBlocks);
+    return (size_t)g.x * (per_group ? G : g.y);
+  };
+  const size_t narrow = by_row<false>(d, rows), wide = by_row<true>(d, rows);
+  return sizeof(float) * (narrow > wide ? narrow : wide) * d;
+}
+hipError_t launch_gated_norm_backward(const GatedNorm& a, void* ws, hipStream_t s) {
+  return by_type(a, true, static_cast<float*>(ws), s);
+}
+
+}  // namespace hla

@@ -1,0 +1,250 @@
+// The residual addition with the norms on both sides of it:
+//   u = y, or post y / sqrt(mean y^2 + eps)      (the norm after a block)
+//   r = x + alpha scale u                        (the residual stream)
+//   out = w r / sqrt(mean r^2 + eps)             (the norm before the next)
+// and its gradients, with hat_v = v / rms(v), g of out and gr of r:
+//   dr = gr + (g w - hat_r mean(g w hat_r)) / rms(r) = dx,  du = alpha scale dr,
+//   dy = du or (du post - hat_y mean(du post hat_y)) / rms(y),
+//   dw = sum g hat_r,  dpost = sum du hat_y,  dscale = sum alpha u dr.
+// out is made from the fp32 r, not from the rounded one that goes on, and the
+// gradients form r again from x and y: a bf16 r would cost the weight's
+// gradient 2^-9 of every term.
+//
+// Bound by memory: every input is read once and every output written once.  A
+// thread keeps its elements of a row while its block goes over the rows, so the
+// weights are loaded once and their gradients summed in registers.
+#include <initializer_list>
+
+#include "block.h"
+#include "rows.h"
+
+namespace hla {
+namespace {
+
+constexpr int kBlocks = 4096;       // of a forward, at most
+constexpr int kBackBlocks = 1024;   // of a backward
+
+// The row's place in memory: sequences laid apart cost a division.
+__device__ __forceinline__ size_t at(const Rows& r, const ResidualNorm& a, unsigned row) {
+  if (a.B == 1) return (size_t)row * r.ts;
+  const unsigned b = row / a.n;
+  return (size_t)b * r.bs + (size_t)(row - b * a.n) * r.ts;
+}
+
+template <typename TX, typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void k_residual_norm(ResidualNorm a) {
+  __shared__ float red[2][2][1][S::WAVES];
+  const int lane = threadIdx.x % S::LANES;
+  const unsigned rows = (unsigned)a.B * a.n;
+  float w[S::E], step[S::E], post[S::E];
+  load_weight<S>(a.w, a.w_dtype, 0, a.D, lane, w);
+  load_weight<S>(a.scale, a.w_dtype, 0, a.D, lane, step);
+  if (a.post) load_weight<S>(a.post, a.w_dtype, 0, a.D, lane, post);
+  int turn = 0;
+  for (unsigned long long r0 = (unsigned long long)blockIdx.x * S::ROWS; r0 < rows;
+       r0 += (unsigned long long)gridDim.x * S::ROWS, turn ^= 1) {
+    const unsigned row = (unsigned)r0 + threadIdx.x / S::LANES;
+    const bool there = row < rows;
+    const int d = there ? a.D : 0;
+    RowRaw<TX, S> x;
+    RowRaw<T, S> y;
+    x.load(static_cast<const TX*>(a.x.p) + (there ? at(a.x, a, row) : 0), d, lane);
+    y.load(static_cast<const T*>(a.y.p) + (there ? at(a.y, a, row) : 0), d, lane);
+    float ry = 1.f;
+    if (a.post) {
+      float ss[1] = {0.f};
+#pragma unroll
+      for (int e = 0; e < S::E; ++e) ss[0] += y.at(e) * y.at(e);
+      row_sums<S, 1>(ss, red[turn][0]);
+      ry = 1.f / sqrtf(ss[0] / a.D + a.eps);
+    }
+    float r[S::E], ss[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float u = a.post ? y.at(e) * ry * post[e] : y.at(e);
+      r[e] = x.at(e) + a.alpha * step[e] * u;
+      ss[0] += r[e] * r[e];
+    }
+    row_sums<S, 1>(ss, red[turn][1]);
+    const float rr = 1.f / sqrtf(ss[0] / a.D + a.eps);
+    const size_t here = there ? (size_t)row * a.D : 0;
+    store_row<TX, S>(static_cast<TX*>(a.r) + here, d, lane, r);
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) r[e] *= rr * w[e];
+    store_row<T, S>(static_cast<T*>(a.out) + here, d, lane, r);
+  }
+}
+
+// Partial sums of the three weights' gradients: [3][blocks][D], the block's
+// rows summed in a fixed order.
+template <typename TX, typename T, typename S>
+__global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm a, float* __restrict__ part) {
+  __shared__ float red[2][4][S::WAVES];
+  const int lane = threadIdx.x % S::LANES;
+  const unsigned rows = (unsigned)a.B * a.n;
+  float w[S::E], step[S::E], post[S::E], dw[S::E], dscale[S::E], dpost[S::E];
+  load_weight<S>(a.w, a.w_dtype, 0, a.D, lane, w);
+  load_weight<S>(a.scale, a.w_dtype, 0, a.D, lane, step);
+  if (a.post) load_weight<S>(a.post, a.w_dtype, 0, a.D, lane, post);
+#pragma unroll
+  for (int e = 0; e < S::E; ++e) dw[e] = dscale[e] = dpost[e] = 0.f;
+  int turn = 0;
+  for (unsigned long long r0 = (unsigned long long)blockIdx.x * S::ROWS; r0 < rows;
+       r0 += (unsigned long long)gridDim.x * S::ROWS, turn ^= 1) {
+    const unsigned row = (unsigned)r0 + threadIdx.x / S::LANES;
+    const bool there = row < rows;
+    const int d = there ? a.D : 0;
+    const size_t here = there ? (size_t)row * a.D : 0;
+    RowRaw<TX, S> x, gr;
+    RowRaw<T, S> y, go;
+    x.load(static_cast<const TX*>(a.x.p) + (there ? at(a.x, a, row) : 0), d, lane);
+    y.load(static_cast<const T*>(a.y.p) + (there ? at(a.y, a, row) : 0), d, lane);
+    go.zero();
+    gr.zero();
+    if (a.dout) go.load(static_cast<const T*>(a.dout) + here, d, lane);
+    if (a.dr) gr.load(static_cast<const TX*>(a.dr) + here, d, lane);
+    float ry = 1.f;
+    if (a.post) {
+      float ss[1] = {0.f};
+#pragma unroll
+      for (int e = 0; e < S::E; ++e) ss[0] += y.at(e) * y.at(e);
+      row_sums<S, 1>(ss, red[turn]);
+      ry = 1.f / sqrtf(ss[0] / a.D + a.eps);
+    }
+    float r[S::E], dr[S::E], two[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float u = a.post ? y.at(e) * ry * post[e] : y.at(e);
+      r[e] = x.at(e) + a.alpha * step[e] * u;
+      two[0] += r[e] * r[e];
+      two[1] += go.at(e) * w[e] * r[e];
+    }
+    row_sums<S, 2>(two, red[turn] + 1);
+    const float rr = 1.f / sqrtf(two[0] / a.D + a.eps), mean = two[1] / a.D * rr;
+    float dot[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float hat = r[e] * rr;
+      dr[e] = gr.at(e) + rr * (go.at(e) * w[e] - hat * mean);
+      dw[e] += go.at(e) * hat;
+      const float yhat = y.at(e) * ry, u = a.post ? yhat * post[e] : y.at(e);
+      dscale[e] += a.alpha * u * dr[e];
+      if (a.post) {
+        const float du = a.alpha * step[e] * dr[e];
+        dpost[e] += du * yhat;
+        dot[0] += du * post[e] * yhat;
+      }
+    }
+    store_row<TX, S>(static_cast<TX*>(a.dx) + here, d, lane, dr);
+    if (a.post) row_sums<S, 1>(dot, red[turn] + 3);
+    const float mean_y = dot[0] / a.D;
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float du = a.alpha * step[e] * dr[e];
+      r[e] = a.post ? ry * (du * post[e] - y.at(e) * ry * mean_y) : du;
+    }
+    store_row<T, S>(static_cast<T*>(a.dy) + here, d, lane, r);
+  }
+  __shared__ float sums[S::ROWS > 1 ? S::ROWS : 1][S::ROWS > 1 ? S::LANES * S::E + 1 : 1];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (!(k == 0 ? a.dw : k == 1 ? a.dpost : a.dscale)) continue;
+    const float(&mine)[S::E] = k == 0 ? dw : k == 1 ? dpost : dscale;
+    float* to = part + ((size_t)k * gridDim.x + blockIdx.x) * a.D;
+    if constexpr (S::ROWS > 1) __syncthreads();
+#pragma unroll
+    for (int ch = 0; ch < S::CH; ++ch)
+#pragma unroll
+      for (int i = 0; i < S::V; ++i) {
+        const int c = (ch * S::LANES + lane) * S::V + i;
+        if constexpr (S::ROWS > 1)
+          sums[threadIdx.x / S::LANES][c] = mine[ch * S::V + i];
+        else if (c < a.D)
+          to[c] = mine[ch * S::V + i];
+      }
+    if constexpr (S::ROWS > 1) {
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.D; c += S::THREADS) {
+        float s = 0.f;
+        for (int o = 0; o < S::ROWS; ++o) s += sums[o][c];
+        to[c] = s;
+      }
+    }
+  }
+}
+
+bool on_16(const void* p, int dtype, std::initializer_list<long long> strides = {}) {
+  if (reinterpret_cast<uintptr_t>(p) & 15) return false;
+  for (long long st : strides)
+    if (st * (dtype == 1 ? 2 : 4) % 16) return false;
+  return true;
+}
+
+// Sequences laid one behind the other are one long one.
+void flatten(ResidualNorm& a) {
+  if (a.B == 1) return;
+  if (a.n == 1) {
+    a.x.ts = a.x.bs;
+    a.y.ts = a.y.bs;
+  } else if (a.x.bs != a.n * a.x.ts || a.y.bs != a.n * a.y.ts) {
+    return;
+  }
+  a.n *= a.B;
+  a.B = 1;
+}
+
+template <typename S>
+int blocks_of(int B, int n, int most) {
+  const long long need = ((long long)B * n + S::ROWS - 1) / S::ROWS;
+  return (int)(need < most ? need : most);
+}
+
+template <typename TX, typename T, bool VEC>
+hipError_t forward(const ResidualNorm& a, hipStream_t s) {
+  return by_row<VEC>(a.D, [&](auto shape) {
+    using S = decltype(shape);
+    return HLA_TIMED("residual_norm", (k_residual_norm<TX, T, S>), dim3(blocks_of<S>(a.B, a.n, kBlocks)), dim3(S::THREADS),
+                     0, s, a);
+  });
+}
+
+template <typename TX, typename T, bool VEC>
+hipError_t backward(const ResidualNorm& a, float* part, hipStream_t s) {
+  int blocks = 0;
+  const hipError_t e = by_row<VEC>(a.D, [&](auto shape) {
+    using S = decltype(shape);
+    blocks = blocks_of<S>(a.B, a.n, kBackBlocks);
+    return HLA_TIMED("residual_norm_back", (k_residual_norm_back<TX, T, S>), dim3(blocks), dim3(S::THREADS), 0, s, a, part);
+  });
+  if (e != hipSuccess || !(a.dw || a.dpost || a.dscale)) return e;
+  return launch_column_sums({part, {a.dw, a.dpost, a.dscale}, blocks, a.D, a.w_dtype}, s);
+}
+
+template <typename TX, typename T>
+hipError_t by_layout(ResidualNorm a, bool back, float* part, hipStream_t s) {
+  flatten(a);
+  bool vec = a.D % 8 == 0 && on_16(a.x.p, a.x_dtype, {a.x.bs, a.x.ts}) && on_16(a.y.p, a.dtype, {a.y.bs, a.y.ts});
+  for (const void* p : {(const void*)a.out, (const void*)a.r, a.dout, a.dr, (const void*)a.dx, (const void*)a.dy})
+    vec = vec && on_16(p, 1);
+  if (back) return vec ? backward<TX, T, true>(a, part, s) : backward<TX, T, false>(a, part, s);
+  return vec ? forward<TX, T, true>(a, s) : forward<TX, T, false>(a, s);
+}
+
+hipError_t by_type(const ResidualNorm& a, bool back, float* part, hipStream_t s) {
+  if (a.dtype == 0) return by_layout<float, float>(a, back, part, s);
+  return a.x_dtype == 0 ? by_layout<float, bf16>(a, back, part, s) : by_layout<bf16, bf16>(a, back, part, s);
+}
+
+}  // namespace
+
+hipError_t launch_residual_norm(const ResidualNorm& a, hipStream_t s) { return by_type(a, false, nullptr, s); }
+size_t residual_norm_backward_ws(int B, int n, int D) {
+  auto blocks = [&](auto shape) { return blocks_of<decltype(shape)>(B, n, kBackBlocks); };
+  const int narrow = by_row<false>(D, blocks), wide = by_row<true>(D, blocks);
+  return sizeof(float) * 3 * (size_t)(narrow > wide ? narrow : wide) * D;
+}
+hipError_t launch_residual_norm_backward(const ResidualNorm& a, void* ws, hipStream_t s) {
+  return by_type(a, true, static_cast<float*>(ws), s);
+}
+
+}  // namespace hla
