@@ -39,7 +39,7 @@ __device__ __forceinline__ const bf16* token(const Rows& r, int n, long long m) 
 
 // Workgroups go to the 8 XCDs in turn: each XCD gets neighbouring tiles, in
 // groups of kGroup tiles of rows j that pass over the same rows i.
-constexpr int kGroup = 8;
+constexpr int kGroup = 4;
 __device__ __forceinline__ void tile_of(int ni, int nj, int& i, int& j) {
   const unsigned total = (unsigned)ni * nj, x = blockIdx.x & 7, k = blockIdx.x >> 3;
   const unsigned per = total >> 3, more = total & 7, id = x * per + min(x, more) + k;
@@ -64,30 +64,32 @@ __device__ __forceinline__ void store_pieces(bf16* row, int at, int end, const f
 template <typename S, bool GELU, bool BACK>
 __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ both) {
   extern __shared__ __align__(1024) char lds[];
-  const int M = p.B * p.n, ni = (p.F + S::OUT - 1) / S::OUT, nj = (M + S::BJ - 1) / S::BJ;
+  const int ni = (p.F + S::OUT - 1) / S::OUT, per = (p.n + S::BJ - 1) / S::BJ;
   int ti, tj;
-  tile_of(ni, nj, ti, tj);
-  const int f0 = ti * S::OUT, m0 = tj * S::BJ;
+  tile_of(ni, p.B * per, ti, tj);
+  const int f0 = ti * S::OUT, b = tj / per, t0 = (tj - b * per) * S::BJ;
+  const bf16* x = static_cast<const bf16*>(p.x.p) + (size_t)b * p.x.bs + (size_t)t0 * p.x.ts;
   f32x4 acc[S::TI][S::TJ] = {};
   tile_products<S>(acc, lds, 0, p.D, [&](int r) {
-    if (r >= S::BI) return token(p.x, p.n, min(m0 + r - S::BI, M - 1));
+    if (r >= S::BI) return RowAt{x, (uint32_t)(min(r - S::BI, p.n - 1 - t0) * p.x.ts * 2)};
     const int wi = r / (16 * S::TI), q = r % (16 * S::TI), c = q % (16 * S::HALF);
-    const bf16* w = static_cast<const bf16*>(q < 16 * S::HALF ? p.wg : p.wu);
-    return w + (size_t)min(f0 + wi * 16 * S::HALF + c, p.F - 1) * p.D;
+    const bf16* w = static_cast<const bf16*>(q < 16 * S::HALF ? p.wg : p.wu) + (size_t)f0 * p.D;
+    return RowAt{w, (uint32_t)(min(wi * 16 * S::HALF + c, p.F - 1 - f0) * p.D * 2)};
   });
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
   const int f = f0 + wi * 16 * S::HALF + (lane >> 4) * 4 * S::HALF;
 #pragma unroll
   for (int j = 0; j < S::TJ; ++j) {
-    const int m = m0 + (wj * S::TJ + j) * 16 + (lane & 15);
-    if (m >= M) continue;
+    const int t = t0 + (wj * S::TJ + j) * 16 + (lane & 15);
+    if (t >= p.n) continue;
+    const size_t m = (size_t)b * p.n + t;
     float o[4 * S::HALF], o2[4 * S::HALF];
     if constexpr (!BACK) {
 #pragma unroll
       for (int e = 0; e < 4 * S::HALF; ++e) o[e] = act<GELU>(acc[e / 4][j][e % 4]) * acc[S::HALF + e / 4][j][e % 4];
-      store_pieces(static_cast<bf16*>(p.h) + (size_t)m * p.F, f, p.F, o);
+      store_pieces(static_cast<bf16*>(p.h) + m * p.F, f, p.F, o);
     } else {
-      const bf16* dh = token(p.dh, p.n, m);
+      const bf16* dh = static_cast<const bf16*>(p.dh.p) + (size_t)b * p.dh.bs + (size_t)t * p.dh.ts;
 #pragma unroll
       for (int q = 0; q < 4 * S::HALF; q += 8) {
         Raw<bf16, 8> g;
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ bo
           o2[q + e] = g.at(e) * a;
         }
       }
-      bf16* to = both + (size_t)m * 2 * p.F;
+      bf16* to = both + m * 2 * p.F;
       store_pieces(to, f, p.F, o);
       store_pieces(to + p.F, f, p.F, o2);
     }
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product p) {
   const int i0 = ti * S::BI, j0 = tj * S::BJ;
   f32x4 acc[S::TI][S::TJ] = {};
   tile_products<S>(acc, lds, 0, p.K, [&](int r) {
-    return r < S::BI ? p.a + (size_t)min(i0 + r, p.I - 1) * p.lda : p.b + (size_t)min(j0 + r - S::BI, p.J - 1) * p.ldb;
+    return r < S::BI ? RowAt{p.a + (size_t)i0 * p.lda, (uint32_t)(min(r, p.I - 1 - i0) * p.lda * 2)}
+                     : RowAt{p.b + (size_t)j0 * p.ldb, (uint32_t)(min(r - S::BI, p.J - 1 - j0) * p.ldb * 2)};
   });
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
   const int i = i0 + wi * 16 * S::TI + (lane >> 4) * 4 * S::TI;
@@ -169,11 +172,26 @@ hipError_t allow_lds(K kernel, int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
+// Sequences laid one behind the other are one long one: a tile lies in one sequence.
+Glu joined(Glu p) {
+  auto fits = [&](const Rows& r) { return !r.p || r.bs == (long long)p.n * r.ts; };
+  if (p.B == 1) return p;
+  if (p.n == 1) {
+    p.x.ts = p.x.bs;
+    p.dh.ts = p.dh.bs;
+  } else if (!fits(p.x) || !fits(p.dh)) {
+    return p;
+  }
+  p.n *= p.B;
+  p.B = 1;
+  return p;
+}
+
 template <bool GELU, bool BACK>
-hipError_t projections(const Glu& p, bf16* both, hipStream_t s) {
+hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
+  const Glu p = joined(given);
   using S = Tile<8, 4, 2, 4, true>;
-  const int M = p.B * p.n;
-  const unsigned tiles = (unsigned)((p.F + S::OUT - 1) / S::OUT) * (unsigned)((M + S::BJ - 1) / S::BJ);
+  const unsigned tiles = (unsigned)((p.F + S::OUT - 1) / S::OUT) * (unsigned)p.B * (unsigned)((p.n + S::BJ - 1) / S::BJ);
   auto kernel = k_glu<S, GELU, BACK>;
   const hipError_t e = allow_lds(kernel, S::LDS);
   if (e != hipSuccess) return e;
