@@ -32,11 +32,6 @@ __device__ __forceinline__ void act_both(float p, float& f, float& d) {
   }
 }
 
-__device__ __forceinline__ const bf16* token(const Rows& r, int n, long long m) {
-  const unsigned b = (unsigned)m / (unsigned)n;
-  return static_cast<const bf16*>(r.p) + (size_t)b * r.bs + (size_t)((unsigned)m - b * n) * r.ts;
-}
-
 // Workgroups go to the 8 XCDs in turn: each XCD gets neighbouring tiles, in
 // groups of kGroup tiles of rows j that pass over the same rows i.
 constexpr int kGroup = 4;
@@ -70,12 +65,13 @@ __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ bo
   const int f0 = ti * S::OUT, b = tj / per, t0 = (tj - b * per) * S::BJ;
   const bf16* x = static_cast<const bf16*>(p.x.p) + (size_t)b * p.x.bs + (size_t)t0 * p.x.ts;
   f32x4 acc[S::TI][S::TJ] = {};
-  tile_products<S>(acc, lds, 0, p.D, [&](int r) {
-    if (r >= S::BI) return RowAt{x, (uint32_t)(min(r - S::BI, p.n - 1 - t0) * p.x.ts * 2)};
+  auto weights = [&](int r) {
     const int wi = r / (16 * S::TI), q = r % (16 * S::TI), c = q % (16 * S::HALF);
     const bf16* w = static_cast<const bf16*>(q < 16 * S::HALF ? p.wg : p.wu) + (size_t)f0 * p.D;
     return RowAt{w, (uint32_t)(min(wi * 16 * S::HALF + c, p.F - 1 - f0) * p.D * 2)};
-  });
+  };
+  tile_products<S>(acc, lds, 0, p.D, weights,
+                   [&](int r) { return RowAt{x, (uint32_t)(min(r, p.n - 1 - t0) * p.x.ts * 2)}; });
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
   const int f = f0 + wi * 16 * S::HALF + (lane >> 4) * 4 * S::HALF;
 #pragma unroll
@@ -110,12 +106,17 @@ __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ bo
   }
 }
 
-// C[j][i] = sum_k A[i][k] B[j][k], a [ni][lda], b [nj][ldb]; rows j of C from `split` on lie at c2.
+// The gradients' products, C[j][i] = sum over one or two spans of k of A[i][k]
+// B[j][k].  A has its rows i contiguous, B its rows j (TRJ) or its k.  The spans
+// are cut into `cuts` parts of `per` k each (a multiple of 64); a workgroup takes
+// one part of a tile, or with one cut all spans of it.  Rows j of C from `split`
+// on lie at c2.  With several cuts, sums go to `part` [cuts spans][J][I].
 struct Product {
-  const bf16 *a, *b;
+  const bf16 *a[2], *b[2];
+  long long lda, ldb;
   bf16 *c, *c2;
-  long long lda, ldb, ldc;
-  int I, J, K, split;
+  float* part;
+  int I, J, K, spans, cuts, per, split;
 };
 template <typename S>
 __global__ __launch_bounds__(S::THREADS) void k_product(Product p) {
@@ -123,47 +124,68 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product p) {
   const int ni = (p.I + S::BI - 1) / S::BI, nj = (p.J + S::BJ - 1) / S::BJ;
   int ti, tj;
   tile_of(ni, nj, ti, tj);
-  const int i0 = ti * S::BI, j0 = tj * S::BJ;
+  const int i0 = ti * S::BI, j0 = tj * S::BJ, z = blockIdx.y;
   f32x4 acc[S::TI][S::TJ] = {};
-  tile_products<S>(acc, lds, 0, p.K, [&](int r) {
-    return r < S::BI ? RowAt{p.a + (size_t)i0 * p.lda, (uint32_t)(min(r, p.I - 1 - i0) * p.lda * 2)}
-                     : RowAt{p.b + (size_t)j0 * p.ldb, (uint32_t)(min(r - S::BI, p.J - 1 - j0) * p.ldb * 2)};
-  });
+  auto over = [&](int span, int k_first, int k_end) {
+    const ByK a{p.a[span] + i0, p.lda, p.I - i0};
+    const bf16* b = p.b[span];
+    if constexpr (S::TRJ) {
+      tile_products<S>(acc, lds, k_first, k_end, a, ByK{b + j0, p.ldb, p.J - j0});
+    } else {
+      b += (size_t)j0 * p.ldb;
+      tile_products<S>(acc, lds, k_first, k_end, a,
+                       [&](int r) { return RowAt{b, (uint32_t)(min(r, p.J - 1 - j0) * p.ldb * 2)}; });
+    }
+  };
+  if (p.cuts == 1 && !p.part) {
+    over(0, 0, p.K);
+    if (p.spans == 2) over(1, 0, p.K);
+  } else {
+    const int k = z / p.spans * p.per;
+    over(z % p.spans, k, min(k + p.per, p.K));
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
-  const int i = i0 + wi * 16 * S::TI + (lane >> 4) * 4 * S::TI;
+  const int i = i0 + wi * 16 * S::TI + (lane >> 4) * 4;
 #pragma unroll
   for (int j = 0; j < S::TJ; ++j) {
     const int row = j0 + (wj * S::TJ + j) * 16 + (lane & 15);
     if (row >= p.J) continue;
-    float o[4 * S::TI];
+    bf16* c = row < p.split ? p.c + (size_t)row * p.I : p.c2 + (size_t)(row - p.split) * p.I;
 #pragma unroll
-    for (int e = 0; e < 4 * S::TI; ++e) o[e] = acc[e / 4][j][e % 4];
-    store_pieces(row < p.split ? p.c + (size_t)row * p.ldc : p.c2 + (size_t)(row - p.split) * p.ldc, i, p.I, o);
+    for (int t = 0; t < S::TI; ++t) {
+      const float o[4] = {acc[t][j][0], acc[t][j][1], acc[t][j][2], acc[t][j][3]};
+      if (i + 16 * t >= p.I) continue;
+      if (p.part)
+        store_vec<float, 4>(p.part + ((size_t)z * p.J + row) * p.I + i + 16 * t, o);
+      else
+        store_vec<bf16, 4>(c + i + 16 * t, o);
+    }
   }
 }
 
-// to[c][at + r] = row(r)[c] for r < R, zeros for r in [R, rows); blocks of 64 x 64.
-constexpr int kTr = 64;
-__global__ __launch_bounds__(256) void k_transposed(Rows x, int n, int R, int C, int rows, bf16* __restrict__ to,
-                                                    long long pitch, long long at) {
-  __shared__ uint16_t tile[kTr][kTr + 2];
-  const int r0 = blockIdx.x * kTr, c0 = blockIdx.y * kTr;
-  for (int e = threadIdx.x; e < kTr * kTr / 8; e += 256) {
-    const int r = e / (kTr / 8), c = e % (kTr / 8) * 8;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (r0 + r < R && c0 + c < C) v = *reinterpret_cast<const uint4*>(token(x, n, r0 + r) + c0 + c);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// The parts joined in their order: eight values a thread.
+__global__ __launch_bounds__(256) void k_joined(Product p) {
+  const size_t all = (size_t)p.J * p.I / 8, e = blockIdx.x * 256ull + threadIdx.x;
+  if (e >= all) return;
+  float s[8] = {};
+  for (int z = 0; z < p.cuts * p.spans; ++z) {
+    float v[8];
+    load_vec<float, 8>(p.part + ((size_t)z * all + e) * 8, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tile[c + i][r] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    for (int i = 0; i < 8; ++i) s[i] += v[i];
   }
-  __syncthreads();
-  for (int e = threadIdx.x; e < kTr * kTr / 8; e += 256) {
-    const int c = e / (kTr / 8), r = e % (kTr / 8) * 8;
-    if (c0 + c >= C || r0 + r >= rows) continue;
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = tile[c][r + 2 * i] | (uint32_t)tile[c][r + 2 * i + 1] << 16;
-    *reinterpret_cast<uint4*>(to + (size_t)(c0 + c) * pitch + at + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+  const size_t half = (size_t)p.split * p.I / 8;
+  store_vec<bf16, 8>(e < half ? p.c + e * 8 : p.c2 + (e - half) * 8, s);
+}
+
+// x [B, n, D] with sequences apart -> [B n, D] without gaps, 16 bytes a thread.
+__global__ __launch_bounds__(256) void k_packed(Rows x, int B, int n, int D, bf16* __restrict__ to) {
+  const size_t all = (size_t)B * n * (D / 8);
+  for (size_t e = blockIdx.x * 256ull + threadIdx.x; e < all; e += gridDim.x * 256ull) {
+    const size_t m = e / (D / 8);
+    const int c = (int)(e - m * (D / 8)) * 8, b = (int)(m / n), t = (int)(m - (size_t)b * n);
+    *reinterpret_cast<uint4*>(to + m * D + c) =
+        *reinterpret_cast<const uint4*>(static_cast<const bf16*>(x.p) + (size_t)b * x.bs + (size_t)t * x.ts + c);
   }
 }
 
@@ -190,7 +212,7 @@ Glu joined(Glu p) {
 template <bool GELU, bool BACK>
 hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
   const Glu p = joined(given);
-  using S = Tile<8, 4, 2, 4, true>;
+  using S = Tile<8, 4, 2, 4, true, false, false>;
   const unsigned tiles = (unsigned)((p.F + S::OUT - 1) / S::OUT) * (unsigned)p.B * (unsigned)((p.n + S::BJ - 1) / S::BJ);
   auto kernel = k_glu<S, GELU, BACK>;
   const hipError_t e = allow_lds(kernel, S::LDS);
@@ -198,32 +220,49 @@ hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
   return HLA_TIMED(BACK ? "glu_gates_back" : "glu", kernel, dim3(tiles), dim3(S::THREADS), S::LDS, s, p, both);
 }
 
-hipError_t product(const Product& p, const char* name, hipStream_t s) {
-  using S = Tile<8, 4, 2, 4, false>;
-  const unsigned tiles = (unsigned)((p.I + S::BI - 1) / S::BI) * (unsigned)((p.J + S::BJ - 1) / S::BJ);
-  const hipError_t e = allow_lds(k_product<S>, S::LDS);
-  if (e != hipSuccess) return e;
-  return HLA_TIMED(name, k_product<S>, dim3(tiles), dim3(S::THREADS), S::LDS, s, p);
+using DxTile = Tile<8, 4, 2, 4, false, true, false>;
+using DwTile = Tile<8, 4, 2, 4, false, true, true>;
+
+// The parts of the two products: as many as leave no CU without a tile, of 512 k at least.
+struct Cuts {
+  int cuts, per;
+};
+template <typename S>
+Cuts cuts_of(long long I, long long J, int K, int spans) {
+  const long long tiles = ((I + S::BI - 1) / S::BI) * ((J + S::BJ - 1) / S::BJ) * spans;
+  long long cuts = 256 / tiles;
+  if (cuts > K / 512) cuts = K / 512;
+  if (cuts <= 1) return {1, K};
+  const int per = (int)(((K + cuts - 1) / cuts + 63) / 64 * 64);
+  return {(K + per - 1) / per, per};
 }
 
-hipError_t transposed(const Rows& x, int n, int R, int C, int rows, bf16* to, long long pitch, long long at, hipStream_t s) {
-  return HLA_TIMED("glu_transposed", k_transposed, dim3((rows + kTr - 1) / kTr, (C + kTr - 1) / kTr), dim3(256), 0, s, x, n, R,
-                   C, rows, to, pitch, at);
+template <typename S>
+hipError_t product(Product p, float* part, const char* name, hipStream_t s) {
+  const Cuts c = cuts_of<S>(p.I, p.J, p.K, p.spans);
+  p.cuts = c.cuts;
+  p.per = c.per;
+  p.part = c.cuts > 1 ? part : nullptr;
+  const unsigned tiles = (unsigned)((p.I + S::BI - 1) / S::BI) * (unsigned)((p.J + S::BJ - 1) / S::BJ);
+  hipError_t e = allow_lds(k_product<S>, S::LDS);
+  if (e != hipSuccess) return e;
+  e = HLA_TIMED(name, k_product<S>, dim3(tiles, p.part ? p.cuts * p.spans : 1), dim3(S::THREADS), S::LDS, s, p);
+  if (e != hipSuccess || !p.part) return e;
+  return HLA_TIMED("glu_joined", k_joined, dim3((unsigned)(((size_t)p.I * p.J / 8 + 255) / 256)), dim3(256), 0, s, p);
 }
 
 struct Space {
-  size_t both, turned, xt, wt, bytes;
-  long long pitch;
+  size_t both, x, part, bytes;
 };
 Space space(int B, int n, int D, int F) {
   Space a;
   const size_t M = (size_t)B * n;
-  a.pitch = (long long)((M + 7) / 8 * 8);
+  const Cuts dx = cuts_of<DxTile>(D, M, F, 2), dw = cuts_of<DwTile>(D, 2LL * F, (int)M, 1);
+  const size_t px = dx.cuts > 1 ? M * D * 4 * dx.cuts * 2 : 0, pw = dw.cuts > 1 ? (size_t)2 * F * D * 4 * dw.cuts : 0;
   a.both = 0;
-  a.turned = a.both + M * 2 * F * 2;
-  a.xt = a.turned + (size_t)a.pitch * 2 * F * 2;
-  a.wt = a.xt + (size_t)a.pitch * D * 2;
-  a.bytes = a.wt + (size_t)D * 2 * F * 2;
+  a.x = a.both + M * 2 * F * 2;
+  a.part = a.x + (B > 1 && n > 1 ? M * D * 2 : 0);
+  a.bytes = a.part + (px > pw ? px : pw);
   return a;
 }
 
@@ -237,18 +276,31 @@ size_t glu_backward_ws(int B, int n, int D, int F) { return space(B, n, D, F).by
 hipError_t launch_glu_backward(const Glu& p, void* ws, hipStream_t s) {
   const Space sp = space(p.B, p.n, p.D, p.F);
   char* w = static_cast<char*>(ws);
-  bf16 *both = reinterpret_cast<bf16*>(w + sp.both), *turned = reinterpret_cast<bf16*>(w + sp.turned);
-  bf16 *xt = reinterpret_cast<bf16*>(w + sp.xt), *wt = reinterpret_cast<bf16*>(w + sp.wt);
+  bf16* both = reinterpret_cast<bf16*>(w + sp.both);
+  float* part = reinterpret_cast<float*>(w + sp.part);
   const int M = p.B * p.n, F2 = 2 * p.F;
   hipError_t e = p.gelu ? projections<true, true>(p, both, s) : projections<false, true>(p, both, s);
   if (e != hipSuccess) return e;
-  const Rows wg{p.wg, 0, p.D}, wu{p.wu, 0, p.D}, b{both, 0, F2};
-  if ((e = transposed(wg, p.F, p.F, p.D, p.F, wt, F2, 0, s)) || (e = transposed(wu, p.F, p.F, p.D, p.F, wt, F2, p.F, s)) ||
-      (e = product({wt, both, static_cast<bf16*>(p.dx), nullptr, F2, F2, p.D, p.D, M, F2, M}, "glu_dx", s)) ||
-      (e = transposed(b, M, M, F2, (int)sp.pitch, turned, sp.pitch, 0, s)) || (e = transposed(p.x, p.n, M, p.D, (int)sp.pitch, xt, sp.pitch, 0, s)))
-    return e;
-  return product({xt, turned, static_cast<bf16*>(p.dwg), static_cast<bf16*>(p.dwu), sp.pitch, sp.pitch, p.D, p.D, F2,
-                  (int)sp.pitch, p.F}, "glu_dw", s);
+  const bf16 *wg = static_cast<const bf16*>(p.wg), *wu = static_cast<const bf16*>(p.wu);
+  Product dx{};
+  dx.a[0] = wg, dx.a[1] = wu, dx.lda = p.D;
+  dx.b[0] = both, dx.b[1] = both + p.F, dx.ldb = F2;
+  dx.c = static_cast<bf16*>(p.dx);
+  dx.I = p.D, dx.J = dx.split = M, dx.K = p.F, dx.spans = 2;
+  if ((e = product<DxTile>(dx, part, "glu_dx", s))) return e;
+  // the tokens as one sequence
+  Rows x = joined(p).x;
+  if (joined(p).B > 1) {
+    bf16* packed = reinterpret_cast<bf16*>(w + sp.x);
+    if ((e = HLA_TIMED("glu_packed", k_packed, dim3(2048), dim3(256), 0, s, p.x, p.B, p.n, p.D, packed))) return e;
+    x = {packed, 0, p.D};
+  }
+  Product dw{};
+  dw.a[0] = static_cast<const bf16*>(x.p), dw.lda = x.ts;
+  dw.b[0] = both, dw.ldb = F2;
+  dw.c = static_cast<bf16*>(p.dwg), dw.c2 = static_cast<bf16*>(p.dwu);
+  dw.I = p.D, dw.J = F2, dw.split = p.F, dw.K = M, dw.spans = 1;
+  return product<DwTile>(dw, part, "glu_dw", s);
 }
 
 }  // namespace hla
