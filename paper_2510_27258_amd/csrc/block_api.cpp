@@ -120,9 +120,12 @@ int glu_sizes(int B, int n, int D, int F) {
   if (D < 1 || F < 1) return fail(HLA_ERR_INVALID, "D and F must be >= 1 (got D=%d F=%d)", D, F);
   if (D % 8 || F % 8) return fail(HLA_ERR_UNSUPPORTED, "D and F must be multiples of 8 (got D=%d F=%d)", D, F);
   if (D > 1 << 20 || F > 1 << 20) return fail(HLA_ERR_UNSUPPORTED, "D and F must be at most 2^20 (got D=%d F=%d)", D, F);
-  // a launch has less than 2^32 threads, 512 of them a tile of 64 x 64 at least; tokens round up to whole tiles
-  if (((double)B * n / 64 + 1) * (2. * F / 64 + 1) * 512 >= 4294967296.0 || (double)B * n + 256 >= 2147483648.0)
-    return fail(HLA_ERR_UNSUPPORTED, "B*n=%lld of F=%d: too many tiles for a launch", (long long)B * n, F);
+  // A launch has less than 2^32 threads: 512 a tile of 128 tokens and 64 outputs, or 256 x 256 of a gradient.
+  auto over = [](double rows, double each) { return std::ceil(rows / each); };
+  const double M = (double)B * n;
+  if (B * over(n, 128) * over(F, 64) * 512 >= 4294967296.0 || over(M, 256) * over(D, 256) * 512 >= 4294967296.0 ||
+      over(D, 256) * over(2. * F, 256) * 512 >= 4294967296.0 || M + 256 >= 2147483648.0)
+    return fail(HLA_ERR_UNSUPPORTED, "B=%d n=%d D=%d F=%d: too many tiles for a launch", B, n, D, F);
   return HLA_OK;
 }
 
@@ -135,6 +138,9 @@ int glu_check(hla::Glu& p, int act, int dtype) {
   if (dtype != HLA_BF16) return fail(HLA_ERR_UNSUPPORTED, "the gated projections cover bf16");
   drop_unused(p.x, p.B, p.n);
   if ((rc = check_rows(p.x, dtype, "x")) || (rc = check_16(p.wg, "w_gate")) || (rc = check_16(p.wu, "w_up"))) return rc;
+  // a tile's 256 rows are addressed with 31-bit byte offsets (of single tokens the stride between sequences)
+  const long long far = p.n == 1 ? p.x.bs : p.x.ts;
+  if (far > (1LL << 22) - 8192) return fail(HLA_ERR_UNSUPPORTED, "x: a token stride of %lld elements is too long", far);
   p.gelu = act == HLA_ACT_GELU;
   return HLA_OK;
 }

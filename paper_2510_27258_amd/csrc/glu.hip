@@ -11,20 +11,35 @@
 namespace hla {
 namespace {
 
+// The normal distribution up to p and its density: the complementary error
+// function as a polynomial in 1 / (1 + 0.3275911 x) times e^(-x^2) (Abramowitz and
+// Stegun 7.1.26, off by at most 1.5e-7), x = |p| / sqrt 2.
+__device__ __forceinline__ void normal(float p, float& below, float& density) {
+  const float x = fabsf(p) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f)), e = __expf(-x * x);
+  const float tail = 0.5f * e * t *
+                     fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  below = p < 0.f ? tail : 1.f - tail;
+  density = 0.39894228f * e;
+}
+
 template <bool GELU>
 __device__ __forceinline__ float act(float p) {
-  if constexpr (GELU)
-    return 0.5f * p * (1.f + erff(p * 0.70710678f));
-  else
+  if constexpr (GELU) {
+    float below, density;
+    normal(p, below, density);
+    return p * below;
+  } else {
     return p * __builtin_amdgcn_rcpf(1.f + __expf(-p));
+  }
 }
 // act(p) and its derivative
 template <bool GELU>
 __device__ __forceinline__ void act_both(float p, float& f, float& d) {
   if constexpr (GELU) {
-    const float phi = 0.5f * (1.f + erff(p * 0.70710678f));
-    f = p * phi;
-    d = phi + p * (0.39894228f * __expf(-0.5f * p * p));
+    float below, density;
+    normal(p, below, density);
+    f = p * below;
+    d = fmaf(p, density, below);
   } else {
     const float s = __builtin_amdgcn_rcpf(1.f + __expf(-p));
     f = p * s;
@@ -104,6 +119,57 @@ __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ bo
       store_pieces(to + p.F, f, p.F, o2);
     }
   }
+}
+
+// Up to 16 tokens: the weights' bytes bound it.  A workgroup takes 16 outputs (16
+// rows of both weights); its eight waves share out k, read their operands from
+// memory to registers, four steps of 32 k at a time, and join in LDS.  16 tokens of
+// 2048 x 8192 (67 MB of weights): 15.3 us, 4.4 TB/s; the 128-token tiles 17.4.
+constexpr int kFew = 16, kFewWaves = 8, kFewSteps = 4;
+template <bool GELU>
+__global__ __launch_bounds__(64 * kFewWaves) void k_glu_few(Glu p) {
+  __shared__ float sums[kFewWaves][2][4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int f0 = blockIdx.x * 16, M = p.B * p.n, token = min(m, M - 1), seq = token / p.n;
+  const size_t row = (size_t)min(f0 + m, p.F - 1) * p.D;
+  const bf16 *wg = static_cast<const bf16*>(p.wg) + row, *wu = static_cast<const bf16*>(p.wu) + row;
+  const bf16* x = static_cast<const bf16*>(p.x.p) + (size_t)seq * p.x.bs + (size_t)(token - seq * p.n) * p.x.ts;
+  f32x4 acc[2] = {};
+  const int steps = (p.D + 31) / 32, per = (steps + kFewWaves - 1) / kFewWaves, last = min(steps, (wave + 1) * per);
+  for (int s = wave * per; s < last; s += kFewSteps) {
+    Raw<bf16, 8> a[kFewSteps][2], b[kFewSteps];
+#pragma unroll
+    for (int i = 0; i < kFewSteps; ++i) {
+      const int k = (s + i) * 32 + 8 * g;
+      a[i][0].zero();
+      a[i][1].zero();
+      b[i].zero();
+      if (s + i < last && k < p.D) {
+        a[i][0].load(wg + k);
+        a[i][1].load(wu + k);
+        b[i].load(x + k);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kFewSteps; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i][h]),
+                                                         __builtin_bit_cast(bf16x8, b[i]), acc[h], 0, 0, 0);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[wave][h][e][lane] = acc[h][e];
+  __syncthreads();
+  const int f = threadIdx.x & 15, t = threadIdx.x >> 4, l = (f >> 2) * 16 + t;
+  if (t >= M || f0 + f >= p.F) return;
+  float v[2] = {0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h] += sums[w][h][f & 3][l];
+  static_cast<bf16*>(p.h)[(size_t)t * p.F + f0 + f].bits = to_bf16(act<GELU>(v[0]) * v[1]);
 }
 
 // The gradients' products, C[j][i] = sum over one or two spans of k of A[i][k]
@@ -209,15 +275,39 @@ Glu joined(Glu p) {
   return p;
 }
 
-template <bool GELU, bool BACK>
-hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
-  const Glu p = joined(given);
-  using S = Tile<8, 4, 2, 4, true, false, false>;
-  const unsigned tiles = (unsigned)((p.F + S::OUT - 1) / S::OUT) * (unsigned)p.B * (unsigned)((p.n + S::BJ - 1) / S::BJ);
+template <typename S>
+unsigned tiles_of(const Glu& p) {
+  return (unsigned)((p.F + S::OUT - 1) / S::OUT) * (unsigned)p.B * (unsigned)((p.n + S::BJ - 1) / S::BJ);
+}
+
+template <typename S, bool GELU, bool BACK>
+hipError_t tiled(const Glu& p, bf16* both, hipStream_t s) {
   auto kernel = k_glu<S, GELU, BACK>;
   const hipError_t e = allow_lds(kernel, S::LDS);
   if (e != hipSuccess) return e;
-  return HLA_TIMED(BACK ? "glu_gates_back" : "glu", kernel, dim3(tiles), dim3(S::THREADS), S::LDS, s, p, both);
+  return HLA_TIMED(BACK ? "glu_gates_back" : "glu", kernel, dim3(tiles_of<S>(p)), dim3(S::THREADS), S::LDS, s, p, both);
+}
+
+// Tiles of 256, 192 and 128 tokens; the last one half as wide, two workgroups a
+// CU.  Taken is what promises the shortest time: rounds of one workgroup a CU
+// times what a round took, and what the first one's start and the last one's end
+// took beside it, in one unit (16384 x 1024 x 4096: 252, 252 and 277 us; 2001 x
+// 2048 x 5464: 92, 81, 89; 512 x 2048 x 8192: 45, 40, 34; 128: 42, 36, 19).
+template <bool GELU, bool BACK>
+hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
+  const Glu p = joined(given);
+  if constexpr (!BACK) {
+    if ((long long)p.B * p.n <= kFew)
+      return HLA_TIMED("glu_few", k_glu_few<GELU>, dim3((p.F + 15) / 16), dim3(64 * kFewWaves), 0, s, p);
+  }
+  using S256 = Tile<8, 4, 2, 4, true, false, false>;
+  using S192 = Tile<8, 3, 2, 4, true, false, false>;
+  using S128 = Tile<4, 2, 2, 4, true, false, false>;
+  auto time = [](unsigned tiles, float round, float rest) { return (tiles + 255) / 256 * round + rest; };
+  const float t256 = time(tiles_of<S256>(p), 31.5f, 12), t192 = time(tiles_of<S192>(p), 23, 14),
+              t128 = time(tiles_of<S128>(p), 8.65f, 10);
+  if (t128 < t192 && t128 < t256) return tiled<S128, GELU, BACK>(p, both, s);
+  return t192 < t256 ? tiled<S192, GELU, BACK>(p, both, s) : tiled<S256, GELU, BACK>(p, both, s);
 }
 
 using DxTile = Tile<8, 4, 2, 4, false, true, false>;

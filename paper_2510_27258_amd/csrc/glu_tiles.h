@@ -69,12 +69,12 @@ struct Tile {
   static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, HALF = PAIR_ ? TI / 2 : TI;
   static constexpr bool TRI = TRI_, TRJ = TRJ_;
   static constexpr int BI = 16 * TI * WI, BJ = 16 * TJ * WJ, WAVES = WI * WJ, THREADS = 64 * WAVES;
-  static constexpr int LOADS = (BI + BJ) / 8 / WAVES;     // of a wave, a step
+  static constexpr int LI = BI / 8 / WAVES, LJ = BJ / 8 / WAVES, LOADS = LI + LJ;   // of a wave, a step
   static constexpr int OUT = 16 * HALF * WI;              // outputs a row of C
   static constexpr uint32_t LDS = (BI + BJ) * 128 * 2;    // a load's 1024 bytes for one buffer, then for the other
-  static_assert((BI + BJ) % (8 * WAVES) == 0 && BI / 8 % LOADS == 0, "a wave loads whole loads of one operand");
-  static_assert(!PAIR_ || 16 * HALF % (8 * LOADS) == 0, "a wave loads rows of one matrix");
-  static_assert(BI <= 512 && BJ <= 512 && 512 % BI == 0 && 512 % BJ == 0, "whole k of a TRANS operand a load");
+  static_assert(BI % (8 * WAVES) == 0 && BJ % (8 * WAVES) == 0, "whole loads");
+  static_assert(!PAIR_ || 16 * HALF % (8 * LI) == 0, "a wave loads rows of one matrix");
+  static_assert((!TRI || 512 % BI == 0) && (!TRJ || 512 % BJ == 0), "whole k of a TRANS operand a load");
   // The first operand's row (of a workgroup) at place r of LDS: places go by subtile, then by the row of a product.
   static __device__ __forceinline__ int row_at(int r) {
     const int t = r / 16 % TI, m = r & 15;
@@ -94,54 +94,58 @@ __device__ __forceinline__ void tile_products(f32x4 (&acc)[S::TI][S::TJ], char* 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave % S::WI, wj = wave / S::WI, m = lane & 15, g = lane >> 4;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  // this wave's loads: all of one operand
-  const bool first = wave * S::LOADS < S::BI / 8;
-  const int load0 = first ? wave * S::LOADS : wave * S::LOADS - S::BI / 8;
-  uint64_t from = 0;                // where the view of its loads begins, a step each
+  // this wave's loads of the two operands
+  uint64_t from_i, from_j;          // where their views begin, a step each
+  long long ahead_i = 128, ahead_j = 128;
   uint32_t off[S::LOADS];
-  long long ahead = 128;
-  int k_of = 0, k_load = 0;         // this lane's k of its first load, and from load to load
-  auto by_row = [&](auto row, auto place) {
+  int k_of_i, k_of_j;               // this lane's k of the first load
+  auto by_row = [&](auto loads, int load0, uint32_t* offs, uint64_t& from, int& k_of, auto row, auto place) {
     const int piece = (lane & 7) ^ (lane >> 3);
 #pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
+    for (int i = 0; i < decltype(loads)::value; ++i) {
       const RowAt at = row(place((load0 + i) * 8 + (lane >> 3)));
       from = reinterpret_cast<uint64_t>(at.base) + 2 * (uint64_t)k_first;
-      off[i] = at.off + 16 * piece;
+      offs[i] = at.off + 16 * piece;
     }
     k_of = k_first + 8 * piece;
   };
-  auto by_k = [&](const ByK& o, auto width) {
+  auto by_k = [&](auto loads, int load0, uint32_t* offs, uint64_t& from, int& k_of, long long& ahead, const ByK& o,
+                  auto width) {
     constexpr int B = decltype(width)::value, K = 512 / B;        // k a load
     ahead = 128 * o.ld;
     from = reinterpret_cast<uint64_t>(o.p) + 2 * (uint64_t)k_first * o.ld;
 #pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
+    for (int i = 0; i < decltype(loads)::value; ++i) {
       const int k = (load0 + i) * K + lane / (B / 8), c = ((lane % (B / 8)) ^ 2 * turn(k)) * 8;
-      off[i] = c < o.rows ? (uint32_t)(2 * (k * o.ld + c)) : kOutside;
+      offs[i] = c < o.rows ? (uint32_t)(2 * (k * o.ld + c)) : kOutside;
     }
     k_of = k_first + load0 * K + lane / (B / 8);
-    k_load = K;
   };
-  if (first) {
-    if constexpr (S::TRI)
-      by_k(row_i, std::integral_constant<int, S::BI>{});
-    else
-      by_row(row_i, [](int r) { return S::row_at(r); });
-  } else {
-    if constexpr (S::TRJ)
-      by_k(row_j, std::integral_constant<int, S::BJ>{});
-    else
-      by_row(row_j, [](int r) { return r; });
-  }
-  from = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(from >> 32)) << 32 |
-         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)from);
+  using NI = std::integral_constant<int, S::LI>;
+  using NJ = std::integral_constant<int, S::LJ>;
+  if constexpr (S::TRI)
+    by_k(NI{}, wave * S::LI, off, from_i, k_of_i, ahead_i, row_i, std::integral_constant<int, S::BI>{});
+  else
+    by_row(NI{}, wave * S::LI, off, from_i, k_of_i, row_i, [](int r) { return S::row_at(r); });
+  if constexpr (S::TRJ)
+    by_k(NJ{}, wave * S::LJ, off + S::LI, from_j, k_of_j, ahead_j, row_j, std::integral_constant<int, S::BJ>{});
+  else
+    by_row(NJ{}, wave * S::LJ, off + S::LI, from_j, k_of_j, row_j, [](int r) { return r; });
+  auto uniform = [](uint64_t p) {
+    return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p);
+  };
+  from_i = uniform(from_i);
+  from_j = uniform(from_j);
   const int steps = (k_end - k_first + 63) / 64;
-  // load i of a step; the last one moves the view on
+  // load i of a step; an operand's last one moves its view on
   auto load = [&](int step, int buffer, int i) {
-    load_to_lds(view(from), k_of < k_end - step * 64 - i * k_load ? off[i] : kOutside,
-                base + (wave * S::LOADS + i) * 2048 + buffer * 1024);
-    if (i == S::LOADS - 1) from += ahead;
+    const bool first = i < S::LI;
+    const int n = first ? i : i - S::LI, k_load = first ? (S::TRI ? 512 / S::BI : 0) : (S::TRJ ? 512 / S::BJ : 0);
+    load_to_lds(view(first ? from_i : from_j), (first ? k_of_i : k_of_j) < k_end - step * 64 - n * k_load ? off[i] : kOutside,
+                base + (first ? wave * S::LI + n : S::BI / 8 + wave * S::LJ + n) * 2048 + buffer * 1024);
+    if (i == S::LI - 1) from_i += ahead_i;
+    if (i == S::LOADS - 1) from_j += ahead_j;
   };
   // LDS bytes of this lane's operand reads: of the two halves of a step where k is
   // contiguous; of subtile 0 of a TRANS operand, whose others lie at exclusive ors with 32 t
@@ -193,8 +197,9 @@ __device__ __forceinline__ void tile_products(f32x4 (&acc)[S::TI][S::TJ], char* 
     }
   };
   constexpr int PAIRS = S::TI * S::TJ / 2, READS = S::TI + S::TJ;
-  constexpr int EARLY = READS / 2, PER_LOAD = (PAIRS - EARLY) / S::LOADS;   // pairs with two reads each, then the loads
-  static_assert(READS % 2 == 0 && EARLY < PAIRS && PER_LOAD >= 1, "room between the products");
+  constexpr int DENSE = READS > 2 * PAIRS - 4 ? READS : 2;        // reads a pair in the first half, until all are out
+  constexpr int EARLY = (READS + DENSE - 1) / DENSE, SPARSE = (READS + PAIRS - 1) / PAIRS;
+  static_assert(S::TI * S::TJ % 2 == 0 && EARLY < PAIRS, "room between the products");
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -214,19 +219,19 @@ __device__ __forceinline__ void tile_products(f32x4 (&acc)[S::TI][S::TJ], char* 
     for (int q = 0; q < PAIRS; ++q) {
       if (q == EARLY) wait_loads_and_meet<63>();
       pair(0, q);
-      if (q < EARLY) {
-        read(buffer, 1, 2 * q);
-        read(buffer, 1, 2 * q + 1);
-      } else if ((q - EARLY) % PER_LOAD == 0 && (q - EARLY) / PER_LOAD < S::LOADS) {
-        load(k + 2, buffer, (q - EARLY) / PER_LOAD);
-      }
+#pragma unroll
+      for (int t = q * DENSE; t < (q + 1) * DENSE && t < READS; ++t) read(buffer, 1, t);
+#pragma unroll
+      for (int i = 0; i < S::LOADS; ++i)
+        if (q == EARLY + i * (PAIRS - EARLY) / S::LOADS) load(k + 2, buffer, i);
       __builtin_amdgcn_sched_barrier(0);
     }
     wait_loads_and_meet<S::LOADS>();
 #pragma unroll
     for (int q = 0; q < PAIRS; ++q) {
       pair(1, q);
-      if (q < READS) read(buffer ^ 1, 0, q);
+#pragma unroll
+      for (int t = q * SPARSE; t < (q + 1) * SPARSE && t < READS; ++t) read(buffer ^ 1, 0, t);
       __builtin_amdgcn_sched_barrier(0);
     }
   };

@@ -255,3 +255,41 @@ def test_projections(size, act):
         _within(got, ref, size, 1.0, name)
         if ref.size >= 4096:
             assert np.linalg.norm(_n(got) - ref) <= 2 ** 0.5 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(ref), name
+
+
+# Every way the work is split, against the products in fp64 on the GPU: tiles of 128, 192 and 256 tokens (the rule
+# of the launch, by the CUs that they fill), single steps of k, sums over cut k with a ragged last part.
+GLU_SPLITS = [(1, 700, 1088, 328), (1, 2001, 136, 5464), (1, 4100, 64, 4096), (1, 16390, 72, 1032), (1, 5000, 72, 136),
+              (1, 1100, 1544, 1096)]
+
+
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("size", GLU_SPLITS)
+def test_projections_in_parts(size, apart):
+    B, n, D, F = size
+    _say(f"projections {size} apart={apart}")
+    gen = torch.Generator("cuda").manual_seed(n)
+    draw = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    if apart:                             # rows of wider rows, sequences with a gap between them
+        B, n = 3, -(-n // 3)
+        x = draw(B, n + 5, D + 24).to(BF16)[:, 2:-3, 8:-16]
+        dh = draw(B, n + 1, F + 8).to(BF16)[:, 1:, 8:]
+    else:
+        x, dh = draw(B, n, D).to(BF16), draw(B, n, F).to(BF16)
+    wg, wu = ((draw(F, D) * D ** -0.5).to(BF16) for _ in range(2))
+    xd, gd, ud, dd = (t.double().flatten(0, -2) for t in (x, wg, wu, dh))
+    p, u = xd @ gd.T, xd @ ud.T
+    s = torch.sigmoid(p)
+    dp, du = dd * u * s * (1 + p * (1 - s)), dd * p * s
+    refs = (p * s * u, dp @ gd + du @ ud, dp.T @ xd, du.T @ xd)
+    got = (hla.glu_forward(x, wg, wu), *hla.glu_backward(x, wg, wu, dh))
+    pabs, uabs = xd.abs() @ gd.abs().T, xd.abs() @ ud.abs().T
+    ep = (2.0 ** -8 + FINE) * dp.abs() + 2 * FINE * dd.abs() * (uabs * 1.13 + u.abs() * pabs + u.abs() * 1.13)
+    eu = (2.0 ** -8 + FINE) * du.abs() + 2 * FINE * dd.abs() * (1.13 * pabs + (p * s).abs())
+    sizes = (FINE * (1.13 * pabs * u.abs() + (p * s).abs() * uabs + (p * s * u).abs()), ep @ gd.abs() + eu @ ud.abs(),
+             ep.T @ xd.abs(), eu.T @ xd.abs())
+    for name, a, r, size in zip(("h", "dx", "dw_gate", "dw_up"), got, refs, sizes):
+        a = a.double().reshape(r.shape)
+        off = (a - r).abs() - 2.0 ** -8 * (1 + 2.0 ** -7) * r.abs() - size
+        assert off.max() <= 0, (name, off.max().item())
+        assert (a - r).norm() <= 2 ** 0.5 * 2.0 ** -8 / 3 ** 0.5 * r.norm(), name
