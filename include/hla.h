@@ -549,7 +549,8 @@ int hla_residual_norm_backward(const void *x, long long x_bs, long long x_ts, co
  * [D]; y [B, n, D] of dtype.  state (optional) fp32 [B, D]: the state before
  * the first token, replaced by that after the last; without it zeros.  kept
  * (optional): hla_glr_kept_bytes(...) bytes for what the gradients need of the
- * forward.  c finite and >= 0, D <= 2^24.  An infinite or NaN input leaves the
+ * forward.  c finite and >= 0, D and the
+ * strides between tokens at most 2^21.  An infinite or NaN input leaves the
  * outputs of its channel from its token on infinite or NaN, and no other.
  * workspace: at least hla_glr_workspace_bytes(...) bytes. */
 size_t hla_glr_workspace_bytes(int B, int n, int D);

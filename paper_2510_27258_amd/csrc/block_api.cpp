@@ -86,11 +86,14 @@ int rn_check(hla::ResidualNorm& a) {
 }
 
 // ---------------------------------------------------------------------------
+// Outputs and inputs of a wave's tokens, 128 at most, are addressed with 31-bit byte offsets.
+constexpr int kGlrWide = 1 << 21;
+
 int glr_sizes(int B, int n, int D) {
   const int rc = check_tokens(B, n);
   if (rc) return rc;
   if (D < 1) return fail(HLA_ERR_INVALID, "D must be >= 1 (got D=%d)", D);
-  if (D > 1 << 24) return fail(HLA_ERR_UNSUPPORTED, "D=%d exceeds 2^24", D);
+  if (D > kGlrWide) return fail(HLA_ERR_UNSUPPORTED, "D=%d exceeds 2^21", D);
   if (hla::glr_threads(B, n, D) >= 4294967296.0)
     return fail(HLA_ERR_UNSUPPORTED, "B=%d D=%d: too many channels for a launch", B, D);
   return HLA_OK;
@@ -106,6 +109,8 @@ int glr_check(hla::Glr& p) {
   for (int i = 0; i < 3; ++i) {
     drop_unused(*rows[i], p.B, p.n);
     if ((rc = check_own(rows[i]->p, es, names[i])) || (rc = check_stride(rows[i]->bs, rows[i]->ts, names[i]))) return rc;
+    if (rows[i]->ts > kGlrWide)
+      return fail(HLA_ERR_UNSUPPORTED, "%s: a token stride of %lld elements is too long", names[i], rows[i]->ts);
   }
   if ((rc = check_own(p.decay, 4, "decay")) || (rc = check_own(p.fb, 4, "f_bias", false)) ||
       (rc = check_own(p.gb, 4, "g_bias", false)))
@@ -295,6 +300,7 @@ int hla_glr_backward(const void* x, long long x_bs, long long x_ts, const void* 
   drop_unused(p.dy, B, n);
   const unsigned es = esize(dtype);
   if ((rc = check_own(kept, 4, "kept")) || (rc = check_own(dy, es, "dy")) || (rc = check_stride(p.dy.bs, p.dy.ts, "dy")) ||
+      (rc = p.dy.ts > kGlrWide ? fail(HLA_ERR_UNSUPPORTED, "dy: a token stride of %lld elements is too long", p.dy.ts) : HLA_OK) ||
       (rc = check_own(dx, es, "dx")) || (rc = check_own(df, es, "df")) || (rc = check_own(dg, es, "dg")) ||
       (rc = check_own(ddecay, 4, "ddecay")) || (rc = check_own(df_bias, 4, "df_bias", false)) ||
       (rc = check_own(dg_bias, 4, "dg_bias", false)) ||

@@ -18,6 +18,7 @@
 // 1 - a^2 is taken as -expm1(2 L): a state that keeps 0.999 of itself a token
 // would lose ten bits of it to the difference.
 #include <cmath>
+#include <type_traits>
 
 #include "block.h"
 #include "lanes.h"
@@ -42,6 +43,18 @@ struct Few {
       w[0] = (uint32_t) reinterpret_cast<const uint16_t*>(p)[0] << 16;
     }
   }
+  // `off` bytes into a view; zeros outside of it
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t view, uint32_t off) {
+    if constexpr (N == 2) {
+      const auto u = __builtin_amdgcn_raw_buffer_load_b64(view, off, 0, 0);
+      w[0] = u[0];
+      w[1] = u[1];
+    } else if constexpr (sizeof(T) * V == 4) {
+      w[0] = __builtin_amdgcn_raw_buffer_load_b32(view, off, 0, 0);
+    } else {
+      w[0] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(view, off, 0, 0) << 16;
+    }
+  }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (sizeof(T) == 4 || V == 1)
       return __uint_as_float(w[i]);
@@ -50,60 +63,85 @@ struct Few {
   }
 };
 template <typename T, int V>
-__device__ __forceinline__ void store_few(T* p, const float (&v)[V]) {
+__device__ __forceinline__ Few<T, V> rounded(const float (&v)[V]) {
+  Few<T, V> r;
   if constexpr (sizeof(T) == 4) {
-    if constexpr (V == 2)
-      *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
-    else
-      *p = v[0];
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.w[i] = __float_as_uint(v[i]);
   } else if constexpr (V == 2) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    *reinterpret_cast<uint32_t*>(p) = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[0], v[1]}, b2));
+    r.w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[0], v[1]}, b2));
   } else {
-    p->bits = to_bf16(v[0]);
+    r.w[0] = to_bf16(v[0]);
+  }
+  return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_few(T* p, const float (&v)[V]) {
+  const Few<T, V> r = rounded<T, V>(v);
+  if constexpr (sizeof(T) * V == 8)
+    *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+  else if constexpr (sizeof(T) * V == 4)
+    *reinterpret_cast<uint32_t*>(p) = r.w[0];
+  else
+    p->bits = (uint16_t)r.w[0];
+}
+// `off` bytes into a view; nothing outside of it
+template <typename T, int V>
+__device__ __forceinline__ void store_few(__amdgpu_buffer_rsrc_t view, uint32_t off, const float (&v)[V]) {
+  const Few<T, V> r = rounded<T, V>(v);
+  if constexpr (sizeof(T) * V == 8) {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64((u2){r.w[0], r.w[1]}, view, off, 0, 0);
+  } else if constexpr (sizeof(T) * V == 4) {
+    __builtin_amdgcn_raw_buffer_store_b32(r.w[0], view, off, 0, 0);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b16((short)r.w[0], view, off, 0, 0);
   }
 }
 
 constexpr float kLog2e = 1.44269504f;
 
-__device__ __forceinline__ float sigm(float v) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
-}
-
-// A channel's constants.
+// A channel's constants: the gates' arguments in powers of two, -f log2 e - fb log2 e.
 struct Channel {
-  float k;        // -c softplus(decay)
-  float fb, gb;
+  float k2, k3;   // -c softplus(decay) times log2 e, and times -2
+  float fb, gb;   // -bias log2 e
 };
 __device__ __forceinline__ float softplus(float d) { return fmaxf(d, 0.f) + log1pf(expf(-fabsf(d))); }
 __device__ __forceinline__ Channel channel(const Glr& p, int c) {
-  return {-p.c * softplus(p.decay[c]), p.fb ? p.fb[c] : 0.f, p.gb ? p.gb[c] : 0.f};
+  const float k = -p.c * softplus(p.decay[c]);
+  return {k * kLog2e, -2.f * k, p.fb ? -kLog2e * p.fb[c] : 0.f, p.gb ? -kLog2e * p.gb[c] : 0.f};
 }
 
-// 1 - e^(2 L) for L <= 0, a = e^L: its series to 2^-26 below 2 |L| = 1/2, the difference above.
-__device__ __forceinline__ float one_minus_square(float L, float a) {
-  const float u = -2.f * L;
-  float s = fmaf(u, -1.f / 40320, 1.f / 5040);
-  s = fmaf(u, s, -1.f / 720);
-  s = fmaf(u, s, 1.f / 120);
-  s = fmaf(u, s, -1.f / 24);
-  s = fmaf(u, s, 1.f / 6);
-  s = fmaf(u, s, -0.5f);
-  s = fmaf(u * u, s, u);
-  return u < 0.5f ? s : fmaf(-a, a, 1.f);
+// sigmoid(v + bias), bias folded in as above
+__device__ __forceinline__ float sigm(float v, float bias) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(fmaf(v, -kLog2e, bias)));
+}
+
+// 1 - e^-u for 0 <= u <= 1/2: u times the polynomial of degree 5 that meets (1 -
+// e^-u) / u at the six Chebyshev points of [0, 1/2], off by at most 3e-9 of it.
+__device__ __forceinline__ float one_minus_exp(float u) {
+  float s = fmaf(u, -0.00112340425f, 0.00818961393f);
+  s = fmaf(u, s, -0.0416300744f);
+  s = fmaf(u, s, 0.166662425f);
+  s = fmaf(u, s, -0.499999821f);
+  return u * fmaf(u, s, 1.f);
 }
 
 struct Gates {
-  float r, i, L, a, om;
+  float r, i, a, om;   // om: 1 - a^2
 };
 __device__ __forceinline__ Gates gates(const Channel& ch, float f, float g) {
   Gates o;
-  o.r = sigm(f + ch.fb);
-  o.i = sigm(g + ch.gb);
-  o.L = ch.k * o.r;
-  o.a = __builtin_amdgcn_exp2f(kLog2e * o.L);
-  o.om = one_minus_square(o.L, o.a);
+  o.r = sigm(f, ch.fb);
+  o.i = sigm(g, ch.gb);
+  o.a = __builtin_amdgcn_exp2f(ch.k2 * o.r);
+  const float u = ch.k3 * o.r;
+  // both are formed and one selected: left to itself the compiler branches
+  float series = one_minus_exp(u), difference = fmaf(-o.a, o.a, 1.f);
+  asm volatile("" : "+v"(series), "+v"(difference));
+  o.om = u <= 0.5f ? series : difference;
   return o;
 }
 
@@ -154,6 +192,38 @@ __device__ __forceinline__ void join_wave(const float (&A)[V], const float (&M)[
   }
 }
 
+// [p, p + bytes) from a uniform address on, the bytes cut at 2^31 - 1: no offset here is larger.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t view_of(const void* from, long long bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(from);
+  const uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p);
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u), (short)0,
+                                           __builtin_amdgcn_readfirstlane((int)min(bytes, 0x7fffffffLL)), 0x00020000);
+}
+constexpr uint32_t kOutside = 1u << 31;
+
+// A thread's S tokens of an input in the tile that is loaded ahead.  A wave's
+// tokens are a view from its first one on, which ends with the sequence: tokens
+// behind it load as zeros, or as other values of the input where rows overlap.
+template <typename T, int V, int S>
+struct Ahead {
+  Few<T, V> raw[S];
+  const T* seq;           // the sequence's token 0
+  uint32_t ts, off;       // bytes between tokens; this thread's first token and channel in the view
+  __amdgpu_buffer_rsrc_t view;
+  __device__ __forceinline__ Ahead(const Rows& r, int b, int c, int row)
+      : seq(static_cast<const T*>(r.p) + (size_t)b * r.bs), ts((uint32_t)(r.ts * sizeof(T))),
+        off((uint32_t)(row * S * r.ts + c) * (uint32_t)sizeof(T)) {}
+  // the wave's tokens from t (uniform) on are next; with !there none
+  __device__ __forceinline__ void aim(long long t, int n, int D, bool there) {
+    asm volatile("" : "+v"(off));   // the tokens' offsets are formed at their loads, not kept in registers
+    const long long tokens = ts / sizeof(T);
+    const bool some = there && t < n;
+    view = view_of(seq + (some ? t * tokens : 0), some ? ((n - 1 - t) * tokens + D) * (long long)sizeof(T) : 0);
+  }
+  __device__ __forceinline__ void load(int s) { raw[s].load(view, off + s * ts); }
+};
+
 // ---------------------------------------------------------------------------
 // Forward.  ENDS: only a segment's A and H, to sums [seg][B][D] (A, H); the
 // first segment's launch also keeps the state at `first` [B][D], which the
@@ -163,12 +233,9 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
   constexpr int CB = V * LPR, RW = 64 / LPR, TILE = S * RW * W;
   __shared__ float2 join[2][W][CB];
   const Spot at = spot(cut, p.B, CB);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR;
-  const bool mine = at.c0 + lane % LPR * V < p.D;
-  const int c = mine ? at.c0 + lane % LPR * V : 0;
-  const T* x = static_cast<const T*>(p.x.p) + (size_t)at.b * p.x.bs + c;
-  const T* f = static_cast<const T*>(p.f.p) + (size_t)at.b * p.f.bs + c;
-  const T* g = static_cast<const T*>(p.g.p) + (size_t)at.b * p.g.bs + c;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR, q = lane % LPR * V;
+  const bool mine = at.c0 + q < p.D;
+  const int c = mine ? at.c0 + q : 0;
   Channel ch[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) ch[v] = channel(p, c + v);
@@ -191,59 +258,68 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
     }
   }
 
-  const long long t_first = (long long)at.seg * cut.tiles * TILE;
+  const long long t_first = (long long)at.seg * cut.tiles * TILE, own = (wave * RW + row) * S;
   const int tiles = (int)min((long long)cut.tiles, (p.n - t_first + TILE - 1) / TILE);
-  Few<T, V> rx[S], rf[S], rg[S];
-  auto load = [&](long long t0) {
-    const long long t = t0 + (wave * RW + row) * S;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const long long u = min(t + s, (long long)p.n - 1);
-      rx[s].load(x + u * p.x.ts);
-      rf[s].load(f + u * p.f.ts);
-      rg[s].load(g + u * p.g.ts);
-    }
+  Ahead<T, V, S> x(p.x, at.b, c, row), f(p.f, at.b, c, row), g(p.g, at.b, c, row);
+  auto aim = [&](long long t0, bool there) {
+    const long long t = t0 + __builtin_amdgcn_readfirstlane(wave) * RW * S;
+    x.aim(t, p.n, p.D, there);
+    f.aim(t, p.n, p.D, there);
+    g.aim(t, p.n, p.D, there);
   };
-  load(t_first);
+  uint32_t out = mine ? (uint32_t)((row * S * p.D + c) * sizeof(T)) : kOutside;   // this thread's first output in its wave's
+  aim(t_first, true);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    f.load(s);
+    g.load(s);
+    x.load(s);
+  }
   for (int k = 0; k < tiles; ++k) {
-    const long long t0 = t_first + (long long)k * TILE, t = t0 + (wave * RW + row) * S;
+    const long long t0 = t_first + (long long)k * TILE, t = t0 + own, tw = t0 + __builtin_amdgcn_readfirstlane(wave) * RW * S;
     float a[S][V], b[S][V], A[V], H[V];
+    asm volatile("" : "+v"(out));
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       A[v] = 1.f;
       H[v] = 0.f;
     }
+    // each token's registers take the next tile's token as soon as they are free
+    aim(t0 + TILE, k + 1 < tiles);
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const Gates o = gates(ch[v], rf[s].at(v), rg[s].at(v));
+        const Gates o = gates(ch[v], f.raw[s].at(v), g.raw[s].at(v));
         a[s][v] = o.a;
-        b[s][v] = __builtin_amdgcn_sqrtf(o.om) * o.i * rx[s].at(v);
-      }
-    if (t0 + TILE > p.n) {
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (t + s >= p.n) {
-            a[s][v] = 1.f;
-            b[s][v] = 0.f;
-          }
-    }
-    if (k + 1 < tiles) load(t0 + TILE);
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
+        b[s][v] = __builtin_amdgcn_sqrtf(o.om) * o.i * x.raw[s].at(v);
         A[v] *= a[s][v];
         H[v] = fmaf(a[s][v], H[v], b[s][v]);
       }
+      f.load(s);
+      g.load(s);
+      x.load(s);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (t0 + TILE > p.n) {       // tokens past the end change nothing
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] = 1.f;
+        H[v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          a[s][v] = t + s < p.n ? a[s][v] : 1.f;
+          b[s][v] = t + s < p.n ? b[s][v] : 0.f;
+          A[v] *= a[s][v];
+          H[v] = fmaf(a[s][v], H[v], b[s][v]);
+        }
+      }
+    }
     float exA[V], exH[V], allA[V], allH[V];
     join_wave<LPR, V, true>(A, H, exA, exH, allA, allH);
     if (row == RW - 1) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) join[k & 1][wave][lane % LPR * V + v] = make_float2(allA[v], allH[v]);
+      for (int v = 0; v < V; ++v) join[k & 1][wave][q + v] = make_float2(allA[v], allH[v]);
     }
     lds_barrier();
     float h[V];
@@ -251,7 +327,7 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
     for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const float2 m = join[k & 1][w][lane % LPR * V + v];
+        const float2 m = join[k & 1][w][q + v];
         if (w == wave) h[v] = fmaf(exA[v], carry[v], exH[v]);
         carry[v] = fmaf(m.x, carry[v], m.y);
         if constexpr (ENDS) through[v] *= m.x;
@@ -262,12 +338,15 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
 #pragma unroll
         for (int v = 0; v < V; ++v) to[v] = h[v];
       }
-      T* y = static_cast<T*>(p.y) + ((size_t)at.b * p.n + t) * p.D + c;
+      // behind the sequence's end, and for lanes behind the last channel, nothing is written
+      const auto y = view_of(static_cast<T*>(p.y) + ((size_t)at.b * p.n + min(tw, (long long)p.n)) * p.D,
+                             max((p.n - tw) * p.D, 0LL) * (long long)sizeof(T));
 #pragma unroll
       for (int s = 0; s < S; ++s) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = fmaf(a[s][v], h[v], b[s][v]);
-        if (mine && t + s < p.n) store_few<T, V>(y + (size_t)s * p.D, h);
+        store_few<T, V>(y, out + s * (uint32_t)(p.D * sizeof(T)), h);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -289,7 +368,7 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
 // segment's A and M.  part: the sums of the parameters' gradients over this
 // segment, [3][B segs][D], formed in fp64 across a thread's runs.
 template <typename T, int V, int LPR, int S, int W, bool ENDS>
-__global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __restrict__ sums, float* __restrict__ part) {
+__global__ __launch_bounds__(64 * W, 2) void k_glr_back(Glr p, Cut cut, float2* __restrict__ sums, float* __restrict__ part) {
   constexpr int CB = V * LPR, RW = 64 / LPR, TILE = S * RW * W;
   static_assert(TILE % kGlrTile == 0, "a tile begins where a state is kept");
   __shared__ float2 join[2][2][W][CB];
@@ -298,10 +377,6 @@ __global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __r
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR, q = lane % LPR * V;
   const bool mine = at.c0 + q < p.D;
   const int c = mine ? at.c0 + q : 0;
-  const T* x = static_cast<const T*>(p.x.p) + (size_t)at.b * p.x.bs + c;
-  const T* f = static_cast<const T*>(p.f.p) + (size_t)at.b * p.f.bs + c;
-  const T* g = static_cast<const T*>(p.g.p) + (size_t)at.b * p.g.bs + c;
-  const T* dy = static_cast<const T*>(p.dy.p) + (size_t)at.b * p.dy.bs + c;
   Channel ch[V];
   float carry[V], through[V];
   double sum[3][V];
@@ -319,50 +394,79 @@ __global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __r
     }
   }
   const int kept = (p.n + kGlrTile - 1) / kGlrTile;
-  const long long t_first = (long long)at.seg * cut.tiles * TILE;
+  const long long t_first = (long long)at.seg * cut.tiles * TILE, own = (wave * RW + row) * S;
   const int tiles = (int)min((long long)cut.tiles, (p.n - t_first + TILE - 1) / TILE);
-  Few<T, V> rx[S], rf[S], rg[S], ry[S];
-  float start[V];
-  auto load = [&](long long t0) {
-    const long long t = t0 + (wave * RW + row) * S;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const long long u = min(t + s, (long long)p.n - 1);
-      rf[s].load(f + u * p.f.ts);
-      ry[s].load(dy + u * p.dy.ts);
-      if constexpr (!ENDS) {
-        rx[s].load(x + u * p.x.ts);
-        rg[s].load(g + u * p.g.ts);
-      }
+  const long long t_last = t_first + (long long)(tiles - 1) * TILE;
+  Ahead<T, V, S> x(p.x, at.b, c, row), f(p.f, at.b, c, row), g(p.g, at.b, c, row), dy(p.dy, at.b, c, row);
+  auto aim = [&](long long t0, bool there) {
+    const long long t = t0 + __builtin_amdgcn_readfirstlane(wave) * RW * S;
+    f.aim(t, p.n, p.D, there);
+    dy.aim(t, p.n, p.D, there);
+    if constexpr (!ENDS) {
+      x.aim(t, p.n, p.D, there);
+      g.aim(t, p.n, p.D, there);
     }
+  };
+  float start[V];
+  auto load_start = [&](long long t0) {
     if constexpr (!ENDS) {
 #pragma unroll
       for (int v = 0; v < V; ++v) start[v] = p.kept[((size_t)at.b * kept + t0 / kGlrTile) * p.D + c + v];
     }
   };
-  load(t_first + (long long)(tiles - 1) * TILE);
-  for (int k = tiles - 1; k >= 0; --k) {
-    const long long t0 = t_first + (long long)k * TILE, t = t0 + (wave * RW + row) * S;
-    const bool whole = t0 + TILE <= p.n;
-    float a[S][V], r[S][V], in[S][V], om[S][V], xs[S][V], dys[S][V], A[V], H[V], M[V], st[V];
+  auto load = [&](int s) {
+    f.load(s);
+    dy.load(s);
+    if constexpr (!ENDS) {
+      x.load(s);
+      g.load(s);
+    }
+  };
+  uint32_t out = mine ? (uint32_t)((row * S * p.D + c) * sizeof(T)) : kOutside;   // this thread's first output in its wave's
+  aim(t_last, true);
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+  for (int s = 0; s < S; ++s) load(s);
+  load_start(t_last);
+  for (int k = tiles - 1; k >= 0; --k) {
+    const long long t0 = t_first + (long long)k * TILE, t = t0 + own, tw = t0 + __builtin_amdgcn_readfirstlane(wave) * RW * S;
+    const bool whole = t0 + TILE <= p.n;
+    asm volatile("" : "+v"(out));
+    float a[S][V], r[S][V], in[S][V], inv[S][V], root[S][V], ix[S][V], dys[S][V], A[V], H[V], M[V], st[V];
+    // each token's registers take the tile before as soon as they are free
+    aim(t0 - TILE, k > 0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) st[v] = start[v];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const bool there = whole || t + s < p.n;
-        const Gates o = gates(ch[v], rf[s].at(v), ENDS ? 0.f : rg[s].at(v));
-        a[s][v] = there ? o.a : 1.f;
-        dys[s][v] = there ? ry[s].at(v) : 0.f;
+        const Gates o = gates(ch[v], f.raw[s].at(v), ENDS ? 0.f : g.raw[s].at(v));
+        a[s][v] = o.a;
+        dys[s][v] = dy.raw[s].at(v);
         if constexpr (!ENDS) {
           r[s][v] = o.r;
           in[s][v] = o.i;
-          om[s][v] = there ? o.om : 0.f;
-          xs[s][v] = there ? rx[s].at(v) : 0.f;
+          // where r = 0 the root is too, and log a / root has the limit 0
+          inv[s][v] = __builtin_amdgcn_rsqf(fmaxf(o.om, 1e-36f));
+          root[s][v] = o.om * inv[s][v];
+          ix[s][v] = o.i * x.raw[s].at(v);
         }
       }
+      load(s);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (k > 0) load_start(t0 - TILE);
+    if (!whole) {               // tokens past the end change nothing
 #pragma unroll
-    for (int v = 0; v < V; ++v) st[v] = start[v];
-    if (k > 0) load(t0 - TILE);
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (t + s >= p.n) {
+            a[s][v] = 1.f;
+            dys[s][v] = 0.f;
+            if constexpr (!ENDS) root[s][v] = ix[s][v] = 0.f;
+          }
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       A[v] = 1.f;
@@ -370,7 +474,7 @@ __global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __r
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         A[v] *= a[s][v];
-        if constexpr (!ENDS) H[v] = fmaf(a[s][v], H[v], __builtin_amdgcn_sqrtf(om[s][v]) * in[s][v] * xs[s][v]);
+        if constexpr (!ENDS) H[v] = fmaf(a[s][v], H[v], root[s][v] * ix[s][v]);
       }
 #pragma unroll
       for (int s = S - 1; s >= 0; --s) M[v] = a[s][v] * (dys[s][v] + M[v]);
@@ -416,33 +520,36 @@ __global__ __launch_bounds__(64 * W) void k_glr_back(Glr p, Cut cut, float2* __r
 #pragma unroll
         for (int s = 0; s < S; ++s) {
           before[s][v] = h[v];
-          h[v] = fmaf(a[s][v], h[v], __builtin_amdgcn_sqrtf(om[s][v]) * in[s][v] * xs[s][v]);
+          h[v] = fmaf(a[s][v], h[v], root[s][v] * ix[s][v]);
         }
       }
-      const size_t to = ((size_t)at.b * p.n + t) * p.D + c;
+      // behind the sequence's end, and for lanes behind the last channel, nothing is written
+      auto output = [&](void* to) {
+        return view_of(static_cast<T*>(to) + ((size_t)at.b * p.n + min(tw, (long long)p.n)) * p.D,
+                       max((p.n - tw) * p.D, 0LL) * (long long)sizeof(T));
+      };
+      const auto dxs = output(p.dx), dfs = output(p.df), dgs = output(p.dg);
 #pragma unroll
       for (int s = S - 1; s >= 0; --s) {
         float dx[V], df[V], dg[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const float l = dys[s][v] + m[v], root = __builtin_amdgcn_sqrtf(om[s][v]);
-          // where r = 0 the root is too, and L / root has the limit 0
-          const float inv = __builtin_amdgcn_rsqf(fmaxf(om[s][v], 1e-36f)), ix = in[s][v] * xs[s][v];
-          const float dL = l * (a[s][v] * before[s][v] - ix * (a[s][v] * (a[s][v] * inv)));
-          dx[v] = l * root * in[s][v];
-          dg[v] = l * root * ix * (1.f - in[s][v]);
-          df[v] = dL * (ch[v].k * r[s][v]) * (1.f - r[s][v]);
-          const bool there = whole || t + s < p.n;
-          run[0][v] += there ? dL * r[s][v] : 0.f;
-          run[1][v] += there ? df[v] : 0.f;
-          run[2][v] += there ? dg[v] : 0.f;
+          const float l = dys[s][v] + m[v], lr = l * root[s][v];
           m[v] = a[s][v] * l;
+          // r times the gradient of log a
+          const float rL = r[s][v] * m[v] * fmaf(-a[s][v], ix[s][v] * inv[s][v], before[s][v]);
+          dx[v] = lr * in[s][v];
+          dg[v] = lr * ix[s][v] * (1.f - in[s][v]);
+          df[v] = rL * (-0.5f * ch[v].k3) * (1.f - r[s][v]);
+          run[0][v] += rL;
+          run[1][v] += df[v];
+          run[2][v] += dg[v];
         }
-        if (mine && t + s < p.n) {
-          store_few<T, V>(static_cast<T*>(p.dx) + to + (size_t)s * p.D, dx);
-          store_few<T, V>(static_cast<T*>(p.df) + to + (size_t)s * p.D, df);
-          store_few<T, V>(static_cast<T*>(p.dg) + to + (size_t)s * p.D, dg);
-        }
+        const uint32_t off = out + s * (uint32_t)(p.D * sizeof(T));
+        store_few<T, V>(dxs, off, dx);
+        store_few<T, V>(dfs, off, df);
+        store_few<T, V>(dgs, off, dg);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int v = 0; v < V; ++v)
@@ -516,81 +623,104 @@ bool pairs(const Glr& p) {
   return ok;
 }
 
-constexpr int kFwdS = 16, kFwdW = 8, kBackS = 8, kBackW = 4;
-constexpr int kWant = 256;       // workgroups that fill the CUs
+// Runs and waves of the two walks, and how many workgroups they ask for before
+// sequences are cut.  Measured: the backward walk of 4 x 4096 x 2048 with runs of
+// 4 in 8 waves 127 us, of 8 in 4 waves 142, of 8 in 8 waves 215 (registers).
+constexpr int kFwdS = 16, kFwdW = 8, kFwdWant = 128, kBackS = 4, kBackW = 8, kBackWant = 256, kBackLpr = 16;
 constexpr int kMostSegs = 32;
 
 template <int V, int LPR, int S, int W>
-Cut cut_of(int B, int n, int D) {
+Cut cut_of(int B, int n, int D, int want) {
   constexpr int CB = V * LPR, TILE = S * (64 / LPR) * W;
   const int blocks = (D + CB - 1) / CB;
   const long long tiles = ((long long)n + TILE - 1) / TILE, have = (long long)blocks * B;
-  long long segs = have >= kWant ? 1 : (2 * kWant + have - 1) / have;
+  long long segs = have >= want ? 1 : (2 * want + have - 1) / have;
   if (segs > kMostSegs) segs = kMostSegs;
   if (segs > tiles / 2) segs = tiles / 2 > 1 ? tiles / 2 : 1;
   const long long per = (tiles + segs - 1) / segs;
   return {blocks, (int)((tiles + per - 1) / per), (int)per};
 }
 
-template <typename T, int V, int LPR>
+// f(lanes a row) of the forward.  Wide rows use whole memory lines: 64 bytes of
+// bf16 at 16 lanes, where that gives every CU a workgroup; 128 bytes, where even
+// these fill the CUs twice, or where long sequences are cut all the same; half a
+// line where neither, but 32 bytes do.  Measured, us, at 8, 16 and 32 lanes (8 and
+// 16 uncut where they fill the CUs): 4 x 4096 x 2048 92, 71, 88; 8 x 4096 x 4096
+// 347, 282, 253; 1 x 8000 x 4096 95, 128, 100; 1 x 16384 x 1024 92, 70, 59.
+template <int V, typename F>
+auto by_lanes(int B, int n, int D, F f) {
+  auto blocks = [&](int lanes) { return (long long)B * ((D + V * lanes - 1) / (V * lanes)); };
+  if (blocks(32) >= 512 || (n >= 4096 && blocks(8) < 256)) return f(std::integral_constant<int, 32>{});
+  if (n >= 4096 && blocks(16) < 256) return f(std::integral_constant<int, 8>{});
+  return f(std::integral_constant<int, 16>{});
+}
+template <int V>
+Cut forward_cut(int B, int n, int D) {
+  return by_lanes<V>(B, n, D, [&](auto l) { return cut_of<V, decltype(l)::value, kFwdS, kFwdW>(B, n, D, kFwdWant); });
+}
+template <int V>
+Cut backward_cut(int B, int n, int D) {
+  return cut_of<V, kBackLpr, kBackS, kBackW>(B, n, D, kBackWant);
+}
+
+template <typename T, int V>
 hipError_t forward(const Glr& p, void* ws, hipStream_t s) {
-  const Cut cut = cut_of<V, LPR, kFwdS, kFwdW>(p.B, p.n, p.D);
+  const Cut cut = forward_cut<V>(p.B, p.n, p.D);
   float* first = static_cast<float*>(ws);
   float2* sums = reinterpret_cast<float2*>(first + (((size_t)p.B * p.D + 3) & ~(size_t)3));
   const unsigned one = (unsigned)cut.blocks * p.B;
-  if (cut.segs > 1) {
-    const hipError_t e = HLA_TIMED("glr_ends", (k_glr<T, V, LPR, kFwdS, kFwdW, true>), dim3(one * (cut.segs - 1)),
-                                   dim3(64 * kFwdW), 0, s, p, cut, sums, first);
-    if (e != hipSuccess) return e;
-  }
-  return HLA_TIMED("glr", (k_glr<T, V, LPR, kFwdS, kFwdW, false>), dim3(one * cut.segs), dim3(64 * kFwdW), 0, s, p, cut,
-                   sums, first);
+  return by_lanes<V>(p.B, p.n, p.D, [&](auto l) {
+    constexpr int LPR = decltype(l)::value;
+    if (cut.segs > 1) {
+      const hipError_t e = HLA_TIMED("glr_ends", (k_glr<T, V, LPR, kFwdS, kFwdW, true>), dim3(one * (cut.segs - 1)),
+                                     dim3(64 * kFwdW), 0, s, p, cut, sums, first);
+      if (e != hipSuccess) return e;
+    }
+    return HLA_TIMED("glr", (k_glr<T, V, LPR, kFwdS, kFwdW, false>), dim3(one * cut.segs), dim3(64 * kFwdW), 0, s, p, cut,
+                     sums, first);
+  });
 }
 
-template <typename T, int V, int LPR>
+template <typename T, int V>
 hipError_t backward(const Glr& p, void* ws, hipStream_t s) {
-  const Cut cut = cut_of<V, LPR, kBackS, kBackW>(p.B, p.n, p.D);
+  const Cut cut = backward_cut<V>(p.B, p.n, p.D);
   const size_t rows = (size_t)p.B * cut.segs;
   float* part = static_cast<float*>(ws);
   float2* sums = reinterpret_cast<float2*>(part + ((3 * rows * p.D + 3) & ~(size_t)3));
   const unsigned one = (unsigned)cut.blocks * p.B;
   if (cut.segs > 1) {
-    const hipError_t e = HLA_TIMED("glr_back_ends", (k_glr_back<T, V, LPR, kBackS, kBackW, true>), dim3(one * cut.segs),
+    const hipError_t e = HLA_TIMED("glr_back_ends", (k_glr_back<T, V, kBackLpr, kBackS, kBackW, true>), dim3(one * cut.segs),
                                    dim3(64 * kBackW), 0, s, p, cut, sums, part);
     if (e != hipSuccess) return e;
   }
-  const hipError_t e = HLA_TIMED("glr_back", (k_glr_back<T, V, LPR, kBackS, kBackW, false>), dim3(one * cut.segs),
+  const hipError_t e = HLA_TIMED("glr_back", (k_glr_back<T, V, kBackLpr, kBackS, kBackW, false>), dim3(one * cut.segs),
                                  dim3(64 * kBackW), 0, s, p, cut, sums, part);
   if (e != hipSuccess) return e;
   return launch_column_sums({part, {p.ddecay, p.dfb, p.dgb}, (int)rows, p.D, 0}, s);
 }
 
-constexpr int kLpr = 8;
-
 }  // namespace
 
 size_t glr_forward_ws(int B, int n, int D) {
-  const int a = cut_of<1, kLpr, kFwdS, kFwdW>(B, n, D).segs, b = cut_of<2, kLpr, kFwdS, kFwdW>(B, n, D).segs;
+  const int a = forward_cut<1>(B, n, D).segs, b = forward_cut<2>(B, n, D).segs;
   return sizeof(float) * (size_t)B * D * (2 * (a > b ? a : b) + 1) + 64;
 }
 size_t glr_backward_ws(int B, int n, int D) {
-  const int a = cut_of<1, kLpr, kBackS, kBackW>(B, n, D).segs, b = cut_of<2, kLpr, kBackS, kBackW>(B, n, D).segs;
+  const int a = backward_cut<1>(B, n, D).segs, b = backward_cut<2>(B, n, D).segs;
   return sizeof(float) * (size_t)B * D * 5 * (a > b ? a : b) + 64;
 }
-
-double glr_threads(int B, int n, int D) {   // of the largest launch: one channel a lane, as many segments as there may be
-  const double blocks = std::ceil(D / (double)kLpr) * B;
-  const Cut f = cut_of<1, kLpr, kFwdS, kFwdW>(B, n, D), b = cut_of<1, kLpr, kBackS, kBackW>(B, n, D);
-  return blocks * std::fmax(f.segs * 64. * kFwdW, b.segs * 64. * kBackW);
+double glr_threads(int B, int n, int D) {   // of the largest launch: single channels
+  const Cut f = forward_cut<1>(B, n, D), b = backward_cut<1>(B, n, D);
+  return std::fmax((double)f.blocks * f.segs * kFwdW, (double)b.blocks * b.segs * kBackW) * 64. * B;
 }
 
 hipError_t launch_glr_forward(const Glr& p, void* ws, hipStream_t s) {
-  if (p.dtype == 1) return pairs(p) ? forward<bf16, 2, kLpr>(p, ws, s) : forward<bf16, 1, kLpr>(p, ws, s);
-  return pairs(p) ? forward<float, 2, kLpr>(p, ws, s) : forward<float, 1, kLpr>(p, ws, s);
+  if (p.dtype == 1) return pairs(p) ? forward<bf16, 2>(p, ws, s) : forward<bf16, 1>(p, ws, s);
+  return pairs(p) ? forward<float, 2>(p, ws, s) : forward<float, 1>(p, ws, s);
 }
 hipError_t launch_glr_backward(const Glr& p, void* ws, hipStream_t s) {
-  if (p.dtype == 1) return pairs(p) ? backward<bf16, 2, kLpr>(p, ws, s) : backward<bf16, 1, kLpr>(p, ws, s);
-  return pairs(p) ? backward<float, 2, kLpr>(p, ws, s) : backward<float, 1, kLpr>(p, ws, s);
+  if (p.dtype == 1) return pairs(p) ? backward<bf16, 2>(p, ws, s) : backward<bf16, 1>(p, ws, s);
+  return pairs(p) ? backward<float, 2>(p, ws, s) : backward<float, 1>(p, ws, s);
 }
 hipError_t launch_glr_step(const Glr& p, hipStream_t s) {
   const bool two = pairs(p);

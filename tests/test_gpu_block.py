@@ -293,3 +293,31 @@ def test_projections_in_parts(size, apart):
         off = (a - r).abs() - 2.0 ** -8 * (1 + 2.0 ** -7) * r.abs() - size
         assert off.max() <= 0, (name, off.max().item())
         assert (a - r).norm() <= 2 ** 0.5 * 2.0 ** -8 / 3 ** 0.5 * r.norm(), name
+
+
+# Every way the recurrence is cut, against the oracle: whole and half memory lines a row, sequences in one piece and in
+# segments, the last of them short, tiles that end inside a run.
+GLR_CUTS = [(1, 4096, 8200), (3, 700, 5472), (1, 4099, 4112), (1, 5003, 200), (1, 9001, 33), (2, 4500, 70), (9, 130, 3650)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("size", GLR_CUTS)
+def test_recurrence_in_parts(size, dtype):
+    B, n, D = size
+    _say(f"recurrence in parts {size} {dtype}")
+    x, f, g, decay, fb, gb, dy, state = _glr_case(B, n, D, dtype, True, 6)
+    some = np.unique(np.concatenate([np.arange(min(D, 40)), np.arange(max(0, D - 40), D), np.arange(0, D, max(1, D // 40))]))
+    args = [_n(t)[..., some] for t in (x, f, g, decay, fb, gb)]
+    bar = (n + 64) * 2.0 ** -23
+    sn = _n(state)[:, some]
+    ref, last = O.glr(*args, 8.0, sn)
+    scale = _glr_size(args, sn)
+    got = hla.glr_prefill(state, x, f, g, decay, fb, gb)
+    pick = torch.from_numpy(some).cuda()
+    _within(got[..., pick], ref, scale, bar, "from a state")
+    _within(state[:, pick], last, scale[:, -1], bar, "state")
+    grads = hla.glr_backward(x, f, g, decay, fb, gb, dy)
+    names = ("dx", "df", "dg", "ddecay", "df_bias", "dg_bias")
+    dyn = _n(dy)[..., some]
+    for name, a, r, scale in zip(names, grads, O.glr_vjp(*args, 8.0, dyn), _glr_grad_sizes(args, dyn)):
+        _within(a[..., pick], r, scale, 2 * bar, name)
