@@ -11,8 +11,6 @@
 // Bound by memory: every input is read once and every output written once.
 // A thread keeps its group and its elements of a row while its block goes over
 // the tokens, so the weight is loaded once and its gradient summed in registers.
-#include <initializer_list>
-
 #include "block.h"
 #include "rows.h"
 
@@ -20,7 +18,6 @@ namespace hla {
 namespace {
 
 constexpr int kBlocks = 2048;       // of a forward, at most, a block of groups
-constexpr int kBackBlocks = 1024;   // of a backward, in all
 
 // A thread's place: slots of LANES threads take the block's groups, then its tokens.
 template <typename S>
@@ -41,22 +38,22 @@ __device__ __forceinline__ size_t at(const Rows3& r, unsigned b, unsigned t, int
   return (size_t)b * r.bs + (size_t)t * r.ts + (size_t)g * r.gs;
 }
 
-template <typename TY, typename T, typename S>
+template <typename TY, typename T, typename S, bool WHOLE>
 __global__ __launch_bounds__(S::THREADS) void k_gated_norm(GatedNorm a) {
   __shared__ float red[2][1][S::WAVES];
   constexpr bool kExact = sizeof(T) == 4;
   const Place<S> p(a.G);
   const unsigned toks = (unsigned)a.B * a.n;
   float w[S::E];
-  load_weight<S>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
+  load_weight<S, WHOLE>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
   int turn = 0;
   for (unsigned t0 = blockIdx.x; t0 * (unsigned long long)p.tokens < toks; t0 += gridDim.x, turn ^= 1) {
     const unsigned long long tok = (unsigned long long)t0 * p.tokens + p.off;
     const bool there = p.there && tok < toks;
     const unsigned b = a.B > 1 ? (unsigned)tok / a.n : 0, t = (unsigned)tok - b * a.n;
     const int d = there ? a.d : 0;
-    RowRaw<TY, S> y;
-    RowRaw<T, S> z;
+    RowRaw<TY, S, WHOLE> y;
+    RowRaw<T, S, WHOLE> z;
     y.load(static_cast<const TY*>(a.y.p) + (there ? at(a.y, b, t, p.g) : 0), d, p.lane);
     if (a.z.p) z.load(static_cast<const T*>(a.z.p) + (there ? at(a.z, b, t, p.g) : 0), d, p.lane);
     float v[S::E], gate[S::E], ss[1] = {0.f};
@@ -76,21 +73,21 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm(GatedNorm a) {
       v[e] *= r * w[e];
       if (a.z.p && a.norm_first) v[e] *= gate[e];
     }
-    store_row<T, S>(static_cast<T*>(a.out) + (there ? ((size_t)tok * a.G + p.g) * a.d : 0), d, p.lane, v);
+    store_row<T, S, WHOLE>(static_cast<T*>(a.out) + (there ? ((size_t)tok * a.G + p.g) * a.d : 0), d, p.lane, v);
   }
 }
 
 // Blocks keep their groups and take every gridDim.x-th share of the tokens; the
 // weight's partial sums: [grid.x][G][d] with a weight for each group, else
 // [grid.x grid.y][d], the block's rows summed in a fixed order.
-template <typename TY, typename T, typename S>
+template <typename TY, typename T, typename S, bool WHOLE>
 __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, float* __restrict__ part) {
   __shared__ float red[2][2][1][S::WAVES];
   constexpr bool kExact = sizeof(TY) == 4;
   const Place<S> p(a.G);
   const unsigned toks = (unsigned)a.B * a.n;
   float w[S::E], dw[S::E];
-  load_weight<S>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
+  load_weight<S, WHOLE>(a.w, a.w_dtype, a.per_group ? (size_t)p.g * a.d : 0, p.there ? a.d : 0, p.lane, w);
 #pragma unroll
   for (int e = 0; e < S::E; ++e) dw[e] = 0.f;
   int turn = 0;
@@ -100,8 +97,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
     const unsigned b = a.B > 1 ? (unsigned)tok / a.n : 0, t = (unsigned)tok - b * a.n;
     const int d = there ? a.d : 0;
     const size_t here = there ? ((size_t)tok * a.G + p.g) * a.d : 0;
-    RowRaw<TY, S> y;
-    RowRaw<T, S> z, go;
+    RowRaw<TY, S, WHOLE> y;
+    RowRaw<T, S, WHOLE> z, go;
     y.load(static_cast<const TY*>(a.y.p) + (there ? at(a.y, b, t, p.g) : 0), d, p.lane);
     go.load(static_cast<const T*>(a.dout) + here, d, p.lane);
     if (a.z.p) z.load(static_cast<const T*>(a.z.p) + (there ? at(a.z, b, t, p.g) : 0), d, p.lane);
@@ -136,8 +133,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
       dy[e] = a.norm_first ? dv : dv * gate;
       dz[e] = (a.norm_first ? go.at(e) * w[e] * v[e] : dv * y.at(e)) * (s * (1.f + zz * (1.f - s)));
     }
-    store_row<TY, S>(static_cast<TY*>(const_cast<void*>(a.dy.p)) + (there ? at(a.dy, b, t, p.g) : 0), d, p.lane, dy);
-    if (a.z.p) store_row<T, S>(static_cast<T*>(a.dz) + here, d, p.lane, dz);
+    store_row<TY, S, WHOLE>(static_cast<TY*>(const_cast<void*>(a.dy.p)) + (there ? at(a.dy, b, t, p.g) : 0), d, p.lane, dy);
+    if (a.z.p) store_row<T, S, WHOLE>(static_cast<T*>(a.dz) + here, d, p.lane, dz);
   }
   if (!a.dw) return;
   if constexpr (S::ROWS == 1) {
@@ -145,9 +142,9 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
 #pragma unroll
     for (int ch = 0; ch < S::CH; ++ch)
 #pragma unroll
-      for (int i = 0; i < S::V; ++i) {
-        const int c = (ch * S::LANES + p.lane) * S::V + i;
-        if (c < a.d) to[c] = dw[ch * S::V + i];
+      for (int i = 0; i < 8; ++i) {
+        const int c = (ch * S::LANES + p.lane) * 8 + i;
+        if (c < a.d) to[c] = dw[ch * 8 + i];
       }
   } else {
     __shared__ float sums[S::ROWS][S::LANES * S::E + 1];
@@ -155,8 +152,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
 #pragma unroll
     for (int ch = 0; ch < S::CH; ++ch)
 #pragma unroll
-      for (int i = 0; i < S::V; ++i)
-        sums[slot][(ch * S::LANES + p.lane) * S::V + i] = p.there ? dw[ch * S::V + i] : 0.f;
+      for (int i = 0; i < 8; ++i)
+        sums[slot][(ch * S::LANES + p.lane) * 8 + i] = p.there ? dw[ch * 8 + i] : 0.f;
     __syncthreads();
     if (a.per_group) {
       for (int e = threadIdx.x; e < per * a.d; e += S::THREADS) {
@@ -193,14 +190,6 @@ __global__ __launch_bounds__(kSumRows * kSumCols) void k_column_sums(ColumnSums 
   store_any(to, c.dtype, col, s);
 }
 
-bool on_16(const void* p, int es, std::initializer_list<long long> strides) {
-  if (reinterpret_cast<uintptr_t>(p) & 15) return false;
-  for (long long st : strides)
-    if (st * es % 16) return false;
-  return true;
-}
-bool on_16(const Rows3& r, int dtype) { return on_16(r.p, dtype == 1 ? 2 : 4, {r.bs, r.ts, r.gs}); }
-
 // Sequences laid one behind the other are one long one: no division by n.
 void flatten(GatedNorm& a) {
   auto joined = [&](const Rows3& r) { return !r.p || a.n == 1 || r.bs == (long long)a.n * r.ts; };
@@ -225,22 +214,23 @@ Grid grid_of(int B, int n, int G, int most) {
   return {(int)(shares < x ? shares : x), gy};
 }
 
-template <typename TY, typename T, bool VEC>
+template <typename TY, typename T, bool WHOLE>
 hipError_t forward(const GatedNorm& a, hipStream_t s) {
-  return by_row<VEC>(a.d, [&](auto shape) {
+  return by_row<false>(a.d, [&](auto shape) {
     using S = decltype(shape);
     const Grid g = grid_of<S>(a.B, a.n, a.G, kBlocks * ((a.G + S::ROWS - 1) / S::ROWS));
-    return HLA_TIMED("gated_norm", (k_gated_norm<TY, T, S>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a);
+    return HLA_TIMED("gated_norm", (k_gated_norm<TY, T, S, WHOLE>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a);
   });
 }
 
-template <typename TY, typename T, bool VEC>
+template <typename TY, typename T, bool WHOLE>
 hipError_t backward(const GatedNorm& a, float* part, hipStream_t s) {
   Grid g{};
-  const hipError_t e = by_row<VEC>(a.d, [&](auto shape) {
+  const hipError_t e = by_row<true>(a.d, [&](auto shape) {
     using S = decltype(shape);
-    g = grid_of<S>(a.B, a.n, a.G, kBackBlocks);
-    return HLA_TIMED("gated_norm_back", (k_gated_norm_back<TY, T, S>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a, part);
+    g = grid_of<S>(a.B, a.n, a.G, back_blocks<S>());
+    return HLA_TIMED("gated_norm_back", (k_gated_norm_back<TY, T, S, WHOLE>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a,
+                     part);
   });
   if (e != hipSuccess || !a.dw) return e;
   ColumnSums c{part, {a.dw, nullptr, nullptr}, a.per_group ? g.x : g.x * g.y, a.per_group ? a.G * a.d : a.d, a.w_dtype};
@@ -248,20 +238,16 @@ hipError_t backward(const GatedNorm& a, float* part, hipStream_t s) {
 }
 
 template <typename TY, typename T>
-hipError_t by_layout(GatedNorm a, bool back, float* part, hipStream_t s) {
+hipError_t by_width(GatedNorm a, bool back, float* part, hipStream_t s) {
   flatten(a);
-  bool vec = a.d % 8 == 0 && on_16(a.y, a.y_dtype) && (!a.z.p || on_16(a.z, a.dtype));
-  if (back)
-    vec = vec && on_16(a.dy, a.y_dtype) && on_16(a.dout, 2, {}) && (!a.dz || on_16(a.dz, 2, {}));
-  else
-    vec = vec && on_16(a.out, 2, {});
-  if (back) return vec ? backward<TY, T, true>(a, part, s) : backward<TY, T, false>(a, part, s);
-  return vec ? forward<TY, T, true>(a, s) : forward<TY, T, false>(a, s);
+  const bool whole = a.d % 8 == 0;
+  if (back) return whole ? backward<TY, T, true>(a, part, s) : backward<TY, T, false>(a, part, s);
+  return whole ? forward<TY, T, true>(a, s) : forward<TY, T, false>(a, s);
 }
 
 hipError_t by_type(const GatedNorm& a, bool back, float* part, hipStream_t s) {
-  if (a.dtype == 0) return by_layout<float, float>(a, back, part, s);
-  return a.y_dtype == 0 ? by_layout<float, bf16>(a, back, part, s) : by_layout<bf16, bf16>(a, back, part, s);
+  if (a.dtype == 0) return by_width<float, float>(a, back, part, s);
+  return a.y_dtype == 0 ? by_width<float, bf16>(a, back, part, s) : by_width<bf16, bf16>(a, back, part, s);
 }
 
 }  // namespace
@@ -273,12 +259,11 @@ hipError_t launch_column_sums(const ColumnSums& c, hipStream_t s) {
 
 hipError_t launch_gated_norm(const GatedNorm& a, hipStream_t s) { return by_type(a, false, nullptr, s); }
 size_t gated_norm_backward_ws(int B, int n, int G, int d, int per_group) {
-  auto rows = [&](auto shape) {
-    const Grid g = grid_of<decltype(shape)>(B, n, G, kBackBlocks);
-    return (size_t)g.x * (per_group ? G : g.y);
-  };
-  const size_t narrow = by_row<false>(d, rows), wide = by_row<true>(d, rows);
-  return sizeof(float) * (narrow > wide ? narrow : wide) * d;
+  return by_row<true>(d, [&](auto shape) {
+    using S = decltype(shape);
+    const Grid g = grid_of<S>(B, n, G, back_blocks<S>());
+    return sizeof(float) * g.x * (size_t)(per_group ? G : g.y) * d;
+  });
 }
 hipError_t launch_gated_norm_backward(const GatedNorm& a, void* ws, hipStream_t s) {
   return by_type(a, true, static_cast<float*>(ws), s);

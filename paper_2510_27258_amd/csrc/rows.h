@@ -1,92 +1,139 @@
 // Rows of a normed dimension held by groups of lanes, for the norm kernels.
 // A row of d elements lies in the registers of LANES neighbouring threads, CH
-// vectors of V elements each: element (ch LANES + lane) V + i.  V = 8 needs
-// rows on 16-byte boundaries, V = 1 takes any.
+// pieces of eight elements each: element (ch LANES + lane) 8 + i.  Pieces are
+// read and written 16 bytes at once wherever a row begins (the hardware takes
+// any address of its element's alignment); with !WHOLE a row's last piece may be
+// a part of one, which goes element by element.
 #pragma once
+#include <type_traits>
+
 #include "lanes.h"
 #include "vec.h"
 
 namespace hla {
 
-template <int V_, int CH_, int LANES_>
+template <int CH_, int LANES_>
 struct RowShape {
-  static constexpr int V = V_, CH = CH_, LANES = LANES_, E = V * CH;
+  static constexpr int CH = CH_, LANES = LANES_, E = 8 * CH;
   static constexpr int THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, WAVES = (LANES + 63) / 64;
 };
 
-// One vector as it lies in memory, loaded ahead of its use.
-template <typename T, typename S>
+typedef uint32_t any4 __attribute__((ext_vector_type(4)));
+typedef any4 any4_at2 __attribute__((aligned(2)));
+typedef any4 any4_at4 __attribute__((aligned(4)));
+template <typename T>
+struct Piece {   // eight values as they lie in memory
+  static constexpr int N = sizeof(T) / 2;      // of 16 bytes
+  using any4_at = std::conditional_t<sizeof(T) == 2, any4_at2, any4_at4>;
+  any4 w[N];
+
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = (any4)0;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const any4_at*>(p)[i];
+  }
+  __device__ __forceinline__ void load_first(const T* p, int n) {
+    zero();
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+      if (i >= n) continue;
+      if constexpr (sizeof(T) == 2)
+        w[0][i / 2] |= (uint32_t)p[i].bits << (16 * (i & 1));
+      else
+        w[i / 4][i % 4] = __float_as_uint(p[i]);
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) reinterpret_cast<any4_at*>(p)[i] = w[i];
+  }
+  __device__ __forceinline__ void store_first(T* p, int n) const {
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+      if (i >= n) continue;
+      if constexpr (sizeof(T) == 2)
+        p[i].bits = (uint16_t)(w[0][i / 2] >> (16 * (i & 1)));
+      else
+        p[i] = __uint_as_float(w[i / 4][i % 4]);
+    }
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 2)
+      return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
+    else
+      return __uint_as_float(w[i / 4][i % 4]);
+  }
+  __device__ __forceinline__ void set(const float* v) {
+    if constexpr (sizeof(T) == 2) {
+      typedef float f2 __attribute__((ext_vector_type(2)));
+      typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2 * i], v[2 * i + 1]}, b2));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i / 4][i % 4] = __float_as_uint(v[i]);
+    }
+  }
+};
+
+// A row as it lies in memory, zeros past d.
+template <typename T, typename S, bool WHOLE>
 struct RowRaw {
-  Raw<T, S::V> v[S::CH];
+  Piece<T> v[S::CH];
   __device__ __forceinline__ void load(const T* row, int d, int lane) {
 #pragma unroll
     for (int ch = 0; ch < S::CH; ++ch) {
-      const int c = (ch * S::LANES + lane) * S::V;
+      const int c = (ch * S::LANES + lane) * 8;
       v[ch].zero();
-      if (c < d) v[ch].load(row + c);
+      if (WHOLE ? c < d : c + 8 <= d)
+        v[ch].load(row + c);
+      else if (!WHOLE && c < d)
+        v[ch].load_first(row + c, d - c);
     }
   }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int ch = 0; ch < S::CH; ++ch) v[ch].zero();
   }
-  __device__ __forceinline__ float at(int e) const { return v[e / S::V].at(e % S::V); }
+  __device__ __forceinline__ float at(int e) const { return v[e / 8].at(e % 8); }
 };
 
-template <typename T, typename S>
+template <typename T, typename S, bool WHOLE>
 __device__ __forceinline__ void store_row(T* row, int d, int lane, const float (&v)[S::E]) {
 #pragma unroll
   for (int ch = 0; ch < S::CH; ++ch) {
-    const int c = (ch * S::LANES + lane) * S::V;
-    if (c >= d) continue;
-    if constexpr (S::V == 1) {
-      const float o[1] = {v[ch]};
-      store_vec<T, 1>(row + c, o);
-    } else if constexpr (sizeof(T) == 2) {
-      float o[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = v[ch * 8 + i];
-      store_vec<T, 8>(row + c, o);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = v[ch * 8 + h * 4 + i];
-        store_vec<T, 4>(row + c + h * 4, o);
-      }
-    }
+    const int c = (ch * S::LANES + lane) * 8;
+    Piece<T> p;
+    p.set(v + ch * 8);
+    if (WHOLE ? c < d : c + 8 <= d)
+      p.store(row + c);
+    else if (!WHOLE && c < d)
+      p.store_first(row + c, d - c);
   }
 }
 
 // A weight row of run-time type (null: ones) from element `first`, zeros past d.
-template <typename S>
+template <typename S, bool WHOLE>
 __device__ __forceinline__ void load_weight(const void* w, int dtype, size_t first, int d, int lane, float (&v)[S::E]) {
-  const bool wide = w && S::V == 8 && ((reinterpret_cast<uintptr_t>(w) + first * (dtype == 1 ? 2 : 4)) & 15) == 0;
+  auto take = [&](const auto& raw) {
 #pragma unroll
-  for (int ch = 0; ch < S::CH; ++ch) {
-    const int c = (ch * S::LANES + lane) * S::V;
+    for (int e = 0; e < S::E; ++e) v[e] = raw.at(e);
+  };
+  if (!w) {
 #pragma unroll
-    for (int i = 0; i < S::V; ++i) v[ch * S::V + i] = 0.f;
-    if (c >= d) continue;
-    if constexpr (S::V == 8) {
-      if (wide && dtype == 1) {
-        Raw<bf16, 8> r;
-        r.load(static_cast<const bf16*>(w) + first + c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[ch * 8 + i] = r.at(i);
-        continue;
-      }
-      if (wide) {
-        Raw<float, 8> r;
-        r.load(static_cast<const float*>(w) + first + c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[ch * 8 + i] = r.at(i);
-        continue;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < S::V; ++i) v[ch * S::V + i] = w ? load_any(w, dtype, first + c + i) : 1.f;
+    for (int e = 0; e < S::E; ++e) v[e] = (e / 8 * S::LANES + lane) * 8 + e % 8 < d ? 1.f : 0.f;
+  } else if (dtype == 1) {
+    RowRaw<bf16, S, WHOLE> raw;
+    raw.load(static_cast<const bf16*>(w) + first, d, lane);
+    take(raw);
+  } else {
+    RowRaw<float, S, WHOLE> raw;
+    raw.load(static_cast<const float*>(w) + first, d, lane);
+    take(raw);
   }
 }
 
@@ -126,24 +173,29 @@ __device__ __forceinline__ float sigmoid(float z) {
 }
 
 // f(Shape) with the narrowest shape for rows of d elements.
-template <bool VEC, typename F>
+template <bool BACK, typename F>
 auto by_row(int d, F f) {
-  if constexpr (VEC) {
-    if (d <= 64) return f(RowShape<8, 1, 8>{});
-    if (d <= 128) return f(RowShape<8, 1, 16>{});
-    if (d <= 256) return f(RowShape<8, 1, 32>{});
-    if (d <= 512) return f(RowShape<8, 1, 64>{});
-    if (d <= 1024) return f(RowShape<8, 2, 64>{});
-    if (d <= 2048) return f(RowShape<8, 1, 256>{});
-    if (d <= 4096) return f(RowShape<8, 2, 256>{});
-    if (d <= 8192) return f(RowShape<8, 4, 256>{});
-    return f(RowShape<8, 4, 512>{});
+  if (d <= 64) return f(RowShape<1, 8>{});
+  if (d <= 128) return f(RowShape<1, 16>{});
+  if (d <= 256) return f(RowShape<1, 32>{});
+  if (d <= 512) return f(RowShape<1, 64>{});
+  if (d <= 1024) return f(RowShape<2, 64>{});
+  if (d <= 2048) return f(RowShape<1, 256>{});
+  if constexpr (BACK) {
+    if (d <= 4096) return f(RowShape<1, 512>{});
+    if (d <= 8192) return f(RowShape<2, 512>{});
+    return f(RowShape<4, 512>{});     // holds more than its registers: slow
   } else {
-    if (d <= 64) return f(RowShape<1, 8, 8>{});
-    if (d <= 512) return f(RowShape<1, 8, 64>{});
-    if (d <= 2048) return f(RowShape<1, 8, 256>{});
-    return f(RowShape<1, 32, 512>{});
+    if (d <= 4096) return f(RowShape<2, 256>{});
+    if (d <= 8192) return f(RowShape<2, 512>{});
+    return f(RowShape<2, 1024>{});
   }
+}
+
+// Workgroups of a backward: a row of partial sums each, so fewer where rows are wide.
+template <typename S>
+constexpr int back_blocks() {
+  return S::THREADS <= 256 ? 1024 : 512;
 }
 
 }  // namespace hla
