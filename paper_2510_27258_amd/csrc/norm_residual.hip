@@ -90,8 +90,6 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
   constexpr bool kAhead = S::CH == 1 && S::WAVES > 1;
   RowRaw<TX, S, WHOLE> x1, gr1;
   RowRaw<T, S, WHOLE> y1, go1;
-  go1.zero();
-  gr1.zero();
   auto load = [&](unsigned long long r0) {
     const unsigned long long row = r0 + threadIdx.x / S::LANES;
     const bool there = row < rows;
@@ -99,8 +97,8 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
     const size_t here = there ? (size_t)row * a.D : 0;
     x1.load(static_cast<const TX*>(a.x.p) + (there ? at(a.x, a, (unsigned)row) : 0), d, lane);
     y1.load(static_cast<const T*>(a.y.p) + (there ? at(a.y, a, (unsigned)row) : 0), d, lane);
-    if (a.dout) go1.load(static_cast<const T*>(a.dout) + here, d, lane);
-    if (a.dr) gr1.load(static_cast<const TX*>(a.dr) + here, d, lane);
+    go1.load(static_cast<const T*>(a.dout) + here, a.dout ? d : 0, lane);
+    gr1.load(static_cast<const TX*>(a.dr) + here, a.dr ? d : 0, lane);
   };
   if constexpr (kAhead) load((unsigned long long)blockIdx.x * S::ROWS);
   int turn = 0;
