@@ -16,9 +16,9 @@ from .autograd import once
 from .mixer import _CODES, _code, _launch, _learns, _on_gpu, _out, _ptr, _rows, _same, _space, _upstream
 
 
-def _weights_type(like, **weights):
-    """The type that the weights given share, like's where there is none."""
-    wtype = next((w.dtype for w in weights.values() if w is not None), like.dtype)
+def _weights_type(*weights):
+    """The type of the first weight given; they are held to it."""
+    wtype = next((w.dtype for w in weights if w is not None), torch.float32)
     if wtype not in _CODES:
         raise TypeError(f"weights must be float32 or bfloat16, got {wtype}")
     return wtype
@@ -42,7 +42,7 @@ def _gated_args(y, z, weight, dtype):
     _same("z", z, y.shape, dtype, y.device)
     per_group = int(weight is not None and weight.dim() == 2)
     _same("weight", weight, (G, d) if per_group else (d,), None, y.device, contiguous=True)
-    wtype = _weights_type(y, weight=weight)
+    wtype = _weights_type(weight)
     _on_gpu(y)
     code, ycode = _CODES.get(dtype), _code("y", y)
     if code is None:
@@ -113,7 +113,7 @@ def _residual_args(x, y, weight, post_weight, scale):
     if x.dim() != 3:
         raise ValueError(f"x must have 3 dimensions [B, n, D], got shape {tuple(x.shape)}")
     _same("y", y, x.shape, None, x.device)
-    wtype = _weights_type(y, weight=weight, post_weight=post_weight, scale=scale)
+    wtype = _weights_type(weight, post_weight, scale)
     for name, w in (("weight", weight), ("post_weight", post_weight), ("scale", scale)):
         _same(name, w, x.shape[-1:], wtype, x.device, contiguous=True)
     _on_gpu(x)
