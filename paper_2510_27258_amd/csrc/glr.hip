@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_glr_back(Glr p, Cut cut, float2* 
       __builtin_amdgcn_sched_barrier(0);
     }
     if (k > 0) load_start(t0 - TILE);
-    if (!whole) {               // tokens past the end change nothing
+    if (!whole) {               // tokens past the end change nothing, whatever was loaded for them
 #pragma unroll
       for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_glr_back(Glr p, Cut cut, float2* 
           if (t + s >= p.n) {
             a[s][v] = 1.f;
             dys[s][v] = 0.f;
-            if constexpr (!ENDS) root[s][v] = ix[s][v] = 0.f;
+            if constexpr (!ENDS) root[s][v] = ix[s][v] = r[s][v] = in[s][v] = 0.f;
           }
     }
 #pragma unroll

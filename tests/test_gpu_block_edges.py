@@ -97,6 +97,25 @@ def test_repeated_and_padded_rows(name):
             assert _same(u, v)
 
 
+@pytest.mark.parametrize("which", [0, 1, 2, 3])
+def test_rows_that_overlap_keep_bad_values_in_their_channel(which):
+    """x, f, g or dy in rows of 64 that begin 32 elements apart: what lies where a token behind the last would is the
+    last token's channels 32 to 63.  A NaN there spoils its own channel's sums and no other's."""
+    x, f, g, decay, fb, gb, dy, _ = _glr_case(1, 37, 64, FP32, True, 15)
+    inputs = [t.contiguous() for t in (x, f, g, dy)]
+    flat = torch.randn(36 * 32 + 64, generator=torch.Generator().manual_seed(16)).cuda()
+    got = []
+    for bad in (False, True):
+        if bad:
+            flat[36 * 32 + 32 + 3] = float("nan")                       # token 36's channel 35; token 37's channel 3
+        inputs[which] = flat.as_strided((1, 37, 64), (0, 32, 1))
+        got.append(hla.glr_backward(*inputs[:3], decay, fb, gb, inputs[3]))
+    others = torch.arange(64, device="cuda") != 35
+    for a, b in zip(*got):
+        assert torch.isfinite(b[..., others]).all() and _same(a[..., others], b[..., others])
+    assert not torch.isfinite(got[1][3][35])
+
+
 # ----------------------------------------------------------------------------
 def test_zero_rows_and_eps():
     z = torch.zeros(2, 5, 3, 40, device="cuda", dtype=BF16)
