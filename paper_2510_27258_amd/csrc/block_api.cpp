@@ -119,6 +119,11 @@ int glr_check(hla::Glr& p) {
 }
 
 // ---------------------------------------------------------------------------
+// Whether tiles of 512 threads over rows x cols exceed a launch.
+bool glu_over(double rows, double tall, double cols, double wide, double times = 1.) {
+  return times * std::ceil(rows / tall) * std::ceil(cols / wide) * 512 >= 4294967296.0;
+}
+
 int glu_sizes(int B, int n, int D, int F) {
   const int rc = check_tokens(B, n);
   if (rc) return rc;
@@ -126,10 +131,8 @@ int glu_sizes(int B, int n, int D, int F) {
   if (D % 8 || F % 8) return fail(HLA_ERR_UNSUPPORTED, "D and F must be multiples of 8 (got D=%d F=%d)", D, F);
   if (D > 1 << 20 || F > 1 << 20) return fail(HLA_ERR_UNSUPPORTED, "D and F must be at most 2^20 (got D=%d F=%d)", D, F);
   // A launch has less than 2^32 threads: 512 a tile of 128 tokens and 64 outputs, or 256 x 256 of a gradient.
-  auto over = [](double rows, double each) { return std::ceil(rows / each); };
   const double M = (double)B * n;
-  if (B * over(n, 128) * over(F, 64) * 512 >= 4294967296.0 || over(M, 256) * over(D, 256) * 512 >= 4294967296.0 ||
-      over(D, 256) * over(2. * F, 256) * 512 >= 4294967296.0 || M + 256 >= 2147483648.0)
+  if (glu_over(M, 128, F, 64) || glu_over(M, 256, D, 256) || glu_over(D, 256, 2. * F, 256) || M + 256 >= 2147483648.0)
     return fail(HLA_ERR_UNSUPPORTED, "B=%d n=%d D=%d F=%d: too many tiles for a launch", B, n, D, F);
   return HLA_OK;
 }
@@ -146,6 +149,10 @@ int glu_check(hla::Glu& p, int act, int dtype) {
   // a tile's 256 rows are addressed with 31-bit byte offsets (of single tokens the stride between sequences)
   const long long far = p.n == 1 ? p.x.bs : p.x.ts;
   if (far > (1LL << 22) - 8192) return fail(HLA_ERR_UNSUPPORTED, "x: a token stride of %lld elements is too long", far);
+  // a tile lies in one sequence, unless they lie one behind the other
+  auto apart = [&](const hla::Rows& r) { return r.p && r.bs != p.n * r.ts; };
+  if (p.B > 1 && p.n > 1 && (apart(p.x) || apart(p.dh)) && glu_over(p.n, 128, p.F, 64, p.B))
+    return fail(HLA_ERR_UNSUPPORTED, "B=%d n=%d F=%d: too many tiles for a launch of sequences laid apart", p.B, p.n, p.F);
   p.gelu = act == HLA_ACT_GELU;
   return HLA_OK;
 }

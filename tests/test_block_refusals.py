@@ -154,6 +154,16 @@ def test_projections(back, kw, code, text):
     _refused(_glu(back, **kw), code, text)
 
 
+def test_projections_of_many_short_sequences():
+    """Sequences laid one behind the other are tiled as one; apart, each has tiles of its own."""
+    many = dict(B=1 << 20, F=1 << 14)
+    _refused(_glu(n=2, xb=128, **many), INVALID, "h is NULL")
+    _refused(_glu(n=1, xb=72, **many), INVALID, "h is NULL")
+    _refused(_glu(n=2, xb=192, **many), UNSUP, "laid apart")
+    _refused(_glu(True, n=2, xb=128, dht=1 << 14, **many), UNSUP, "laid apart")       # dh's batches lie on one another
+    assert capi.hla_glu_backward_workspace_bytes(1 << 20, 2, 64, 1 << 14) > 0
+
+
 def test_projections_pointers_and_workspace():
     _refused(_glu(), INVALID, "h is NULL")
     _refused(_glu(h=P + 8), INVALID, "h is not 16-byte")
