@@ -54,6 +54,15 @@ def _calls(seed, B=2, n=37, D=72, dtype=BF16):
     return calls
 
 
+# of the calls above: named without making one, which takes a GPU
+NAMES = ["few projections", "gated norm", "gated norm back", "projections", "projections back", "recurrence", "recurrence back",
+         "residual norm", "residual norm back", "step"]
+
+
+def test_every_call_is_named():
+    assert sorted(_calls(0)) == NAMES
+
+
 # ----------------------------------------------------------------------------
 @pytest.mark.parametrize("D", [72, 71])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
@@ -75,7 +84,7 @@ def test_any_address_of_the_elements_type(dtype, D):
                 assert torch.allclose(u.float(), v.float(), rtol=2 ** -7 if u.dtype == BF16 else 1e-5, atol=1e-4)
 
 
-@pytest.mark.parametrize("name", sorted(_calls(0)))
+@pytest.mark.parametrize("name", NAMES)
 def test_repeated_and_padded_rows(name):
     """Batches, tokens or groups with a stride of zero, and rows of a wider tensor, give what a copy gives."""
     call, args = _calls(12)[name]
@@ -316,7 +325,7 @@ def test_offsets_past_32_bits():
 
 
 # ----------------------------------------------------------------------------
-@pytest.mark.parametrize("name", sorted(_calls(0)))
+@pytest.mark.parametrize("name", NAMES)
 def test_other_streams_and_repeats(name):
     """Two calls at once on streams of their own, and again: one result."""
     first, second = _calls(17, n=900), _calls(18, n=900)
@@ -333,7 +342,7 @@ def test_other_streams_and_repeats(name):
             assert all(_same(a, b) for a, b in zip(got, ref))
 
 
-@pytest.mark.parametrize("name", sorted(_calls(0)))
+@pytest.mark.parametrize("name", NAMES)
 def test_captured_graphs(name):
     """Captured once, replayed on new inputs between eager work: the eager results."""
     call, args = _calls(19, n=260)[name]
