@@ -18,20 +18,31 @@ from .mixer import _CODES, _code, _launch, _learns, _on_gpu, _out, _ptr, _rows, 
 
 def _weights_type(*weights):
     """The type of the first weight given; they are held to it."""
-    wtype = next((w.dtype for w in weights if w is not None), torch.float32)
+    wtype = torch.float32
+    for w in weights:
+        if w is not None:
+            wtype = w.dtype
+            break
     if wtype not in _CODES:
         raise TypeError(f"weights must be float32 or bfloat16, got {wtype}")
     return wtype
+
+
+def _fresh(like, dtype=None):
+    """An output of this shape, contiguous (torch.empty takes twice as long)."""
+    return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
 
 
 # ----------------------------------------------------------------------------
 # Norm of a mixer's output with its gate
 def _rows3(name, t):
     """(address, elements between batches, tokens, groups) of t [B, n, G, d]."""
-    if t.shape[-1] != 1 and t.stride(-1) != 1:
+    B, n, G, d = t.shape
+    bs, ts, gs, one = t.stride()
+    if d != 1 and one != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous, got shape {tuple(t.shape)} with strides "
                          f"{t.stride()}")
-    return t.data_ptr(), *(t.stride(i) if t.shape[i] != 1 else 0 for i in range(3))
+    return t.data_ptr(), bs if B != 1 else 0, ts if n != 1 else 0, gs if G != 1 else 0
 
 
 def _gated_args(y, z, weight, dtype):
@@ -64,7 +75,7 @@ def gated_norm_forward(y, z=None, weight=None, eps=1e-6, norm_first=False, out_d
     o.transpose(1, 2) of an attention's [B, G, n, d] is fine."""
     dtype = _out_type(y, z, out_dtype)
     lead, sizes, codes = _gated_args(y, z, weight, dtype)
-    out = torch.empty(y.shape, dtype=dtype, device=y.device)
+    out = _fresh(y, dtype)
     _launch(capi.hla_gated_norm, y, *lead, out.data_ptr(), *sizes, int(bool(norm_first)), float(eps), *codes)
     return out
 
@@ -76,8 +87,8 @@ def gated_norm_backward(y, z, weight, dout, eps=1e-6, norm_first=False):
     _same("dout", dout, y.shape, None, y.device, contiguous=True)
     dy = torch.empty_like(y)
     if y.shape[-1] != 1 and dy.stride(-1) != 1:
-        dy = torch.empty(y.shape, dtype=y.dtype, device=y.device)
-    dz = None if z is None else torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        dy = _fresh(y)
+    dz = None if z is None else _fresh(z)
     dw = None if weight is None else torch.empty_like(weight)
     ws, nb = _space(capi.hla_gated_norm_backward_workspace_bytes(*sizes), y.device)
     _launch(capi.hla_gated_norm_backward, y, *lead, dout.data_ptr(), *_rows3("dy", dy), _ptr(dz), _ptr(dw), *sizes,
@@ -114,8 +125,9 @@ def _residual_args(x, y, weight, post_weight, scale):
         raise ValueError(f"x must have 3 dimensions [B, n, D], got shape {tuple(x.shape)}")
     _same("y", y, x.shape, None, x.device)
     wtype = _weights_type(weight, post_weight, scale)
+    device, row = x.device, x.shape[-1:]
     for name, w in (("weight", weight), ("post_weight", post_weight), ("scale", scale)):
-        _same(name, w, x.shape[-1:], wtype, x.device, contiguous=True)
+        _same(name, w, row, wtype, device, contiguous=True)
     _on_gpu(x)
     codes = _code("x", x), _code("y", y), _CODES[wtype]
     return (*_rows("x", x, 1), *_rows("y", y, 1), _ptr(weight), _ptr(post_weight), _ptr(scale)), tuple(x.shape), codes
@@ -128,8 +140,7 @@ def residual_norm_forward(x, y, weight=None, post_weight=None, scale=None, alpha
     sqrt(mean(r^2) + eps) of y's type, r of x's type).  weight, post_weight and
     scale [D] share a type; x may be fp32 beside a bf16 y."""
     lead, sizes, codes = _residual_args(x, y, weight, post_weight, scale)
-    out = torch.empty(x.shape, dtype=y.dtype, device=x.device)
-    r = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    out, r = _fresh(y), _fresh(x)
     _launch(capi.hla_residual_norm, x, *lead, out.data_ptr(), r.data_ptr(), *sizes, float(alpha), float(eps), *codes)
     return out, r
 
@@ -141,7 +152,7 @@ def residual_norm_backward(x, y, weight, post_weight, scale, dout, dr, alpha=1.0
     lead, sizes, codes = _residual_args(x, y, weight, post_weight, scale)
     _same("dout", dout, x.shape, y.dtype, x.device, contiguous=True)
     _same("dr", dr, x.shape, x.dtype, x.device, contiguous=True)
-    dx, dy = (torch.empty(x.shape, dtype=t.dtype, device=x.device) for t in (x, y))
+    dx, dy = _fresh(x), _fresh(y)
     dws = tuple(None if w is None else torch.empty_like(w) for w in (weight, post_weight, scale))
     ws, nb = _space(capi.hla_residual_norm_backward_workspace_bytes(*sizes), x.device)
     _launch(capi.hla_residual_norm_backward, x, *lead, _ptr(dout), _ptr(dr), dx.data_ptr(), dy.data_ptr(),
@@ -180,10 +191,12 @@ def residual_norm(x, y, weight=None, post_weight=None, scale=None, alpha=1.0, ep
 def _glr_args(x, f, g, decay, f_bias, g_bias, rank):
     if x.dim() != rank:
         raise ValueError(f"x must have {rank} dimensions, got shape {tuple(x.shape)}")
-    _same("f", f, x.shape, x.dtype, x.device)
-    _same("g", g, x.shape, x.dtype, x.device)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    _same("f", f, shape, dtype, device)
+    _same("g", g, shape, dtype, device)
+    row = shape[-1:]
     for name, t in (("decay", decay), ("f_bias", f_bias), ("g_bias", g_bias)):
-        _same(name, t, x.shape[-1:], torch.float32, x.device, contiguous=True)
+        _same(name, t, row, torch.float32, device, contiguous=True)
     _on_gpu(x)
     return (_rows("x", x, 1), _rows("f", f, 1), _rows("g", g, 1)), (decay.data_ptr(), _ptr(f_bias), _ptr(g_bias)), \
         _code("x", x)
@@ -241,7 +254,7 @@ def glr_backward(x, f, g, decay, f_bias, g_bias, dy, c=8.0, kept=None):
     if kept is None:
         kept = _glr(None, x, f, g, decay, f_bias, g_bias, c, None, None, keep=True)[1]
     _same("kept", kept, (capi.hla_glr_kept_bytes(B, n, D) // 4,), torch.float32, x.device, contiguous=True)
-    dx, df, dg = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(3))
+    dx, df, dg = _fresh(x), _fresh(x), _fresh(x)
     dd, dfb, dgb = (None if t is None else torch.empty_like(t) for t in (decay, f_bias, g_bias))
     ws, nb = _space(capi.hla_glr_backward_workspace_bytes(B, n, D), x.device)
     _launch(capi.hla_glr_backward, x, *rx, *rf, *rg, *params, kept.data_ptr(), *ry, dx.data_ptr(), df.data_ptr(),
@@ -307,7 +320,7 @@ def glu_backward(x, w_gate, w_up, dh, act="silu"):
     """Gradients (dx, dw_gate, dw_up) of glu_forward for dh [B, n, F]; both projections are formed again."""
     rows, sizes, codes = _glu_args(x, w_gate, w_up, act)
     _same("dh", dh, (*sizes[:2], sizes[3]), x.dtype, x.device)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = _fresh(x)
     dwg, dwu = torch.empty_like(w_gate), torch.empty_like(w_up)
     ws, nb = _space(capi.hla_glu_backward_workspace_bytes(*sizes), x.device)
     _launch(capi.hla_glu_backward, x, *rows, w_gate.data_ptr(), w_up.data_ptr(), *_rows("dh", dh, 1), dx.data_ptr(),

@@ -29,15 +29,15 @@ def _rows(name, t, inner):
     """(address, elements between batches, elements between tokens) of t, whose
     last `inner` dimensions must be one contiguous row.  The stride of a
     dimension of size one is not used."""
-    want = 1
+    want, shape, strides = 1, t.shape, t.stride()
     for i in range(1, inner + 1):
-        if t.shape[-i] != 1 and t.stride(-i) != want:
-            raise ValueError(f"{name}: the last {inner} dimension(s) must be contiguous, got shape {tuple(t.shape)} "
-                             f"with strides {t.stride()}")
-        want *= t.shape[-i]
-    lead = t.dim() - inner
-    bs = t.stride(0) if t.shape[0] != 1 else 0
-    ts = t.stride(1) if lead == 2 and t.shape[1] != 1 else 0
+        if strides[-i] != want and shape[-i] != 1:
+            raise ValueError(f"{name}: the last {inner} dimension(s) must be contiguous, got shape {tuple(shape)} "
+                             f"with strides {strides}")
+        want *= shape[-i]
+    lead = len(shape) - inner
+    bs = strides[0] if shape[0] != 1 else 0
+    ts = strides[1] if lead == 2 and shape[1] != 1 else 0
     return t.data_ptr(), bs, ts
 
 
@@ -49,7 +49,7 @@ def _same(what, t, shape, dtype=None, device=None, contiguous=False):
     """t, optional, must have this shape (and type, device, layout)."""
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
@@ -98,6 +98,8 @@ def _learns(*tensors):
 
 
 def _out(out, shape, like, name="out"):
+    if out is None and like.shape == shape:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     if out is None:
         return torch.empty(shape, dtype=like.dtype, device=like.device)
     _same(name, out, shape, like.dtype, like.device, contiguous=True)
