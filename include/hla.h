@@ -587,7 +587,7 @@ int hla_glu_forward(const void *x, long long x_bs, long long x_ts, const void *w
 
 /* hla_glu_backward — its gradients for dh [B, n, F] (strides as x's): dx
  * [B, n, D], dw_gate, dw_up [F, D].  The gradients of the two projections are
- * rounded to bf16 before they meet weights and inputs (2^-9 of a term).
+ * rounded to bf16 before they meet weights and inputs (up to 2^-8 of a term).
  * workspace: at least hla_glu_backward_workspace_bytes(...) bytes. */
 size_t hla_glu_backward_workspace_bytes(int B, int n, int D, int F);
 int hla_glu_backward(const void *x, long long x_bs, long long x_ts, const void *w_gate, const void *w_up,

@@ -8,7 +8,7 @@
 //   dw = sum g hat_r,  dpost = sum du hat_y,  dscale = sum alpha u dr.
 // out is made from the fp32 r, not from the rounded one that goes on, and the
 // gradients form r again from x and y: a bf16 r would cost the weight's
-// gradient 2^-9 of every term.
+// gradient up to 2^-8 of every term.
 //
 // Bound by memory: every input is read once and every output written once.  A
 // thread keeps its elements of a row while its block goes over the rows, so the
