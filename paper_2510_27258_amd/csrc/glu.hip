@@ -50,8 +50,8 @@ __device__ __forceinline__ void act_both(float p, float& f, float& d) {
 // Workgroups go to the 8 XCDs in turn: each XCD gets neighbouring tiles, in
 // groups of kGroup tiles of rows j that pass over the same rows i.
 constexpr int kGroup = 4;
-__device__ __forceinline__ void tile_of(int ni, int nj, int& i, int& j) {
-  const unsigned total = (unsigned)ni * nj, x = blockIdx.x & 7, k = blockIdx.x >> 3;
+__device__ __forceinline__ void tile_of(unsigned block, int ni, int nj, int& i, int& j) {
+  const unsigned total = (unsigned)ni * nj, x = block & 7, k = block >> 3;
   const unsigned per = total >> 3, more = total & 7, id = x * per + min(x, more) + k;
   const unsigned group = id / (kGroup * ni), rest = id - group * kGroup * ni, high = min((unsigned)(nj - group * kGroup), (unsigned)kGroup);
   j = group * kGroup + rest % high;
@@ -70,55 +70,69 @@ __device__ __forceinline__ void store_pieces(bf16* row, int at, int end, const f
   }
 }
 
-// h, or with BACK dp and du, side by side in rows of 2 F at `both`.
+// h, or with BACK dp and du, side by side in rows of 2 F at `both`.  A workgroup
+// takes every gridDim.x-th tile.  Products and gate in one kernel leave p and u in
+// registers: two products by themselves would write and read 8 bytes of each
+// output, 0.5 GB or 107 us at 16384 x 4096.
 template <typename S, bool GELU, bool BACK>
 __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ both) {
   extern __shared__ __align__(1024) char lds[];
   const int ni = (p.F + S::OUT - 1) / S::OUT, per = (p.n + S::BJ - 1) / S::BJ;
-  int ti, tj;
-  tile_of(ni, p.B * per, ti, tj);
-  const int f0 = ti * S::OUT, b = tj / per, t0 = (tj - b * per) * S::BJ;
-  const bf16* x = static_cast<const bf16*>(p.x.p) + (size_t)b * p.x.bs + (size_t)t0 * p.x.ts;
-  f32x4 acc[S::TI][S::TJ] = {};
-  auto weights = [&](int r) {
-    const int wi = r / (16 * S::TI), q = r % (16 * S::TI), c = q % (16 * S::HALF);
-    const bf16* w = static_cast<const bf16*>(q < 16 * S::HALF ? p.wg : p.wu) + (size_t)f0 * p.D;
-    return RowAt{w, (uint32_t)(min(wi * 16 * S::HALF + c, p.F - 1 - f0) * p.D * 2)};
+  const unsigned tiles = (unsigned)ni * p.B * per;
+  struct Spot {
+    int f0, b, t0;
   };
-  tile_products<S>(acc, lds, 0, p.D, weights,
-                   [&](int r) { return RowAt{x, (uint32_t)(min(r, p.n - 1 - t0) * p.x.ts * 2)}; });
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
-  const int f = f0 + wi * 16 * S::HALF + (lane >> 4) * 4 * S::HALF;
+  auto spot = [&](int n) {
+    int ti, tj;
+    tile_of(blockIdx.x + n * gridDim.x, ni, p.B * per, ti, tj);
+    const int b = tj / per;
+    return Spot{ti * S::OUT, b, (tj - b * per) * S::BJ};
+  };
+  auto at = [&](int n, auto take) {
+    const Spot o = spot(n);
+    const bf16* x = static_cast<const bf16*>(p.x.p) + (size_t)o.b * p.x.bs + (size_t)o.t0 * p.x.ts;
+    const size_t w = (size_t)o.f0 * p.D;
+    take(Operand{static_cast<const bf16*>(p.wg) + w, static_cast<const bf16*>(p.wu) + w, p.D, p.F - o.f0},
+         Operand{x, nullptr, p.x.ts, p.n - o.t0}, 0, p.D);
+  };
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto done = [&](int n, f32x4(&acc)[S::TI][S::TJ]) {
+    const int lane = lane_here(), wi = wave % S::WI, wj = wave / S::WI;
+    const Spot at = spot(n);
+    const int f = at.f0 + wi * 16 * S::HALF + (lane >> 4) * 4 * S::HALF;
 #pragma unroll
-  for (int j = 0; j < S::TJ; ++j) {
-    const int t = t0 + (wj * S::TJ + j) * 16 + (lane & 15);
-    if (t >= p.n) continue;
-    const size_t m = (size_t)b * p.n + t;
-    float o[4 * S::HALF], o2[4 * S::HALF];
-    if constexpr (!BACK) {
+    for (int j = 0; j < S::TJ; ++j) {
+      const int t = at.t0 + (wj * S::TJ + j) * 16 + (lane & 15);
+      if (t < p.n) {
+        const size_t m = (size_t)at.b * p.n + t;
+        float o[4 * S::HALF], o2[4 * S::HALF];
+        if constexpr (!BACK) {
 #pragma unroll
-      for (int e = 0; e < 4 * S::HALF; ++e) o[e] = act<GELU>(acc[e / 4][j][e % 4]) * acc[S::HALF + e / 4][j][e % 4];
-      store_pieces(static_cast<bf16*>(p.h) + m * p.F, f, p.F, o);
-    } else {
-      const bf16* dh = static_cast<const bf16*>(p.dh.p) + (size_t)b * p.dh.bs + (size_t)t * p.dh.ts;
+          for (int e = 0; e < 4 * S::HALF; ++e) o[e] = act<GELU>(acc[e / 4][j][e % 4]) * acc[S::HALF + e / 4][j][e % 4];
+          store_pieces(static_cast<bf16*>(p.h) + m * p.F, f, p.F, o);
+        } else {
+          const bf16* dh = static_cast<const bf16*>(p.dh.p) + (size_t)at.b * p.dh.bs + (size_t)t * p.dh.ts;
 #pragma unroll
-      for (int q = 0; q < 4 * S::HALF; q += 8) {
-        Raw<bf16, 8> g;
-        g.zero();
-        if (f + q < p.F) g.load(dh + f + q);
+          for (int q = 0; q < 4 * S::HALF; q += 8) {
+            Raw<bf16, 8> g;
+            g.zero();
+            if (f + q < p.F) g.load(dh + f + q);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float a, d;
-          act_both<GELU>(acc[(q + e) / 4][j][e % 4], a, d);
-          o[q + e] = g.at(e) * acc[S::HALF + (q + e) / 4][j][e % 4] * d;
-          o2[q + e] = g.at(e) * a;
+            for (int e = 0; e < 8; ++e) {
+              float a, d;
+              act_both<GELU>(acc[(q + e) / 4][j][e % 4], a, d);
+              o[q + e] = g.at(e) * acc[S::HALF + (q + e) / 4][j][e % 4] * d;
+              o2[q + e] = g.at(e) * a;
+            }
+          }
+          bf16* to = both + m * 2 * p.F;
+          store_pieces(to, f, p.F, o);
+          store_pieces(to + p.F, f, p.F, o2);
         }
       }
-      bf16* to = both + m * 2 * p.F;
-      store_pieces(to, f, p.F, o);
-      store_pieces(to + p.F, f, p.F, o2);
     }
-  }
+  };
+  tile_products<S, false>(lds, (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x), at, done);
 }
 
 // Up to 16 tokens: the weights' bytes bound it.  A workgroup takes 16 outputs (16
@@ -189,44 +203,34 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product p) {
   extern __shared__ __align__(1024) char lds[];
   const int ni = (p.I + S::BI - 1) / S::BI, nj = (p.J + S::BJ - 1) / S::BJ;
   int ti, tj;
-  tile_of(ni, nj, ti, tj);
-  const int i0 = ti * S::BI, j0 = tj * S::BJ, z = blockIdx.y;
-  f32x4 acc[S::TI][S::TJ] = {};
-  auto over = [&](int span, int k_first, int k_end) {
-    const ByK a{p.a[span] + i0, p.lda, p.I - i0};
-    const bf16* b = p.b[span];
-    if constexpr (S::TRJ) {
-      tile_products<S>(acc, lds, k_first, k_end, a, ByK{b + j0, p.ldb, p.J - j0});
-    } else {
-      b += (size_t)j0 * p.ldb;
-      tile_products<S>(acc, lds, k_first, k_end, a,
-                       [&](int r) { return RowAt{b, (uint32_t)(min(r, p.J - 1 - j0) * p.ldb * 2)}; });
+  tile_of(blockIdx.x, ni, nj, ti, tj);
+  const int i0 = ti * S::BI, j0 = tj * S::BJ, z = blockIdx.y, runs = !S::TRJ && p.cuts == 1 && !p.part ? p.spans : 1;
+  auto at = [&](int n, auto take) {
+    const int span = runs == 2 ? n : z % p.spans, k = z / p.spans * p.per;
+    take(Operand{p.a[span] + i0, nullptr, p.lda, p.I - i0},
+         Operand{p.b[span] + (S::TRJ ? j0 : (size_t)j0 * p.ldb), nullptr, p.ldb, p.J - j0}, k, min(k + p.per, p.K));
+  };
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto done = [&](int n, f32x4(&acc)[S::TI][S::TJ]) {
+    const int lane = lane_here(), wi = wave % S::WI, wj = wave / S::WI;
+    const int i = i0 + wi * 16 * S::TI + (lane >> 4) * 4;
+#pragma unroll
+    for (int j = 0; j < S::TJ; ++j) {
+      const int row = j0 + (wj * S::TJ + j) * 16 + (lane & 15);
+      if (row >= p.J) continue;
+      bf16* c = row < p.split ? p.c + (size_t)row * p.I : p.c2 + (size_t)(row - p.split) * p.I;
+#pragma unroll
+      for (int t = 0; t < S::TI; ++t) {
+        const float o[4] = {acc[t][j][0], acc[t][j][1], acc[t][j][2], acc[t][j][3]};
+        if (i + 16 * t >= p.I) continue;
+        if (p.part)
+          store_vec<float, 4>(p.part + ((size_t)z * p.J + row) * p.I + i + 16 * t, o);
+        else
+          store_vec<bf16, 4>(c + i + 16 * t, o);
+      }
     }
   };
-  if (p.cuts == 1 && !p.part) {
-    over(0, 0, p.K);
-    if (p.spans == 2) over(1, 0, p.K);
-  } else {
-    const int k = z / p.spans * p.per;
-    over(z % p.spans, k, min(k + p.per, p.K));
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave % S::WI, wj = wave / S::WI;
-  const int i = i0 + wi * 16 * S::TI + (lane >> 4) * 4;
-#pragma unroll
-  for (int j = 0; j < S::TJ; ++j) {
-    const int row = j0 + (wj * S::TJ + j) * 16 + (lane & 15);
-    if (row >= p.J) continue;
-    bf16* c = row < p.split ? p.c + (size_t)row * p.I : p.c2 + (size_t)(row - p.split) * p.I;
-#pragma unroll
-    for (int t = 0; t < S::TI; ++t) {
-      const float o[4] = {acc[t][j][0], acc[t][j][1], acc[t][j][2], acc[t][j][3]};
-      if (i + 16 * t >= p.I) continue;
-      if (p.part)
-        store_vec<float, 4>(p.part + ((size_t)z * p.J + row) * p.I + i + 16 * t, o);
-      else
-        store_vec<bf16, 4>(c + i + 16 * t, o);
-    }
-  }
+  tile_products<S, true>(lds, runs, at, done);
 }
 
 // The parts joined in their order: eight values a thread.
@@ -285,14 +289,17 @@ hipError_t tiled(const Glu& p, bf16* both, hipStream_t s) {
   auto kernel = k_glu<S, GELU, BACK>;
   const hipError_t e = allow_lds(kernel, S::LDS);
   if (e != hipSuccess) return e;
-  return HLA_TIMED(BACK ? "glu_gates_back" : "glu", kernel, dim3(tiles_of<S>(p)), dim3(S::THREADS), S::LDS, s, p, both);
+  const unsigned tiles = tiles_of<S>(p), most = 256 * (S::LDS > 81920 ? 1 : 2);
+  return HLA_TIMED(BACK ? "glu_gates_back" : "glu", kernel, dim3(tiles < most ? tiles : most), dim3(S::THREADS), S::LDS, s, p,
+                   both);
 }
 
 // Tiles of 256, 192 and 128 tokens; the last one half as wide, two workgroups a
-// CU.  Taken is what promises the shortest time: rounds of one workgroup a CU
-// times what a round took, and what the first one's start and the last one's end
-// took beside it, in one unit (16384 x 1024 x 4096: 252, 252 and 277 us; 2001 x
-// 2048 x 5464: 92, 81, 89; 512 x 2048 x 8192: 45, 40, 34; 128: 42, 36, 19).
+// CU.  Taken is what promises the shortest time: rounds of one tile a CU times what
+// a round took, and what the first one's start and the last one's end took beside
+// it, in one unit (16384 x 1024 x 4096: 251, 265 and 299 us; 2001 x 2048 x 5464: 96,
+// 85, 95; 2048 x 1024 x 4096: 32, 42, 36; 512 x 2048 x 8192: 46, 41, 34; 128: 42,
+// 36, 18).
 template <bool GELU, bool BACK>
 hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
   const Glu p = joined(given);
