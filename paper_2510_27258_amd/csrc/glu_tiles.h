@@ -18,7 +18,7 @@
 // a lane 4 TI rows in succession, which it stores as whole 16-byte pieces.
 //
 // Measured on 16384 x 1024 x 4096 projections (275 GFLOP, 16 steps a tile): 1.07
-// PFLOP/s, the matrix cores busy 54 % of the time, LDS 21 % without a bank
+// PFLOP/s, the matrix cores busy 57 % of the time, LDS 21 % without a bank
 // conflict; 8192 x 4096 x 4096 1.29 PFLOP/s, where a library's 8192^3 product
 // reaches 1.51.  The loads bound it: with the products taken out they alone are
 // 86 % of an 8192^3 product, 12 TB/s from the XCDs' second-level caches; with the
