@@ -238,11 +238,16 @@ __global__ __launch_bounds__(256) void k_joined(Product p) {
   const size_t all = (size_t)p.J * p.I / 8, e = blockIdx.x * 256ull + threadIdx.x;
   if (e >= all) return;
   float s[8] = {};
-  for (int z = 0; z < p.cuts * p.spans; ++z) {
-    float v[8];
-    load_vec<float, 8>(p.part + ((size_t)z * all + e) * 8, v);
+  const int slabs = p.cuts * p.spans;
+  for (int z0 = 0; z0 < slabs; z0 += 4) {
+    float v[4][8] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] += v[i];
+    for (int z = 0; z < 4; ++z)
+      if (z0 + z < slabs) load_vec<float, 8>(p.part + ((size_t)(z0 + z) * all + e) * 8, v[z]);
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += v[z][i];
   }
   const size_t half = (size_t)p.split * p.I / 8;
   store_vec<bf16, 8>(e < half ? p.c + e * 8 : p.c2 + (e - half) * 8, s);
@@ -320,18 +325,35 @@ hipError_t projections(const Glu& given, bf16* both, hipStream_t s) {
 using DxTile = Tile<8, 4, 2, 4, false, true, false>;
 using DwTile = Tile<8, 4, 2, 4, false, true, true>;
 
-// The parts of the two products: as many as leave no CU without a tile, of 512 k at least.
+// How a product's sums over `spans` spans of K are cut: `cuts` parts of `per` k of
+// each, in slabs of their own that are joined behind, or (slabs = 0) one workgroup
+// a tile for all.  Taken is what promises the shortest time, in us: rounds of one
+// workgroup a CU, at 1.5 a step of 64 k and 6 for its start and end; the join takes
+// 4, 0.3 a slab and their bytes written and read at 6 TB/s.  Measured with parts of
+// 512 k at least, cut over idle CUs alone, and by this rule, the join with it: 22 x
+// 200 from 696 outputs 31.7 and 12.1 us, 1124 x 176 from 720 35.5 and 17.9, 512 x
+// 2048 from 8192 52.2 and 52.1.
 struct Cuts {
-  int cuts, per;
+  int cuts, per, slabs;
 };
 template <typename S>
 Cuts cuts_of(long long I, long long J, int K, int spans) {
-  const long long tiles = ((I + S::BI - 1) / S::BI) * ((J + S::BJ - 1) / S::BJ) * spans;
-  long long cuts = 256 / tiles;
-  if (cuts > K / 512) cuts = K / 512;
-  if (cuts <= 1) return {1, K};
-  const int per = (int)(((K + cuts - 1) / cuts + 63) / 64 * 64);
-  return {(K + per - 1) / per, per};
+  const long long tiles = ((I + S::BI - 1) / S::BI) * ((J + S::BJ - 1) / S::BJ);
+  auto time = [&](long long groups, long long k) {
+    const long long steps = (k + 63) / 64;
+    return (double)((groups + 255) / 256) * (1.5 * (steps > 2 ? steps : 2) + 6);
+  };
+  Cuts best{1, K, 0};
+  double least = time(tiles, (long long)spans * K);
+  for (int c = spans > 1 ? 1 : 2; c <= 64 && (c == 1 || K / c >= 128); ++c) {
+    const int per = (int)((((long long)K + c - 1) / c + 63) / 64 * 64), cuts = (int)(((long long)K + per - 1) / per);
+    const double t = time(tiles * spans * cuts, per) + 4 + cuts * spans * (0.3 + (double)I * (double)J * 8 / 6e6);
+    if (t < least) {
+      least = t;
+      best = {cuts, per, cuts * spans};
+    }
+  }
+  return best;
 }
 
 template <typename S>
@@ -339,11 +361,11 @@ hipError_t product(Product p, float* part, const char* name, hipStream_t s) {
   const Cuts c = cuts_of<S>(p.I, p.J, p.K, p.spans);
   p.cuts = c.cuts;
   p.per = c.per;
-  p.part = c.cuts > 1 ? part : nullptr;
+  p.part = c.slabs ? part : nullptr;
   const unsigned tiles = (unsigned)((p.I + S::BI - 1) / S::BI) * (unsigned)((p.J + S::BJ - 1) / S::BJ);
   hipError_t e = allow_lds(k_product<S>, S::LDS);
   if (e != hipSuccess) return e;
-  e = HLA_TIMED(name, k_product<S>, dim3(tiles, p.part ? p.cuts * p.spans : 1), dim3(S::THREADS), S::LDS, s, p);
+  e = HLA_TIMED(name, k_product<S>, dim3(tiles, c.slabs ? c.slabs : 1), dim3(S::THREADS), S::LDS, s, p);
   if (e != hipSuccess || !p.part) return e;
   return HLA_TIMED("glu_joined", k_joined, dim3((unsigned)(((size_t)p.I * p.J / 8 + 255) / 256)), dim3(256), 0, s, p);
 }
@@ -355,7 +377,7 @@ Space space(int B, int n, int D, int F) {
   Space a;
   const size_t M = (size_t)B * n;
   const Cuts dx = cuts_of<DxTile>(D, M, F, 2), dw = cuts_of<DwTile>(D, 2LL * F, (int)M, 1);
-  const size_t px = dx.cuts > 1 ? M * D * 4 * dx.cuts * 2 : 0, pw = dw.cuts > 1 ? (size_t)2 * F * D * 4 * dw.cuts : 0;
+  const size_t px = M * D * 4 * dx.slabs, pw = (size_t)2 * F * D * 4 * dw.slabs;
   a.both = 0;
   a.x = a.both + M * 2 * F * 2;
   a.part = a.x + (B > 1 && n > 1 ? M * D * 2 : 0);
