@@ -196,6 +196,20 @@ __device__ __forceinline__ void join_wave(const float (&A)[V], const float (&M)[
   }
 }
 
+// v after the maps of segments [from, to), or backwards from the last one on: eight at a time are loaded together.
+template <bool BACK>
+__device__ __forceinline__ float joined(const float2* __restrict__ sums, size_t apart, int from, int to, float v) {
+  for (int s = 0; s < to - from; s += 8) {
+    float2 m[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      m[k] = s + k < to - from ? sums[(size_t)(BACK ? to - 1 - s - k : from + s + k) * apart] : make_float2(1.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v = fmaf(m[k].x, v, m[k].y);
+  }
+  return v;
+}
+
 // [p, p + bytes) from a uniform address on, the bytes cut at 2^31 - 1: no offset here is larger.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t view_of(const void* from, long long bytes) {
   const uint64_t p = reinterpret_cast<uint64_t>(from);
@@ -255,10 +269,7 @@ __global__ __launch_bounds__(64 * W) void k_glr(Glr p, Cut cut, float2* __restri
       if (at.seg == 0 && wave == 0 && row == 0 && mine) first[s0] = p.state ? p.state[s0] : 0.f;
     } else {
       carry[v] = cut.segs > 1 ? first[s0] : p.state ? p.state[s0] : 0.f;
-      for (int s = 0; s < at.seg; ++s) {
-        const float2 m = sums[(size_t)s * p.B * p.D + s0];
-        carry[v] = fmaf(m.x, carry[v], m.y);
-      }
+      carry[v] = joined<false>(sums + s0, (size_t)p.B * p.D, 0, at.seg, carry[v]);
     }
   }
 
@@ -391,10 +402,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_glr_back(Glr p, Cut cut, float2* 
     carry[v] = 0.f;
     sum[0][v] = sum[1][v] = sum[2][v] = 0.;
     if constexpr (!ENDS) {
-      for (int s = cut.segs - 1; s > at.seg; --s) {
-        const float2 m = sums[((size_t)s * p.B + at.b) * p.D + c + v];
-        carry[v] = fmaf(m.x, carry[v], m.y);
-      }
+      carry[v] = joined<true>(sums + (size_t)at.b * p.D + c + v, (size_t)p.B * p.D, at.seg + 1, cut.segs, 0.f);
     }
   }
   const int kept = (p.n + kGlrTile - 1) / kGlrTile;
@@ -630,7 +638,7 @@ bool pairs(const Glr& p) {
 // Runs and waves of the two walks, and how many workgroups they ask for before
 // sequences are cut.  Measured: the backward walk of 4 x 4096 x 2048 with runs of
 // 4 in 8 waves 127 us, of 8 in 4 waves 142, of 8 in 8 waves 215 (registers).
-constexpr int kFwdS = 16, kFwdW = 8, kFwdWant = 128, kBackS = 4, kBackW = 8, kBackWant = 256, kBackLpr = 16;
+constexpr int kFwdS = 16, kFwdW = 8, kBackS = 4, kBackW = 8, kBackWant = 256, kBackLpr = 16;
 constexpr int kMostSegs = 32;
 
 template <int V, int LPR, int S, int W>
@@ -645,22 +653,43 @@ Cut cut_of(int B, int n, int D, int want) {
   return {blocks, (int)((tiles + per - 1) / per), (int)per};
 }
 
-// f(lanes a row) of the forward.  Wide rows use whole memory lines: 64 bytes of
-// bf16 at 16 lanes, where that gives every CU a workgroup; 128 bytes, where even
-// these fill the CUs twice, or where long sequences are cut all the same; half a
-// line where neither, but 32 bytes do.  Measured, us, at 8, 16 and 32 lanes (8 and
-// 16 uncut where they fill the CUs): 4 x 4096 x 2048 92, 71, 88; 8 x 4096 x 4096
-// 347, 282, 253; 1 x 8000 x 4096 95, 128, 100; 1 x 16384 x 1024 92, 70, 59.
-template <int V, typename F>
-auto by_lanes(int B, int n, int D, F f) {
-  auto blocks = [&](int lanes) { return (long long)B * ((D + V * lanes - 1) / (V * lanes)); };
-  if (blocks(32) >= 512 || (n >= 4096 && blocks(8) < 256)) return f(std::integral_constant<int, 32>{});
-  if (n >= 4096 && blocks(16) < 256) return f(std::integral_constant<int, 8>{});
-  return f(std::integral_constant<int, 16>{});
-}
+// The forward's lanes a row, 32, 16 or 8 (128, 64 or 32 bytes of bf16), and its cut:
+// what promises the shortest time, in us.  A workgroup's tile of 16384 values takes
+// 5 on an empty chip, and 8, 9 or 12 where every CU has one; a launch takes 4.
+// Measured at 32, 16 and 8 lanes (cut where that fills CUs): 4 x 4096 x 2048 88, 71,
+// 92; 8 x 4096 x 4096 253, 282, 347; 1 x 8000 x 4096 100, 128, 95; 1 x 16384 x 1024
+// 59, 70, 92; 2 x 12000 x 3000 264, 159, 245; 1 x 2500 x 512 27, 38, 20; 4 x 2500 x
+// 512 30, 41, 26.
+struct Plan {
+  int lanes;
+  Cut cut;
+};
 template <int V>
-Cut forward_cut(int B, int n, int D) {
-  return by_lanes<V>(B, n, D, [&](auto l) { return cut_of<V, decltype(l)::value, kFwdS, kFwdW>(B, n, D, kFwdWant); });
+Plan forward_plan(int B, int n, int D) {
+  Plan best{};
+  float least = 0.f;
+  auto consider = [&](int lanes, float full) {
+    const int cb = V * lanes, blocks = (D + cb - 1) / cb, tile = kFwdS * (64 / lanes) * kFwdW;
+    const int tiles = (int)(((long long)n + tile - 1) / tile);
+    const long long have = (long long)blocks * B;
+    auto walk = [&](long long groups, int per) {
+      const float load = groups < 256 ? groups / 256.f : 1.f;
+      return 4.f + (float)((groups + 255) / 256) * per * (5.f + (full - 5.f) * load);
+    };
+    const int fill = have < 256 ? (int)((256 + have - 1) / have) : 1;
+    for (int want : {1, fill, 2 * fill, fill / 2, tiles}) {
+      if (want < 1 || want > kMostSegs || want > tiles || (want > 1 && have >= 256)) continue;
+      const int per = (tiles + want - 1) / want, segs = (tiles + per - 1) / per;
+      const float t = walk(have * segs, per) + (segs > 1 ? walk(have * (segs - 1), per) : 0.f);
+      if (best.lanes && t >= least) continue;
+      least = t;
+      best = {lanes, {blocks, segs, per}};
+    }
+  };
+  consider(16, 9.f);
+  consider(32, 8.f);
+  consider(8, 12.f);
+  return best;
 }
 template <int V>
 Cut backward_cut(int B, int n, int D) {
@@ -669,11 +698,12 @@ Cut backward_cut(int B, int n, int D) {
 
 template <typename T, int V>
 hipError_t forward(const Glr& p, void* ws, hipStream_t s) {
-  const Cut cut = forward_cut<V>(p.B, p.n, p.D);
+  const Plan plan = forward_plan<V>(p.B, p.n, p.D);
+  const Cut cut = plan.cut;
   float* first = static_cast<float*>(ws);
   float2* sums = reinterpret_cast<float2*>(first + (((size_t)p.B * p.D + 3) & ~(size_t)3));
   const unsigned one = (unsigned)cut.blocks * p.B;
-  return by_lanes<V>(p.B, p.n, p.D, [&](auto l) {
+  auto run = [&](auto l) {
     constexpr int LPR = decltype(l)::value;
     if (cut.segs > 1) {
       const hipError_t e = HLA_TIMED("glr_ends", (k_glr<T, V, LPR, kFwdS, kFwdW, true>), dim3(one * (cut.segs - 1)),
@@ -682,7 +712,10 @@ hipError_t forward(const Glr& p, void* ws, hipStream_t s) {
     }
     return HLA_TIMED("glr", (k_glr<T, V, LPR, kFwdS, kFwdW, false>), dim3(one * cut.segs), dim3(64 * kFwdW), 0, s, p, cut,
                      sums, first);
-  });
+  };
+  return plan.lanes == 32   ? run(std::integral_constant<int, 32>{})
+         : plan.lanes == 16 ? run(std::integral_constant<int, 16>{})
+                            : run(std::integral_constant<int, 8>{});
 }
 
 template <typename T, int V>
@@ -706,7 +739,7 @@ hipError_t backward(const Glr& p, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t glr_forward_ws(int B, int n, int D) {
-  const int a = forward_cut<1>(B, n, D).segs, b = forward_cut<2>(B, n, D).segs;
+  const int a = forward_plan<1>(B, n, D).cut.segs, b = forward_plan<2>(B, n, D).cut.segs;
   return sizeof(float) * (size_t)B * D * (2 * (a > b ? a : b) + 1) + 64;
 }
 size_t glr_backward_ws(int B, int n, int D) {
@@ -714,7 +747,7 @@ size_t glr_backward_ws(int B, int n, int D) {
   return sizeof(float) * (size_t)B * D * 5 * (a > b ? a : b) + 64;
 }
 double glr_threads(int B, int n, int D) {   // of the largest launch: single channels
-  const Cut f = forward_cut<1>(B, n, D), b = backward_cut<1>(B, n, D);
+  const Cut f = forward_plan<1>(B, n, D).cut, b = backward_cut<1>(B, n, D);
   return std::fmax((double)f.blocks * f.segs * kFwdW, (double)b.blocks * b.segs * kBackW) * 64. * B;
 }
 
