@@ -635,31 +635,37 @@ bool pairs(const Glr& p) {
   return ok;
 }
 
-// Runs and waves of the two walks, and how many workgroups they ask for before
-// sequences are cut.  Measured: the backward walk of 4 x 4096 x 2048 with runs of
+// Runs and waves of the two walks, and segments at most.  Measured: the backward walk of 4 x 4096 x 2048 with runs of
 // 4 in 8 waves 127 us, of 8 in 4 waves 142, of 8 in 8 waves 215 (registers).
-constexpr int kFwdS = 16, kFwdW = 8, kBackS = 4, kBackW = 8, kBackWant = 256, kBackLpr = 16;
+constexpr int kFwdS = 16, kFwdW = 8, kBackS = 4, kBackW = 8, kBackLpr = 16;
 constexpr int kMostSegs = 32;
 
-template <int V, int LPR, int S, int W>
-Cut cut_of(int B, int n, int D, int want) {
-  constexpr int CB = V * LPR, TILE = S * (64 / LPR) * W;
-  const int blocks = (D + CB - 1) / CB;
-  const long long tiles = ((long long)n + TILE - 1) / TILE, have = (long long)blocks * B;
-  long long segs = have >= want ? 1 : (2 * want + have - 1) / have;
-  if (segs > kMostSegs) segs = kMostSegs;
-  if (segs > tiles / 2) segs = tiles / 2 > 1 ? tiles / 2 : 1;
-  const long long per = (tiles + segs - 1) / segs;
-  return {blocks, (int)((tiles + per - 1) / per), (int)per};
+// One launch of `groups` workgroups of `per` tiles each, in us: in rounds of one
+// workgroup a CU, a tile `empty` on an empty chip and `full` where every CU has one;
+// a launch takes 2 and a round's start 2.
+float launch_time(long long groups, int per, float empty, float full) {
+  const float load = groups < 256 ? groups / 256.f : 1.f;
+  return 2.f + (float)((groups + 255) / 256) * (2.f + per * (empty + (full - empty) * load));
+}
+// f(segments' count, tiles each) of uncut sequences, and of those cut so as to fill the CUs, or half or twice of that.
+template <typename F>
+void each_cut(long long have, int tiles, F f) {
+  f(1, tiles);
+  if (have >= 256) return;
+  const int fill = (int)(256 / have), more = (int)((255 + have) / have);
+  for (int want : {fill, more, 2 * more, more / 2, tiles}) {
+    if (want < 2 || want > kMostSegs || want > tiles) continue;
+    const int per = (tiles + want - 1) / want;
+    f((tiles + per - 1) / per, per);
+  }
 }
 
 // The forward's lanes a row, 32, 16 or 8 (128, 64 or 32 bytes of bf16), and its cut:
-// what promises the shortest time, in us.  A workgroup's tile of 16384 values takes
-// 5 on an empty chip, and 8, 9 or 12 where every CU has one; a launch takes 4.
+// what promises the shortest time: a tile is 16384 values.
 // Measured at 32, 16 and 8 lanes (cut where that fills CUs): 4 x 4096 x 2048 88, 71,
 // 92; 8 x 4096 x 4096 253, 282, 347; 1 x 8000 x 4096 100, 128, 95; 1 x 16384 x 1024
-// 59, 70, 92; 2 x 12000 x 3000 264, 159, 245; 1 x 2500 x 512 27, 38, 20; 4 x 2500 x
-// 512 30, 41, 26.
+// 59, 70, 92; 2 x 12000 x 3000 264, 159, 245; 1 x 2500 x 512 27, 38, 20 (by
+// this rule 18); 4 x 2500 x 512 30, 41, 26.
 struct Plan {
   int lanes;
   Cut cut;
@@ -672,28 +678,37 @@ Plan forward_plan(int B, int n, int D) {
     const int cb = V * lanes, blocks = (D + cb - 1) / cb, tile = kFwdS * (64 / lanes) * kFwdW;
     const int tiles = (int)(((long long)n + tile - 1) / tile);
     const long long have = (long long)blocks * B;
-    auto walk = [&](long long groups, int per) {
-      const float load = groups < 256 ? groups / 256.f : 1.f;
-      return 4.f + (float)((groups + 255) / 256) * per * (5.f + (full - 5.f) * load);
-    };
-    const int fill = have < 256 ? (int)((256 + have - 1) / have) : 1;
-    for (int want : {1, fill, 2 * fill, fill / 2, tiles}) {
-      if (want < 1 || want > kMostSegs || want > tiles || (want > 1 && have >= 256)) continue;
-      const int per = (tiles + want - 1) / want, segs = (tiles + per - 1) / per;
-      const float t = walk(have * segs, per) + (segs > 1 ? walk(have * (segs - 1), per) : 0.f);
-      if (best.lanes && t >= least) continue;
+    each_cut(have, tiles, [&](int segs, int per) {
+      const float t = launch_time(have * segs, per, 5.f, full) +
+                      (segs > 1 ? launch_time(have * (segs - 1), per, 5.f, full) : 0.f);
+      if (best.lanes && t >= least) return;
       least = t;
       best = {lanes, {blocks, segs, per}};
-    }
+    });
   };
   consider(16, 9.f);
   consider(32, 8.f);
   consider(8, 12.f);
   return best;
 }
+// The gradients' cut: a tile of 128 tokens takes 2.7 to 4, of the ends alone 0.9 to
+// 1.3.  Uncut, and cut into 4, 8 and 32: 4 x 12000 x 512 301, 131, 131 and 173; 1 x
+// 12000 x 1000 266, -, 67 and 91; 2 x 12000 x 3000 316 uncut, 431 in two.
 template <int V>
 Cut backward_cut(int B, int n, int D) {
-  return cut_of<V, kBackLpr, kBackS, kBackW>(B, n, D, kBackWant);
+  constexpr int CB = V * kBackLpr, TILE = kBackS * (64 / kBackLpr) * kBackW;
+  const int blocks = (D + CB - 1) / CB, tiles = (int)(((long long)n + TILE - 1) / TILE);
+  const long long have = (long long)blocks * B;
+  Cut best{};
+  float least = 0.f;
+  each_cut(have, tiles, [&](int segs, int per) {
+    const float t = launch_time(have * segs, per, 2.7f, 4.f) +
+                    (segs > 1 ? launch_time(have * segs, per, 0.9f, 1.3f) : 0.f);
+    if (best.segs && t >= least) return;
+    least = t;
+    best = {blocks, segs, per};
+  });
+  return best;
 }
 
 template <typename T, int V>
