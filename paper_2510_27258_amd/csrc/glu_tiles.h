@@ -37,7 +37,8 @@ namespace hla {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// This wave's loads but the last N have arrived, its operand reads have too, and every wave is here.
+// This wave's loads but the last N have arrived (memory operations count in their
+// order, so a caller has no others, spilled registers' either, behind those N), its operand reads have too, and every wave is here.
 template <int N>
 __device__ __forceinline__ void wait_loads_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");

@@ -1,6 +1,8 @@
 """The kernels of a block's operators keep what they hold in registers: none
 spills, but for the gradients of the norms over rows beyond 8192 elements (and
-of bf16 rows beyond 4096, a few).  The counts come from the metadata of the
+of bf16 rows beyond 4096, a few).  In the projections a spill would be wrong,
+not slow alone: their waits count the loads between them, and a spilled
+register's store would be one more.  The counts come from the metadata of the
 code objects in libhla.so.  CPU only.
 """
 import os
