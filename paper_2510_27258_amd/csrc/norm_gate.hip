@@ -182,8 +182,17 @@ __global__ __launch_bounds__(kSumRows * kSumCols) void k_column_sums(ColumnSums 
   if (!to) return;
   const float* part = c.part + (size_t)blockIdx.y * c.rows * c.cols;
   float s = 0.f;
-  if (col < c.cols)
-    for (int r = rg; r < c.rows; r += kSumRows) s += part[(size_t)r * c.cols + col];
+  if (col < c.cols) {
+    constexpr int kAtOnce = 8;      // loads on their way together
+    for (int r0 = rg; r0 < c.rows; r0 += kSumRows * kAtOnce) {
+      float v[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        v[k] = r0 + k * kSumRows < c.rows ? part[(size_t)(r0 + k * kSumRows) * c.cols + col] : 0.f;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) s += v[k];
+    }
+  }
   red[rg][cl] = s;
   __syncthreads();
   if (rg != 0 || col >= c.cols) return;
