@@ -82,7 +82,9 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm(GatedNorm a) {
 // weight's partial sums: [grid.x][G][d] with a weight for each group, else
 // [grid.x grid.y][d], the block's rows summed in a fixed order.
 template <typename TY, typename T, typename S, bool WHOLE>
-__global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, float* __restrict__ part) {
+__global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, float* __restrict__ part,
+                                                               float* __restrict__ stats) {
+  constexpr bool kSums = !sums_apart<S>();
   __shared__ float red[2][2][1][S::WAVES];
   constexpr bool kExact = sizeof(TY) == 4;
   const Place<S> p(a.G);
@@ -121,7 +123,10 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
       v[e] *= r;                                   // hat from here on
       const float g = a.z.p && a.norm_first ? go.at(e) * (z.at(e) * sig[e]) : go.at(e);
       dot[0] += g * w[e] * v[e];
-      dw[e] += g * v[e];
+      if constexpr (kSums) dw[e] += g * v[e];
+    }
+    if constexpr (!kSums) {
+      if (p.lane == 0 && there) stats[(size_t)tok * a.G + p.g] = r;
     }
     row_sums<S, 1>(dot, red[turn][1]);
     const float mean = dot[0] / a.d;
@@ -137,7 +142,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
     store_row<TY, S, WHOLE>(static_cast<TY*>(const_cast<void*>(a.dy.p)) + (there ? at(a.dy, b, t, p.g) : 0), d, p.lane, dy);
     if (a.z.p) store_row<T, S, WHOLE>(static_cast<T*>(a.dz) + here, d, p.lane, dz);
   }
-  if (!a.dw) return;
+  if (!kSums || !a.dw) return;
   if constexpr (S::ROWS == 1) {
     float* to = part + (a.per_group ? (size_t)blockIdx.x * a.G + p.g : (size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.d;
 #pragma unroll
@@ -172,6 +177,40 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
       }
     }
   }
+}
+
+// The weight's sums of wide rows, from each one's 1 / rms(v): with a weight for each
+// group [kShares][G][d], blockIdx.z the group, else [kShares][d].
+template <typename TY, typename T, bool WHOLE>
+__global__ __launch_bounds__(256) void k_gated_norm_sums(GatedNorm a, float* __restrict__ part,
+                                                         const float* __restrict__ stats) {
+  using S = Columns;
+  constexpr bool kExact = sizeof(TY) == 4;
+  const int lane = blockIdx.x * 256 + threadIdx.x;
+  const unsigned toks = (unsigned)a.B * a.n, groups = a.per_group ? 1 : a.G;
+  float dw[S::E];
+#pragma unroll
+  for (int e = 0; e < S::E; ++e) dw[e] = 0.f;
+#pragma unroll 2
+  for (unsigned long long row = blockIdx.y; row < (unsigned long long)toks * groups; row += kShares) {
+    const unsigned tok = (unsigned)(row / groups), b = tok / a.n, t = tok - b * a.n;
+    const int g = a.per_group ? blockIdx.z : (int)(row - (unsigned long long)tok * groups);
+    const size_t at_row = (size_t)tok * a.G + g;
+    const float r = stats[at_row];
+    RowRaw<TY, S, WHOLE> y;
+    RowRaw<T, S, WHOLE> z, go;
+    y.load(static_cast<const TY*>(a.y.p) + at(a.y, b, t, g), a.d, lane);
+    go.load(static_cast<const T*>(a.dout) + at_row * a.d, a.d, lane);
+    if (a.z.p) z.load(static_cast<const T*>(a.z.p) + at(a.z, b, t, g), a.d, lane);
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float gate = a.z.p ? z.at(e) * sigmoid<kExact>(z.at(e)) : 1.f;
+      dw[e] += go.at(e) * gate * (y.at(e) * r);      // the gate belongs to the one or the other
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < S::E; ++e)
+    if (lane * 8 + e < a.d) part[((size_t)blockIdx.y * gridDim.z + blockIdx.z) * a.d + lane * 8 + e] = dw[e];
 }
 
 constexpr int kSumRows = 64, kSumCols = 16;
@@ -238,9 +277,15 @@ hipError_t backward(const GatedNorm& a, float* part, hipStream_t s) {
   Grid g{};
   const hipError_t e = by_row<true>(a.d, [&](auto shape) {
     using S = decltype(shape);
-    g = grid_of<S>(a.B, a.n, a.G, back_blocks<S>());
-    return HLA_TIMED("gated_norm_back", (k_gated_norm_back<TY, T, S, WHOLE>), dim3(g.x, g.y), dim3(S::THREADS), 0, s, a,
-                     part);
+    float* stats = part;
+    g = grid_of<S>(a.B, a.n, a.G, sums_apart<S>() ? kBlocks : back_blocks<S>());
+    const hipError_t e = HLA_TIMED("gated_norm_back", (k_gated_norm_back<TY, T, S, WHOLE>), dim3(g.x, g.y), dim3(S::THREADS),
+                                   0, s, a, part, stats);
+    if (e != hipSuccess || !sums_apart<S>() || !a.dw) return e;
+    part += ((size_t)a.B * a.n * a.G + 3) & ~(size_t)3;
+    g = {kShares, 1};
+    return HLA_TIMED("gated_norm_sums", (k_gated_norm_sums<TY, T, WHOLE>),
+                     dim3((a.d + 2047) / 2048, kShares, a.per_group ? a.G : 1), dim3(256), 0, s, a, part, stats);
   });
   if (e != hipSuccess || !a.dw) return e;
   ColumnSums c{part, {a.dw, nullptr, nullptr}, a.per_group ? g.x : g.x * g.y, a.per_group ? a.G * a.d : a.d, a.w_dtype};
@@ -271,6 +316,8 @@ hipError_t launch_gated_norm(const GatedNorm& a, hipStream_t s) { return by_type
 size_t gated_norm_backward_ws(int B, int n, int G, int d, int per_group) {
   return by_row<true>(d, [&](auto shape) {
     using S = decltype(shape);
+    if (sums_apart<S>())
+      return sizeof(float) * ((((size_t)B * n * G + 3) & ~(size_t)3) + (size_t)kShares * (per_group ? G : 1) * d);
     const Grid g = grid_of<S>(B, n, G, back_blocks<S>());
     return sizeof(float) * g.x * (size_t)(per_group ? G : g.y) * d;
   });

@@ -78,7 +78,9 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm(ResidualNorm a) {
 // times: where a thread has one piece of each, the next rows are loaded meanwhile
 // (8192 rows of 4096 in bf16 92 us, 118 without; of 2048 53 and 58).
 template <typename TX, typename T, typename S, bool WHOLE>
-__global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm a, float* __restrict__ part) {
+__global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm a, float* __restrict__ part,
+                                                                  float4* __restrict__ stats) {
+  constexpr bool kSums = !sums_apart<S>();
   __shared__ float red[2][4][S::WAVES];
   const int lane = threadIdx.x % S::LANES;
   const unsigned rows = (unsigned)a.B * a.n;
@@ -135,14 +137,19 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
     for (int e = 0; e < S::E; ++e) {
       const float hat = r[e] * rr;
       dr[e] = gr.at(e) + rr * (go.at(e) * w[e] - hat * mean);
-      dw[e] += go.at(e) * hat;
       const float yhat = y.at(e) * ry, u = a.post ? yhat * post[e] : y.at(e);
-      dscale[e] += a.alpha * u * dr[e];
+      if constexpr (kSums) {
+        dw[e] += go.at(e) * hat;
+        dscale[e] += a.alpha * u * dr[e];
+      }
       if (a.post) {
         const float du = a.alpha * step[e] * dr[e];
-        dpost[e] += du * yhat;
+        if constexpr (kSums) dpost[e] += du * yhat;
         dot[0] += du * post[e] * yhat;
       }
+    }
+    if constexpr (!kSums) {
+      if (lane == 0 && row < rows) stats[row] = make_float4(ry, rr, mean, 0.f);
     }
     store_row<TX, S, WHOLE>(static_cast<TX*>(a.dx) + here, d, lane, dr);
     if (a.post) row_sums<S, 1>(dot, red[turn] + 3);
@@ -154,6 +161,7 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
     }
     store_row<T, S, WHOLE>(static_cast<T*>(a.dy) + here, d, lane, r);
   }
+  if constexpr (!kSums) return;
   __shared__ float sums[S::ROWS > 1 ? S::ROWS : 1][S::ROWS > 1 ? S::LANES * S::E + 1 : 1];
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
@@ -179,6 +187,52 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
         to[c] = s;
       }
     }
+  }
+}
+
+// The weights' sums of wide rows, from the statistics 1 / rms(y), 1 / rms(r) and
+// mean(g w hat_r) of each: [3][kShares][D].
+template <typename TX, typename T, bool WHOLE>
+__global__ __launch_bounds__(256) void k_residual_norm_sums(ResidualNorm a, float* __restrict__ part,
+                                                            const float4* __restrict__ stats) {
+  using S = Columns;
+  const int lane = blockIdx.x * 256 + threadIdx.x;
+  const unsigned rows = (unsigned)a.B * a.n;
+  float w[S::E], step[S::E], post[S::E], dw[S::E], dscale[S::E], dpost[S::E];
+  load_weight<S, WHOLE>(a.w, a.w_dtype, 0, a.D, lane, w);
+  load_weight<S, WHOLE>(a.scale, a.w_dtype, 0, a.D, lane, step);
+  load_weight<S, WHOLE>(a.post, a.w_dtype, 0, a.D, lane, post);
+#pragma unroll
+  for (int e = 0; e < S::E; ++e) dw[e] = dscale[e] = dpost[e] = 0.f;
+#pragma unroll 2
+  for (unsigned row = blockIdx.y; row < rows; row += kShares) {
+    const float4 st = stats[row];
+    const size_t here = (size_t)row * a.D;
+    RowRaw<TX, S, WHOLE> x, gr;
+    RowRaw<T, S, WHOLE> y, go;
+    x.load(static_cast<const TX*>(a.x.p) + at(a.x, a, row), a.D, lane);
+    y.load(static_cast<const T*>(a.y.p) + at(a.y, a, row), a.D, lane);
+    go.load(static_cast<const T*>(a.dout) + here, a.dout ? a.D : 0, lane);
+    gr.load(static_cast<const TX*>(a.dr) + here, a.dr ? a.D : 0, lane);
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) {
+      const float yhat = y.at(e) * st.x, u = a.post ? yhat * post[e] : y.at(e);
+      const float hat = (x.at(e) + a.alpha * step[e] * u) * st.y;
+      const float dr = gr.at(e) + st.y * (go.at(e) * w[e] - hat * st.z);
+      dw[e] += go.at(e) * hat;
+      dscale[e] += a.alpha * u * dr;
+      dpost[e] += a.alpha * step[e] * dr * yhat;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < S::E; ++e) {
+    const int c = lane * 8 + e;
+    if (c >= a.D) continue;
+    float* to = part + (size_t)blockIdx.y * a.D + c;
+    const size_t apart = (size_t)kShares * a.D;
+    to[0] = dw[e];
+    to[apart] = dpost[e];
+    to[2 * apart] = dscale[e];
   }
 }
 
@@ -215,9 +269,15 @@ hipError_t backward(const ResidualNorm& a, float* part, hipStream_t s) {
   int blocks = 0;
   const hipError_t e = by_row<true>(a.D, [&](auto shape) {
     using S = decltype(shape);
-    blocks = blocks_of<S>(a.B, a.n, back_blocks<S>());
-    return HLA_TIMED("residual_norm_back", (k_residual_norm_back<TX, T, S, WHOLE>), dim3(blocks), dim3(S::THREADS), 0, s, a,
-                     part);
+    float4* stats = reinterpret_cast<float4*>(part);
+    blocks = blocks_of<S>(a.B, a.n, sums_apart<S>() ? kBlocks : back_blocks<S>());
+    const hipError_t e = HLA_TIMED("residual_norm_back", (k_residual_norm_back<TX, T, S, WHOLE>), dim3(blocks),
+                                   dim3(S::THREADS), 0, s, a, part, stats);
+    if (e != hipSuccess || !sums_apart<S>() || !(a.dw || a.dpost || a.dscale)) return e;
+    part += 4 * (size_t)a.B * a.n;
+    blocks = kShares;
+    return HLA_TIMED("residual_norm_sums", (k_residual_norm_sums<TX, T, WHOLE>), dim3((a.D + 2047) / 2048, kShares),
+                     dim3(256), 0, s, a, part, stats);
   });
   if (e != hipSuccess || !(a.dw || a.dpost || a.dscale)) return e;
   return launch_column_sums({part, {a.dw, a.dpost, a.dscale}, blocks, a.D, a.w_dtype}, s);
@@ -242,6 +302,7 @@ hipError_t launch_residual_norm(const ResidualNorm& a, hipStream_t s) { return b
 size_t residual_norm_backward_ws(int B, int n, int D) {
   return by_row<true>(D, [&](auto shape) {
     using S = decltype(shape);
+    if (sums_apart<S>()) return sizeof(float) * (4 * (size_t)B * n + 3 * (size_t)kShares * D);
     return sizeof(float) * 3 * (size_t)blocks_of<S>(B, n, back_blocks<S>()) * D;
   });
 }

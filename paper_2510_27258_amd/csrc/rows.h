@@ -184,7 +184,7 @@ auto by_row(int d, F f) {
   if constexpr (BACK) {
     if (d <= 4096) return f(RowShape<1, 512>{});
     if (d <= 8192) return f(RowShape<2, 512>{});
-    return f(RowShape<4, 512>{});     // holds more than its registers: slow
+    return f(RowShape<2, 1024>{});    // without the weights' sums
   } else {
     if (d <= 4096) return f(RowShape<2, 256>{});
     if (d <= 8192) return f(RowShape<2, 512>{});
@@ -197,5 +197,17 @@ template <typename S>
 constexpr int back_blocks() {
   return S::THREADS <= 256 ? 1024 : 512;
 }
+
+// Rows beyond 8192 leave their gradients' kernel no registers for the weights'
+// sums, which a second kernel then forms from the inputs and each row's statistics:
+// a thread keeps eight columns and takes every kShares-th row.  (Sums in the rows'
+// kernel too, 2048 rows of 16384 in bf16: residual norm 493 us and 34 for their join,
+// now 122, 63 and 12.  Gated norm 227 and 12, now 154, 56 and 6.)
+template <typename S>
+constexpr bool sums_apart() {
+  return S::THREADS > 512;
+}
+constexpr int kShares = 64;
+using Columns = RowShape<1, 256>;
 
 }  // namespace hla

@@ -100,6 +100,14 @@ def test_gated_norm(size, types, first):
         _gn_check(y, z, w, 1e-3, first, g, out, grads, form)
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("size", [(1, 70, 2, 8208), (2, 67, 1, 9001)])
+def test_gated_norm_of_many_wide_rows(size, types):
+    """More rows than the shares of the weight's sums, which a kernel of their own forms."""
+    test_gated_norm(size, types, False)
+    test_gated_norm(size, types, True)
+
+
 # ----------------------------------------------------------------------------
 RN_SIZES = [(1, 1, 8), (2, 3, 64), (1, 70, 333), (3, 5, 1024), (2, 2, 1001), (1, 9, 2048), (1, 3, 4096), (1, 2, 8192),
             (2, 2, 7777), (1, 2, 16384), (1, 3, 1)]
@@ -154,6 +162,12 @@ def test_residual_norm(size, types):
         assert (outs[0].dtype, outs[1].dtype) == (types[1], types[0])
         grads = hla.residual_norm_backward(x, y, w, post, scale, go, gr, alpha, 1e-3)
         _rn_check(x, y, w, post, scale, alpha, 1e-3, go, gr, outs, grads, form)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("size", [(1, 150, 8208), (2, 70, 9001)])
+def test_residual_norm_of_many_wide_rows(size, types):
+    test_residual_norm(size, types)
 
 
 # ----------------------------------------------------------------------------
