@@ -10,8 +10,9 @@
 //
 // Bound by memory: every input is read once and every output written once: 16384
 // tokens of 16 heads of 64, fp32 beside bf16 gates, 35 us, 3.8 TB/s where heads lie
-// apart, their gradients 47 us, 5.0 TB/s.  A thread keeps its group and its elements of a row while its block goes over
-// the tokens, so the weight is loaded once and its gradient summed in registers.
+// apart, their gradients 47 us, 5.0 TB/s.  A thread keeps its group and its elements
+// of a row while its block goes over the tokens, so the weight is loaded once and
+// its gradient summed in registers.
 #include "block.h"
 #include "rows.h"
 
