@@ -100,7 +100,8 @@ __global__ __launch_bounds__(S::THREADS) void k_glu(Glu p, bf16* __restrict__ bo
     const int lane = lane_here(), wi = wave % S::WI, wj = wave / S::WI;
     const Spot at = spot(n);
     const int f = at.f0 + wi * 16 * S::HALF + (lane >> 4) * 4 * S::HALF;
-    Raw<bf16, 8> up[3][S::HALF / 2];      // dh, asked for three rows ahead: 79 -> 75 us at 4096 x 1024 x 4096 (one wait a row before)
+    // dh, asked for three rows ahead (4096 x 1024 x 4096 75 us, 79 with a wait a row)
+    Raw<bf16, 8> up[3][S::HALF / 2];
     auto ask = [&](int j) {
       const int t = at.t0 + (wj * S::TJ + j) * 16 + (lane & 15);
       const bf16* dh = static_cast<const bf16*>(p.dh.p) + (size_t)at.b * p.dh.bs + (size_t)t * p.dh.ts + f;

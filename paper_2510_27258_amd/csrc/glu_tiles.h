@@ -165,7 +165,8 @@ __device__ __forceinline__ void tile_products(char* lds, int count, AT at, DONE 
     const bool first = i < S::LI, trans = first ? S::TRI : S::TRJ;
     const int n = first ? i : i - S::LI, left = length - step * 64 - (trans ? 2 * n : 0);
     // operands laid out alike have their k alike
-    load_to_lds(view(first ? from_i : from_j), (first || (S::TRI == S::TRJ && (!S::TRI || S::LI == S::LJ)) ? k_i : k_j) < left ? off[i] : kOutside,
+    constexpr bool kAlike = S::TRI == S::TRJ && (!S::TRI || S::LI == S::LJ);
+    load_to_lds(view(first ? from_i : from_j), (first || kAlike ? k_i : k_j) < left ? off[i] : kOutside,
                 base + (first ? wave * S::LI + n : S::BI / 8 + wave * S::LJ + n) * 2048 + buffer * 1024);
     if (i == S::LI - 1) from_i += ahead_i;
     if (i == S::LOADS - 1) from_j += ahead_j;
