@@ -117,7 +117,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gated_norm_back(GatedNorm a, flo
       ss[0] += v[e] * v[e];
     }
     row_sums<S, 1>(ss, red[turn][0]);
-    const float r = 1.f / sqrtf(ss[0] / a.d + a.eps);
+    // behind the last token 0: the rows there are zeros, and with eps = 0 an infinite r would make NaN of the weight's sums
+    const float r = there ? 1.f / sqrtf(ss[0] / a.d + a.eps) : 0.f;
     float dot[1] = {0.f};
 #pragma unroll
     for (int e = 0; e < S::E; ++e) {
