@@ -109,19 +109,22 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
   for (unsigned long long r0 = (unsigned long long)blockIdx.x * S::ROWS; r0 < rows;
        r0 += (unsigned long long)gridDim.x * S::ROWS, turn ^= 1) {
     const unsigned long long row = r0 + threadIdx.x / S::LANES;
-    const int d = row < rows ? a.D : 0;
-    const size_t here = row < rows ? (size_t)row * a.D : 0;
+    const bool there = row < rows;
+    const int d = there ? a.D : 0;
+    const size_t here = there ? (size_t)row * a.D : 0;
     if constexpr (!kAhead) load(r0);
     const RowRaw<TX, S, WHOLE> x = x1, gr = gr1;
     const RowRaw<T, S, WHOLE> y = y1, go = go1;
     if constexpr (kAhead) load(r0 + (unsigned long long)gridDim.x * S::ROWS);
+    // behind the last row both inverse roots are 0: those rows are zeros, and with eps = 0 infinite roots would make NaN
+    // of the weights' sums
     float ry = 1.f;
     if (a.post) {
       float ss[1] = {0.f};
 #pragma unroll
       for (int e = 0; e < S::E; ++e) ss[0] += y.at(e) * y.at(e);
       row_sums<S, 1>(ss, red[turn]);
-      ry = 1.f / sqrtf(ss[0] / a.D + a.eps);
+      ry = there ? 1.f / sqrtf(ss[0] / a.D + a.eps) : 0.f;
     }
     float r[S::E], dr[S::E], two[2] = {0.f, 0.f};
 #pragma unroll
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
       two[1] += go.at(e) * w[e] * r[e];
     }
     row_sums<S, 2>(two, red[turn] + 1);
-    const float rr = 1.f / sqrtf(two[0] / a.D + a.eps), mean = two[1] / a.D * rr;
+    const float rr = there ? 1.f / sqrtf(two[0] / a.D + a.eps) : 0.f, mean = two[1] / a.D * rr;
     float dot[1] = {0.f};
 #pragma unroll
     for (int e = 0; e < S::E; ++e) {
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(S::THREADS) void k_residual_norm_back(ResidualNorm 
       }
     }
     if constexpr (!kSums) {
-      if (lane == 0 && row < rows) stats[row] = make_float4(ry, rr, mean, 0.f);
+      if (lane == 0 && there) stats[row] = make_float4(ry, rr, mean, 0.f);
     }
     store_row<TX, S, WHOLE>(static_cast<TX*>(a.dx) + here, d, lane, dr);
     if (a.post) row_sums<S, 1>(dot, red[turn] + 3);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2510_27258_amd as hla
-from tests.test_gpu_block import TYPES, _gn_check, _rng, _say, _t
+from tests.test_gpu_block import TYPES, _gn_check, _rn_check, _rng, _say, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,24 @@ def test_gated_norm_without_eps(size, types, first):
         grads = hla.gated_norm_backward(y, z, w, g, 0.0, first)
         assert all(torch.isfinite(t.float()).all() for t in (out, *grads) if t is not None)
         _gn_check(y, z, w, 0.0, first, g, out, grads, form)
+
+
+RN_SIZES = [(1, 5, 64), (2, 1, 20), (1, 33, 100), (1, 7, 200), (1, 1, 333), (3, 1021, 333), (1, 3, 1000), (1, 3, 2048),
+            (1, 3, 9000)]
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("size", RN_SIZES)
+def test_residual_norm_without_eps(size, types):
+    for form in ("all", "weight", "scale", "no out", "no r"):
+        _say(f"residual norm {size} {types} {form}")
+        r = _rng(62, *size)
+        x, y, gr, go = (_t(r.standard_normal(size), t) for t in (types[0], types[1], types[0], types[1]))
+        w = _t(1 + 0.2 * r.standard_normal(size[-1]), types[1])
+        post = None if form in ("weight", "scale") else _t(1 + 0.2 * r.standard_normal(size[-1]), types[1])
+        scale = None if form == "weight" else _t(0.5 + 0.1 * r.standard_normal(size[-1]), types[1])
+        go, gr = None if form == "no out" else go, None if form == "no r" else gr
+        outs = hla.residual_norm_forward(x, y, w, post, scale, 0.5, 0.0)
+        grads = hla.residual_norm_backward(x, y, w, post, scale, go, gr, 0.5, 0.0)
+        assert all(torch.isfinite(t.float()).all() for t in (*outs, *grads) if t is not None)
+        _rn_check(x, y, w, post, scale, 0.5, 0.0, go, gr, outs, grads, form)
