@@ -216,29 +216,37 @@ __global__ __launch_bounds__(256) void k_gated_norm_sums(GatedNorm a, float* __r
 }
 
 constexpr int kSumRows = 64, kSumCols = 16;
+// Workgroups of a sum, at most: a launch has less than 2^32 threads a dimension, and one with more runs a part of them
+// without an error.  Wider sums take several turns of the same workgroups.
+constexpr int kSumBlocks = 65536;
 __global__ __launch_bounds__(kSumRows * kSumCols) void k_column_sums(ColumnSums c) {
   __shared__ float red[kSumRows][kSumCols];
-  const int cl = threadIdx.x % kSumCols, rg = threadIdx.x / kSumCols, col = blockIdx.x * kSumCols + cl;
+  const int cl = threadIdx.x % kSumCols, rg = threadIdx.x / kSumCols, apart = gridDim.x * kSumCols;
   void* to = c.to[blockIdx.y];
   if (!to) return;
   const float* part = c.part + (size_t)blockIdx.y * c.rows * c.cols;
-  float s = 0.f;
-  if (col < c.cols) {
-    constexpr int kAtOnce = 8;      // loads on their way together
-    for (int r0 = rg; r0 < c.rows; r0 += kSumRows * kAtOnce) {
-      float v[kAtOnce];
+  for (int c0 = blockIdx.x * kSumCols; c0 < c.cols; c0 += apart) {
+    const int col = c0 + cl;
+    float s = 0.f;
+    if (col < c.cols) {
+      constexpr int kAtOnce = 8;      // loads on their way together
+      for (int r0 = rg; r0 < c.rows; r0 += kSumRows * kAtOnce) {
+        float v[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-        v[k] = r0 + k * kSumRows < c.rows ? part[(size_t)(r0 + k * kSumRows) * c.cols + col] : 0.f;
+        for (int k = 0; k < kAtOnce; ++k)
+          v[k] = r0 + k * kSumRows < c.rows ? part[(size_t)(r0 + k * kSumRows) * c.cols + col] : 0.f;
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) s += v[k];
+        for (int k = 0; k < kAtOnce; ++k) s += v[k];
+      }
     }
+    red[rg][cl] = s;
+    __syncthreads();
+    if (rg == 0 && col < c.cols) {
+      for (int r = 1; r < kSumRows; ++r) s += red[r][cl];
+      store_any(to, c.dtype, col, s);
+    }
+    if (c.cols - c0 > apart) __syncthreads();      // another turn writes red again
   }
-  red[rg][cl] = s;
-  __syncthreads();
-  if (rg != 0 || col >= c.cols) return;
-  for (int r = 1; r < kSumRows; ++r) s += red[r][cl];
-  store_any(to, c.dtype, col, s);
 }
 
 // Sequences laid one behind the other are one long one: no division by n.
@@ -310,8 +318,9 @@ hipError_t by_type(const GatedNorm& a, bool back, float* part, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_column_sums(const ColumnSums& c, hipStream_t s) {
-  return HLA_TIMED("column_sums", k_column_sums, dim3((c.cols + kSumCols - 1) / kSumCols, 3), dim3(kSumRows * kSumCols), 0,
-                   s, c);
+  const int blocks = (c.cols + kSumCols - 1) / kSumCols;
+  return HLA_TIMED("column_sums", k_column_sums, dim3(blocks < kSumBlocks ? blocks : kSumBlocks, 3),
+                   dim3(kSumRows * kSumCols), 0, s, c);
 }
 
 hipError_t launch_gated_norm(const GatedNorm& a, hipStream_t s) { return by_type(a, false, nullptr, s); }

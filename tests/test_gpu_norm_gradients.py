@@ -1,7 +1,7 @@
-"""Gradients of the norms of a block where the tokens do not fill a workgroup's
-rows, without an eps that would hide what idle rows bring, against the oracle.
-Bars as in test_gpu_block.py: they hold for any eps, since rows of these random
-values are far from zero."""
+"""Gradients of the norms of a block: where the tokens do not fill a workgroup's
+rows, without an eps that would hide what idle rows bring, against the oracle;
+and weights wider than a launch.  Bars as in test_gpu_block.py: they hold for
+any eps, since rows of these random values are far from zero."""
 import pytest
 import torch
 
@@ -52,3 +52,27 @@ def test_residual_norm_without_eps(size, types):
         grads = hla.residual_norm_backward(x, y, w, post, scale, go, gr, 0.5, 0.0)
         assert all(torch.isfinite(t.float()).all() for t in (*outs, *grads) if t is not None)
         _rn_check(x, y, w, post, scale, 0.5, 0.0, go, gr, outs, grads, form)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_weights_of_many_groups(n):
+    """A weight for each of 8193 groups of 8192: more columns than one launch sums, 64 threads a column of fewer than
+    2^32.  Without a gate dweight is sum dout y / rms(y)."""
+    G, d = 8193, 8192
+    gen = torch.Generator("cuda").manual_seed(n)
+    y, g = (torch.randn(1, n, G, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(G, d, generator=gen, device="cuda").bfloat16()
+    _say(f"gated norm of {G} groups of {d}, {n} tokens")
+    dy, _, dw = hla.gated_norm_backward(y, None, w, g, 1e-3)
+    for at in (slice(0, 40), slice(4090, 4100), slice(G - 40, G)):
+        yd, gd, wd = y[0, :, at].double(), g[0, :, at].double(), w[at].double()
+        inv = (yd.square().mean(-1, keepdim=True) + 1e-3).rsqrt()
+        hat = yd * inv
+        ref = (gd * hat).sum(0)
+        off = (dw[at].double() - ref).abs() - 2.0 ** -8 * (1 + 2.0 ** -7) * ref.abs() - 1e-5 * (gd * hat).abs().sum(0)
+        assert off.max() <= 0
+        gw = gd * wd
+        ref = inv * (gw - hat * (gw * hat).mean(-1, keepdim=True))
+        size = inv * (gw.abs() + hat.abs() * (gw * hat).abs().mean(-1, keepdim=True))
+        off = (dy[0, :, at].double() - ref).abs() - 2.0 ** -8 * (1 + 2.0 ** -7) * ref.abs() - 1e-5 * size
+        assert off.max() <= 0
