@@ -107,7 +107,7 @@ def glr_vjp(x, f, g, decay, fb, gb, c, dy):
 
 
 # ----------------------------------------------------------------------------
-_erf = np.vectorize(math.erf, otypes=[float])
+_erfc = np.vectorize(math.erfc, otypes=[float])
 
 
 def act(p, kind):
@@ -115,7 +115,7 @@ def act(p, kind):
     if kind == "silu":
         s = sigmoid(p)
         return p * s, s * (1 + p * (1 - s))
-    phi = 0.5 * (1 + _erf(p / math.sqrt(2)))
+    phi = 0.5 * _erfc(-p / math.sqrt(2))      # 1 + erf would lose what is left far below zero
     return p * phi, phi + p * np.exp(-0.5 * p * p) / math.sqrt(2 * math.pi)
 
 
