@@ -549,9 +549,10 @@ int hla_residual_norm_backward(const void *x, long long x_bs, long long x_ts, co
  * [D]; y [B, n, D] of dtype.  state (optional) fp32 [B, D]: the state before
  * the first token, replaced by that after the last; without it zeros.  kept
  * (optional): hla_glr_kept_bytes(...) bytes for what the gradients need of the
- * forward.  c finite and >= 0, D and the
- * strides between tokens at most 2^21.  An infinite or NaN input leaves the
- * outputs of its channel from its token on infinite or NaN, and no other.
+ * forward.  c finite and >= 0, D and the strides between tokens at most 2^21.
+ * An infinite or NaN x or state, or a NaN f or g, leaves the outputs of its
+ * channel from its token on infinite or NaN, and no other.  An infinite f or g
+ * shuts or opens its gate: the outputs take the formula's limit.
  * workspace: at least hla_glr_workspace_bytes(...) bytes. */
 size_t hla_glr_workspace_bytes(int B, int n, int D);
 size_t hla_glr_kept_bytes(int B, int n, int D);
@@ -580,8 +581,9 @@ int hla_glr_backward(const void *x, long long x_bs, long long x_ts, const void *
 /* hla_glu_forward — gated feed-forward projections
  *   h = act(x w_gate^T) * (x w_up^T),  act SiLU or GELU (by the error function)
  * x [B, n, D], w_gate, w_up [F, D], h [B, n, F], all bf16 (dtype = HLA_BF16;
- * fp32 returns HLA_ERR_UNSUPPORTED), sums in fp32, rounded once.  D and F are
- * multiples of 8, at most 2^20; addresses and strides whole 16-byte pieces. */
+ * fp32 returns HLA_ERR_UNSUPPORTED), sums in fp32, rounded once; GELU far below
+ * zero is within 2e-5 of itself before that, down to x w_gate^T = -13.  D and F
+ * are multiples of 8, at most 2^20; addresses and strides whole 16-byte pieces. */
 int hla_glu_forward(const void *x, long long x_bs, long long x_ts, const void *w_gate, const void *w_up, void *h,
                     int B, int n, int D, int F, int act, int dtype, void *stream);
 

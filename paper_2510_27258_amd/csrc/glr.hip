@@ -16,9 +16,9 @@
 // segments: a first launch brings each segment's A and H (or, backwards, its
 // effect on l), and every segment of the second joins what lies before it.
 // Bound by vector instructions (six exponentials, roots and quotients a value, at a
-// quarter of the rate) and by the loads in flight of one workgroup a CU: 4 x 4096 x
-// 2048 in bf16 82 us, 3.3 TB/s, vector instructions 63 % of the time; gradients 128
-// us, 3.7 TB/s, 75 %.
+// quarter of the rate) and by the loads in flight of one workgroup a CU, two waves a
+// SIMD: 4 x 4096 x 2048 in bf16 82 us, 3.3 TB/s, vector instructions 63 % of the
+// time; gradients 128 us, 3.7 TB/s, 75 %.  In fp32 125 and 214 us.
 // 1 - a^2 is taken as -expm1(2 L): a state that keeps 0.999 of itself a token
 // would lose ten bits of it to the difference.
 #include <cmath>
@@ -636,13 +636,15 @@ bool pairs(const Glr& p) {
 }
 
 // Runs and waves of the two walks, and segments at most.  Measured: the backward walk of 4 x 4096 x 2048 with runs of
-// 4 in 8 waves 127 us, of 8 in 4 waves 142, of 8 in 8 waves 215 (registers).
+// 4 in 8 waves 127 us, of 8 in 4 waves 142, of 8 in 8 waves 215 (registers).  The forward's were not compared by figures.
 constexpr int kFwdS = 16, kFwdW = 8, kBackS = 4, kBackW = 8, kBackLpr = 16;
 constexpr int kMostSegs = 32;
 
 // One launch of `groups` workgroups of `per` tiles each, in us: in rounds of one
 // workgroup a CU, a tile `empty` on an empty chip and `full` where every CU has one;
-// a launch takes 2 and a round's start 2.
+// a launch takes 2 and a round's start 2.  So it is for pairs of channels, which the
+// constants were measured with.  Single channels (118 registers at most) fit two
+// workgroups a CU and are cut by the same rule, without figures of their own.
 float launch_time(long long groups, int per, float empty, float full) {
   const float load = groups < 256 ? groups / 256.f : 1.f;
   return 2.f + (float)((groups + 255) / 256) * (2.f + per * (empty + (full - empty) * load));
